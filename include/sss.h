@@ -80,6 +80,11 @@ typedef enum {
                                    sss_gemm_noalloc), sss_quantize or
                                    sss_quantize_rotated expired; the output is
                                    incomplete                                         */
+#define SSS_FLAG_INDEX 0x8u     /* sss_page_plan, sss_qk_norm_rope, sss_attention: a length,
+                                   position, slot or page lies outside what the call's
+                                   arguments allow; what the calls do then is said there */
+#define SSS_FLAG_PAGES 0x10u    /* sss_page_plan: the free pages, or the table's columns, do
+                                   not suffice                                         */
 
 typedef enum { SSS_OUT_F32 = 0, SSS_OUT_F16 = 1, SSS_OUT_BF16 = 2 } sss_dtype_t;
 
@@ -389,6 +394,168 @@ sss_status_t sss_quantize_lsq(const float* w, const sss_qtensor_t* out, int32_t 
 sss_status_t sss_sign_diagnostics(const float* w, int64_t n, int64_t k, int32_t q,
                                   int32_t group, int16_t* margin, double* gain,
                                   uint64_t* hist, uint32_t* dev_status, void* stream);
+
+/*
+ * Between a layer's {q, k, v} projection and its o_proj: a paged key/value
+ * cache, what fills it and the attention that reads it.  The paper's path ends
+ * at the projections (the weights are what it quantizes); these calls take
+ * sss_gemm_multi's or sss_gemv's fp32 outputs to the bf16 activations that the
+ * next projection reads.
+ *
+ * The cache of a layer is a matrix of slots, a slot per token: slot s holds the
+ * token's keys (and values) of every key/value head.  A page is page_size
+ * consecutive slots; request b's token at position p lies in slot
+ * block_table[b][p / page_size] * page_size + p % page_size.
+ */
+typedef struct {
+  void* k;           /* [slots][heads][dim], slots `stride` elements apart                 */
+  void* v;           /* as k                                                               */
+  int64_t slots;     /* 0 .. 2^31 - 1                                                      */
+  int64_t stride;    /* >= heads * dim and a multiple of 8 (heads * dim where it is dense) */
+  int32_t page_size; /* 16, 32, 64, 128 or 256 with a block table; else ignored            */
+  int32_t heads;     /* key/value heads, 1 ..                                              */
+  int32_t dim;       /* 64 or 128                                                          */
+  int32_t dtype;     /* SSS_OUT_F16 or SSS_OUT_BF16                                        */
+} sss_kv_cache_t;
+
+/*
+ * sss_page_plan -- a step's pages and slots from its requests' lengths: request
+ * b holds the pages of past[b] tokens and gets fresh[b] new ones.  The
+ * ceil((past + fresh) / page_size) - ceil(past / page_size) pages that it lacks
+ * are taken from the front of free_pages, requests in order, and entered in its
+ * row of the block table.  One launch; nothing is read back.
+ *   past, fresh  [in]  device int32 [batch], >= 0.
+ *   page_size    [in]  16, 32, 64, 128 or 256.
+ *   free_pages   [in]  device int32 [free_count]: pages that no request holds.
+ *   block_table  [in,out] device int32 [batch][table_width]: entries below
+ *                      ceil(past / page_size) are read, the taken pages' written,
+ *                      others left alone.
+ *   cu_q         [out] device int32 [batch + 1]: the first token of each request
+ *                      among the step's, and their number.
+ *   kv_len       [out] device int32 [batch]: past + fresh.
+ *   positions    [out] device int32 [tokens]: each new token's position.
+ *   slots        [out] device int32 [tokens]: its slot.  Rows past the step's
+ *                      tokens get position 0 and slot -1 (a buffer may be larger
+ *                      than the step, as in a captured graph).
+ *   used         [out] device int32: how many of free_pages were taken.
+ *   dev_status   [out] nullable.  SSS_FLAG_PAGES: free pages or table columns do
+ *                      not suffice; the tokens without a page get slot -1 (and
+ *                      the table -1).  SSS_FLAG_INDEX: a length is negative
+ *                      (taken as 0), the new tokens are more than `tokens` (cu_q
+ *                      ends there), or an entry of a held page is not one (slot
+ *                      -1).
+ * Errors: SSS_E_ARG, SSS_E_ALIGN, SSS_E_CUDA.
+ */
+sss_status_t sss_page_plan(const int32_t* past, const int32_t* fresh, int32_t batch,
+                           int32_t page_size, const int32_t* free_pages, int32_t free_count,
+                           int32_t* block_table, int32_t table_width, int32_t* cu_q,
+                           int32_t* kv_len, int32_t* positions, int32_t* slots,
+                           int64_t tokens, int32_t* used, uint32_t* dev_status,
+                           void* stream);
+
+#define SSS_ROPE_HALF 0  /* pairs (i, i + rot_dim / 2) */
+#define SSS_ROPE_PAIRS 1 /* pairs (2i, 2i + 1)         */
+
+/* The rotation of a model's heads, and their norm if it has one. */
+typedef struct {
+  const float* cos;    /* device fp32 [max_pos][rot_dim / 2]                             */
+  const float* sin;    /* as cos                                                         */
+  const float* q_norm; /* nullable device fp32 [dim]: the weights of the query heads' norm */
+  const float* k_norm; /* nullable, of the key heads'                                    */
+  int64_t max_pos;
+  int32_t rot_dim;     /* values of a head that are rotated, from its first: 0 .. dim, a
+                          multiple of 8                                                  */
+  int32_t style;       /* SSS_ROPE_HALF or SSS_ROPE_PAIRS                                */
+  float eps;           /* >= 0                                                           */
+} sss_rope_t;
+
+/*
+ * sss_qk_norm_rope -- per head x of q and k: y = x / sqrt(mean(x^2) + eps) * w
+ * (where the norm's weights are given), then each pair (a, b) of y's first
+ * rot_dim values turned by the token's angle i: (a cos_i - b sin_i, b cos_i + a
+ * sin_i).  q is rounded to q_out, k and the unchanged v to the token's slot of
+ * the cache.  fp32 arithmetic, one rounding.
+ *   q, k, v    [in]  device [tokens][heads * dim] and [tokens][cache->heads * dim]
+ *                    of in_dtype (sss_dtype_t; fp32 is what the projections
+ *                    write), rows q_stride, k_stride and v_stride elements apart
+ *                    (multiples of 4: the three may be columns of one matrix);
+ *                    16-byte aligned (16-bit types: 8).
+ *   heads      [in]  query heads, any number.
+ *   rope       [in]  16-byte aligned arrays; cos and sin may be NULL at rot_dim 0.
+ *   positions  [in]  device int32 [tokens] (may be NULL at rot_dim 0).
+ *   q_out      [out] device [tokens][heads][dim] of the cache's dtype, dense,
+ *                    16-byte aligned.
+ *   cache      [in]  written at the tokens' slots.
+ *   slots      [in]  device int32 [tokens], no two alike; negative: the token's
+ *                    key and value are not kept.  NULL: token t's slot is t (a
+ *                    prompt whose keys are packed as its tokens are).
+ *   dev_status [out] nullable.  SSS_FLAG_INDEX: a slot past the cache (not
+ *                    written), or a position outside 0 .. max_pos - 1 (the
+ *                    nearest is taken).
+ * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim), SSS_E_ALIGN, SSS_E_CUDA.
+ */
+sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, int32_t in_dtype,
+                              int64_t tokens, int32_t heads, const sss_rope_t* rope,
+                              const int32_t* positions, void* q_out,
+                              const sss_kv_cache_t* cache, const int32_t* slots,
+                              uint32_t* dev_status, void* stream);
+
+/*
+ * sss_attention -- causal attention of each request's new tokens over its keys
+ * and values: with n new tokens (cu_q[b] .. cu_q[b + 1] - 1) and kv_len[b] keys,
+ * token i sees keys 0 .. kv_len - n + i, and
+ *   o_i = sum_j p_ij v_j / sum_j p_ij,  p_ij = exp(scale q_i.k_j - max_j).
+ * A whole prompt (kv_len = n), a chunk of one after what the cache holds, a
+ * single token (n = 1) and drafted ones are the same call, and a batch may mix
+ * them.  Query head h reads key/value head h / (heads / cache->heads).  A row
+ * that sees no key is zero.  Scores, sums and outputs are held in fp32; p_ij is
+ * rounded to the cache's type for its product with v_j (relative to a maximum
+ * that may lie 8 powers of two below the row's own), the output once.
+ * Keys and values that a row does not see have no part in it, whatever they
+ * hold (infinities and NaN among them); what lies in the cache past kv_len is
+ * never used.
+ *   q           [in]  device [tokens][heads][dim] of the cache's dtype, rows
+ *                     q_stride elements apart (a multiple of 8, >= heads * dim);
+ *                     16-byte aligned.
+ *   heads       [in]  a multiple of cache->heads.
+ *   cache       [in]  k and v 16-byte aligned.
+ *   cu_q        [in]  device int32 [batch + 1], cu_q[batch] <= tokens.  Rows of no
+ *                     request are not written.
+ *   kv_len      [in]  device int32 [batch].
+ *   block_table [in]  device int32 [batch][table_width], or NULL: key j of request
+ *                     b lies in slot cu_q[b] + j (keys packed as the queries;
+ *                     kv_len may then be NULL: the request's new tokens).
+ *   max_q, max_kv [in] bounds of a request's new tokens and keys; what is near
+ *                     them is faster.
+ *   scale       [in]  > 0, finite.
+ *   out         [out] device [tokens][heads][dim] of the cache's dtype, dense,
+ *                     16-byte aligned (bf16: the x_bf16 of the o_proj).
+ *   workspace   [in]  device scratch of ws_bytes >=
+ *                     sss_attention_workspace_bytes(...) bytes, 16-byte aligned,
+ *                     or NULL when that size is 0.  Contents on entry are ignored.
+ *   dev_status  [out] nullable.  SSS_FLAG_INDEX: cu_q, kv_len or the table point
+ *                     outside what they may (a request past `tokens` is left
+ *                     out, lengths are cut to max_q, max_kv, the table's width or
+ *                     the request's own rows, a page that is none reads as zeros).
+ * The result does not depend on timing, and a request's not on the others in the
+ * batch but through max_q, max_kv and their number, by which the work is split.
+ * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim), SSS_E_ALIGN, SSS_E_WORKSPACE,
+ * SSS_E_CUDA.
+ */
+sss_status_t sss_attention(const void* q, int64_t q_stride, int32_t heads,
+                           const sss_kv_cache_t* cache, const int32_t* cu_q,
+                           const int32_t* kv_len, const int32_t* block_table,
+                           int32_t table_width, int32_t batch, int64_t tokens,
+                           int32_t max_q, int64_t max_kv, float scale, void* out,
+                           void* workspace, size_t ws_bytes, uint32_t* dev_status,
+                           void* stream);
+
+/* Workspace bytes of that call (0 for invalid arguments, or if none are needed:
+ * partial results where keys are split over CTAs). */
+size_t sss_attention_workspace_bytes(int64_t tokens, int32_t heads,
+                                     const sss_kv_cache_t* cache, int32_t batch,
+                                     int32_t max_q, int64_t max_kv);
 
 #define SSS_OP_GEMV 0
 #define SSS_OP_GEMM 1

@@ -1,0 +1,486 @@
+// attn_rows.cu -- attention of few rows: the single tokens (or a few drafted ones)
+// of a decode step over the paged cache, and the joining of partial results.
+//
+//   o_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c q_i.k_j - m_i),  c = scale log2(e)
+//
+// Bound by HBM: every key and value is read once, for group x 2 operations a byte.
+// So the matrix products run on mma.sync (m16n8k16; 16 or 32 rows of tokens x
+// heads, at a fraction of its rate), and everything else serves the loads: each of
+// the CTA's four warps streams its own steps of 16 keys and 16 values through a
+// private ring of cp.async copies, without a barrier in the loop, and keeps a
+// running maximum m, sum and fp32 output of its own; they meet once, at the end.
+// 16 keys never leave a page, so a step's rows have one base address; 32 steps'
+// table entries are read ahead, one per lane.
+// m is raised only where a score passes it by 8 (then 2^8 at most enters the
+// 16-bit p, in range): the outputs are rescaled seldom and the warp votes on it
+// without first reducing its maxima.
+#include <algorithm>
+
+#include "attn.cuh"
+
+namespace sss {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStep = 16;   // keys of a warp's step
+constexpr int kStages = 3;  // steps in a warp's ring
+constexpr float kRaise = 8.0f;
+
+template <int D>
+struct RowsSmem {
+  static constexpr int TILE = kStep * D * 2;             // 16 keys (or values)
+  static constexpr int RING = kStages * 2 * TILE;        // of a warp
+  static constexpr int TOTAL = kWarps * RING;
+};
+
+__device__ __forceinline__ uint32_t smem_addr(const void* p) {
+  return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool in) {
+  const int bytes = in ? 16 : 0;  // the rest is filled with zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t (&r)[4], uint32_t addr) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr)
+               : "memory");
+}
+template <typename T>
+__device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], uint32_t b0,
+                                         uint32_t b1) {
+  if constexpr (std::is_same<T, __half>::value)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+        "{%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// MT tiles of 16 rows
+template <typename T, int D, int MT>
+__global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_constant__ AttnArgs a) {
+  using S = RowsSmem<D>;
+  constexpr int R = 16 * MT;
+  constexpr int CH = D / 8;       // 16-byte pieces of a row
+  constexpr int KD = D / 16;      // mma steps along d
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ float wmax[kWarps][R], wsum[kWarps][R];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  // this CTA's work
+  const int z = blockIdx.x % a.nsplit;
+  const int hx = (blockIdx.x / a.nsplit) % (a.kv_heads * a.hchunks);
+  const int tile = blockIdx.x / (a.nsplit * a.kv_heads * a.hchunks);
+  const int kh = hx / a.hchunks, g0 = hx % a.hchunks * a.hpt;
+  const int nh = min(a.hpt, a.group - g0);  // heads of the tile
+  int b, i0;
+  if (!attn_tile(a, tile, b, i0)) return;
+  uint32_t flags = 0;
+  const AttnRequest rq = attn_request(a, b, flags);
+  const int nt = min(a.tpt, rq.n - i0);  // tokens of the tile
+  if (nt <= 0) {
+    if (flags && a.status && threadIdx.x == 0) atomicOr(a.status, flags);
+    return;
+  }
+  const int lim0 = attn_limit(rq, i0), lim1 = attn_limit(rq, i0 + nt - 1);
+  const int k0 = z * a.chunk, k1 = min(lim1, k0 + a.chunk);
+  if (k0 >= k1 && z > 0) return;
+  const int steps = (max(k1 - k0, 0) + kStep - 1) / kStep;
+
+  // the rows' queries as mma operands, and how many keys each row sees
+  uint32_t qf[MT][KD][4];
+  int lim[MT][2];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = 16 * m + 8 * e + (lane >> 2);
+      const int i = row / a.hpt, g = row - i * a.hpt;
+      const bool in = i < nt && g < nh;
+      lim[m][e] = in ? attn_limit(rq, i0 + i) : 0;
+      const T* src = static_cast<const T*>(a.q) + (rq.q0 + i0 + (in ? i : 0)) * a.q_stride +
+                     (kh * a.group + g0 + (in ? g : 0)) * D + 2 * (lane & 3);
+#pragma unroll
+      for (int kk = 0; kk < KD; ++kk) {
+        qf[m][kk][e] = in ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * kk)) : 0u;
+        qf[m][kk][2 + e] = in ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * kk + 8)) : 0u;
+      }
+    }
+
+  // The warp's steps: warp, warp + 4, ... of the split's.  Lane l keeps the table
+  // entry of the warp's step 32 n + l.
+  const int mine = warp < steps ? (steps - warp + kWarps - 1) / kWarps : 0;
+  const int32_t* table = a.table ? a.table + static_cast<int64_t>(b) * a.table_width : nullptr;
+  int page = 0;
+  unsigned char* ring = smem + warp * S::RING;
+  const uint32_t ring_addr = smem_addr(ring);
+  const int64_t row_bytes = a.kv_stride * 2;
+  auto issue = [&](int s) {
+    if (s < mine) {
+      if (table && (s & 31) == 0) {
+        const int ahead = s + lane;
+        const int key = k0 + kStep * (warp + kWarps * ahead);
+        page = ahead < mine ? __ldg(table + (key >> a.page_shift)) : 0;
+      }
+      const int key = k0 + kStep * (warp + kWarps * s);
+      int64_t slot = rq.q0 + key;
+      if (table) slot = attn_slot(a, __shfl_sync(0xffffffffu, page, s & 31), key);
+      if (slot < 0) flags |= SSS_FLAG_INDEX;
+      const uint32_t dst = ring_addr + (s % kStages) * 2 * S::TILE;
+      const int64_t at = (slot < 0 ? 0 : slot) * row_bytes + kh * D * 2;
+      const char* ksrc = static_cast<const char*>(a.k) + at;
+      const char* vsrc = static_cast<const char*>(a.v) + at;
+#pragma unroll
+      for (int i = 0; i < kStep * CH / 32; ++i) {
+        const int row = (lane + 32 * i) / CH, c = (lane + 32 * i) % CH;
+        const bool in = slot >= 0 && key + row < k1;
+        const int64_t off = in ? row * row_bytes + c * 16 : 0;
+        const uint32_t to = dst + row * (D * 2) + ((c ^ (row & 7)) * 16);
+        copy16(to, ksrc + off, in);
+        copy16(to + S::TILE, vsrc + off, in);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+
+  float o[MT][D / 8][4];
+  float mx[MT][2], sum[MT][2];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      mx[m][e] = -INFINITY;
+      sum[m][e] = 0.f;
+    }
+#pragma unroll
+    for (int n = 0; n < D / 8; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[m][n][i] = 0.f;
+  }
+
+  for (int s = 0; s < kStages - 1; ++s) issue(s);
+  for (int s = 0; s < mine; ++s) {
+    issue(s + kStages - 1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+    __syncwarp();
+    const uint32_t kt = ring_addr + (s % kStages) * 2 * S::TILE, vt = kt + S::TILE;
+    const int key0 = k0 + kStep * (warp + kWarps * s);
+
+    // scores: two tiles of 8 keys
+    float sc[MT][2][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[m][n][i] = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < KD; ++kk) {
+      const int row = (lane & 7) + ((lane >> 4) << 3), c = 2 * kk + ((lane >> 3) & 1);
+      uint32_t kf[4];
+      ldsm4(kf, kt + row * (D * 2) + ((c ^ (row & 7)) * 16));
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        mma16816<T>(sc[m][0], qf[m][kk], kf[0], kf[1]);
+        mma16816<T>(sc[m][1], qf[m][kk], kf[2], kf[3]);
+      }
+    }
+    // scale, mask, and raise the maxima where a score passes them by much
+    bool raise = false;
+    const bool cut = key0 + kStep > lim0;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = sc[m][n][i] * a.scale_log2;
+          if (cut && key0 + 8 * n + 2 * (lane & 3) + (i & 1) >= lim[m][i >> 1]) x = -INFINITY;
+          sc[m][n][i] = x;
+          raise = raise || x > mx[m][i >> 1] + kRaise;
+        }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float t = fmaxf(fmaxf(sc[m][0][2 * e], sc[m][0][2 * e + 1]),
+                          fmaxf(sc[m][1][2 * e], sc[m][1][2 * e + 1]));
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
+          t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
+          t = fmaxf(t, mx[m][e]);
+          const float f = t == -INFINITY ? 1.f : ex2(mx[m][e] - t);
+          mx[m][e] = t;
+          sum[m][e] *= f;
+#pragma unroll
+          for (int n = 0; n < D / 8; ++n) {
+            o[m][n][2 * e] *= f;
+            o[m][n][2 * e + 1] *= f;
+          }
+        }
+    }
+    uint32_t pf[MT][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) {
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float ref = mx[m][i >> 1];
+          const float p = ex2(sc[m][n][i] - (ref == -INFINITY ? 0.f : ref));
+          sc[m][n][i] = p;
+          sum[m][i >> 1] += p;
+        }
+      pf[m][0] = Pair<T>::pack(sc[m][0][0], sc[m][0][1]);
+      pf[m][1] = Pair<T>::pack(sc[m][0][2], sc[m][0][3]);
+      pf[m][2] = Pair<T>::pack(sc[m][1][0], sc[m][1][1]);
+      pf[m][3] = Pair<T>::pack(sc[m][1][2], sc[m][1][3]);
+    }
+    // A value that is infinite or NaN reaches the rows that see its key and no
+    // other: 0 x NaN would reach all.  Where a step's keys are not seen by every
+    // row, such values are added by hand and leave the tile.
+    if (cut && lim0 < lim1) {
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < kStep * CH / 32; ++i) {
+        uint32_t w[4];
+        const uint32_t at = vt + (lane + 32 * i) * 16;
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                     : "r"(at)
+                     : "memory");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) odd = odd || pair_nonfinite<T>(w[j]);
+      }
+      if (__any_sync(0xffffffffu, odd)) {
+        for (int key = 0; key < kStep; ++key) {
+          const int from = (lane & ~3) | ((key & 7) >> 1);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            float pk[2];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float lo = (key & 1) ? sc[m][0][2 * e + 1] : sc[m][0][2 * e];
+              const float hi = (key & 1) ? sc[m][1][2 * e + 1] : sc[m][1][2 * e];
+              pk[e] = __shfl_sync(0xffffffffu, key < 8 ? lo : hi, from);
+            }
+#pragma unroll
+            for (int n = 0; n < D / 8; ++n) {
+              uint32_t w;
+              const uint32_t at = vt + key * (D * 2) + ((n ^ (key & 7)) * 16) + 4 * (lane & 3);
+              asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+#pragma unroll
+              for (int x = 0; x < 2; ++x) {
+                const uint16_t bits = static_cast<uint16_t>(x ? w >> 16 : w & 0xFFFFu);
+                if ((bits & Pair<T>::kExp) != Pair<T>::kExp) continue;
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  if (key0 + key < lim[m][e]) o[m][n][2 * e + x] += pk[e] * Pair<T>::value(bits);
+              }
+            }
+          }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kStep * CH / 32; ++i) {
+          unsigned char* at = ring + (s % kStages) * 2 * S::TILE + S::TILE + (lane + 32 * i) * 16;
+          uint16_t* v16 = reinterpret_cast<uint16_t*>(at);
+          for (int j = 0; j < 8; ++j)
+            if ((v16[j] & Pair<T>::kExp) == Pair<T>::kExp) v16[j] = 0;
+        }
+        __syncwarp();
+      }
+    }
+#pragma unroll
+    for (int n2 = 0; n2 < D / 16; ++n2) {
+      const int row = lane & 15, c = 2 * n2 + (lane >> 4);
+      uint32_t vf[4];
+      ldsm4_t(vf, vt + row * (D * 2) + ((c ^ (row & 7)) * 16));
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        mma16816<T>(o[m][2 * n2], pf[m], vf[0], vf[1]);
+        mma16816<T>(o[m][2 * n2 + 1], pf[m], vf[2], vf[3]);
+      }
+    }
+    __syncwarp();  // the stage is read; the next issue may overwrite it
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  if (flags && a.status) atomicOr(a.status, flags);
+
+  // join the warps
+  constexpr int LD = D + 4;  // (rows' lanes in distinct banks)
+  static_assert(kWarps * R * LD * 4 <= S::TOTAL, "the partial outputs reuse the rings");
+  float* part = reinterpret_cast<float*>(smem);
+  __syncthreads();
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = 16 * m + 8 * e + (lane >> 2);
+      float t = sum[m][e];
+      t += __shfl_xor_sync(0xffffffffu, t, 1);
+      t += __shfl_xor_sync(0xffffffffu, t, 2);
+      if ((lane & 3) == 0) {
+        wmax[warp][row] = mx[m][e];
+        wsum[warp][row] = t;
+      }
+      float* dst = part + (warp * R + row) * LD + 2 * (lane & 3);
+#pragma unroll
+      for (int n = 0; n < D / 8; ++n)
+        *reinterpret_cast<float2*>(dst + 8 * n) = make_float2(o[m][n][2 * e], o[m][n][2 * e + 1]);
+    }
+  __syncthreads();
+  const bool alone = lim1 <= a.chunk;  // the tile has no other split
+  for (int x = threadIdx.x; x < R * (D / 4); x += kThreads) {
+    const int row = x / (D / 4), d = 4 * (x % (D / 4));
+    const int i = row / a.hpt, g = row - i * a.hpt;
+    if (i >= nt || g >= nh) continue;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, wmax[w][row]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = ex2(wmax[w][row] - ref);
+      if (f == 0.f && wsum[w][row] == 0.f) continue;  // (a warp without keys)
+      const float4 v = *reinterpret_cast<const float4*>(part + (w * R + row) * LD + d);
+      total += f * wsum[w][row];
+      acc.x += f * v.x;
+      acc.y += f * v.y;
+      acc.z += f * v.z;
+      acc.w += f * v.w;
+    }
+    const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
+    acc = make_float4(acc.x * r, acc.y * r, acc.z * r, acc.w * r);
+    const int64_t at =
+        static_cast<int64_t>(rq.q0 + i0 + i) * a.heads + kh * a.group + g0 + g;
+    if (alone) {
+      const uint2 u = make_uint2(Pair<T>::pack(acc.x, acc.y), Pair<T>::pack(acc.z, acc.w));
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
+    } else {
+      const int64_t zat = static_cast<int64_t>(z) * a.tokens * a.heads + at;
+      *reinterpret_cast<float4*>(a.part + zat * D + d) = acc;
+      if (d == 0) a.part_lse[zat] = total == 0.f ? -INFINITY : top + log2f(total);
+    }
+  }
+}
+
+// The rows whose tile has more than one split: the splits' outputs, weighted by
+// 2^lse, in split order.  A warp per row.
+template <typename T, int D>
+__global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ AttnArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int lane = threadIdx.x & 31;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
+  const int64_t rows = static_cast<int64_t>(a.tokens) * a.heads;
+  if (row >= rows) return;
+  const int t = static_cast<int>(row / a.heads);
+  // the token's request: the last whose first token is not behind it
+  int lo = 0, hi = a.batch;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a.cu_q[mid] <= t) lo = mid;
+    else hi = mid;
+  }
+  uint32_t flags = 0;
+  const AttnRequest rq = attn_request(a, lo, flags);
+  const int i = t - rq.q0;
+  if (i < 0 || i >= rq.n) return;
+  const int last = min(i / a.tpt * a.tpt + a.tpt, rq.n) - 1;
+  const int lim = attn_limit(rq, last);
+  if (lim <= a.chunk) return;
+  const int n = (lim + a.chunk - 1) / a.chunk;
+  float top = -INFINITY;
+  for (int z = lane; z < n; z += 32) top = fmaxf(top, a.part_lse[z * rows + row]);
+#pragma unroll
+  for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+  const float ref = top == -INFINITY ? 0.f : top;
+  constexpr int PER = D / 32;
+  float acc[PER], total = 0.f;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) acc[j] = 0.f;
+  for (int z = 0; z < n; ++z) {
+    const float lse = a.part_lse[z * rows + row];
+    if (lse == -INFINITY) continue;
+    const float f = ex2(lse - ref);
+    total += f;
+    const float* src = a.part + (z * rows + row) * D + lane * PER;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) acc[j] += f * src[j];
+  }
+  const float r = total == 0.f ? 0.f : 1.f / total;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + row * D + lane * PER);
+#pragma unroll
+  for (int j = 0; j < PER; j += 2) dst[j / 2] = Pair<T>::pack(acc[j] * r, acc[j + 1] * r);
+}
+
+template <typename K>
+cudaError_t launch(K kern, const AttnArgs& a, int64_t blocks, int threads, int smem,
+                   cudaStream_t stream) {
+  if (blocks > INT32_MAX) return cudaErrorNotSupported;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+template <typename T, int D, int MT>
+cudaError_t run_rows(const AttnArgs& a, cudaStream_t stream) {
+  auto kern = attn_rows_kernel<T, D, MT>;
+  cudaError_t e = ensure_smem(kern, RowsSmem<D>::TOTAL);
+  if (e != cudaSuccess) return e;
+  const int64_t blocks = static_cast<int64_t>(a.tiles) * a.kv_heads * a.hchunks * a.nsplit;
+  return launch(kern, a, blocks, kThreads, RowsSmem<D>::TOTAL, stream);
+}
+template <typename T>
+cudaError_t rows_dim(const AttnArgs& a, int dim, int mt, cudaStream_t stream) {
+  if (dim == 64) return mt == 1 ? run_rows<T, 64, 1>(a, stream) : run_rows<T, 64, 2>(a, stream);
+  return mt == 1 ? run_rows<T, 128, 1>(a, stream) : run_rows<T, 128, 2>(a, stream);
+}
+template <typename T>
+cudaError_t join_dim(const AttnArgs& a, int dim, cudaStream_t stream) {
+  const int64_t blocks = (static_cast<int64_t>(a.tokens) * a.heads + 3) / 4;
+  return dim == 64 ? launch(attn_join_kernel<T, 64>, a, blocks, 128, 0, stream)
+                   : launch(attn_join_kernel<T, 128>, a, blocks, 128, 0, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_attn_rows(const AttnArgs& a, int dtype, int dim, int row_tiles16,
+                             cudaStream_t stream) {
+  return dtype == SSS_OUT_F16 ? rows_dim<__half>(a, dim, row_tiles16, stream)
+                              : rows_dim<__nv_bfloat16>(a, dim, row_tiles16, stream);
+}
+cudaError_t launch_attn_join(const AttnArgs& a, int dtype, int dim, cudaStream_t stream) {
+  return dtype == SSS_OUT_F16 ? join_dim<__half>(a, dim, stream)
+                              : join_dim<__nv_bfloat16>(a, dim, stream);
+}
+
+}  // namespace sss

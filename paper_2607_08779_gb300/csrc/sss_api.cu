@@ -25,6 +25,9 @@ void set_error(const char* what, cudaError_t e) {
 // GEMM's token-tile grid dimension inside its 65535 limit
 constexpr int64_t kMaxDim = int64_t{1} << 31;
 constexpr int64_t kMaxTokens = int64_t{1} << 24;
+// the most heads and requests of an attention: its grid stays far inside int64
+constexpr int32_t kMaxHeads = 1 << 16;
+constexpr int32_t kMaxBatch = 1 << 20;
 
 bool aligned(const void* p, size_t a) {
   return (reinterpret_cast<uintptr_t>(p) % a) == 0;
@@ -444,6 +447,132 @@ sss_status_t sss_quantize_act_q8(const uint16_t* x_bf16, int64_t rows, int64_t k
   if (dev_status && !aligned(dev_status, 4)) return SSS_E_ALIGN;
   return finish("sss_quantize_act_q8",
                 launch_act_q8(x_bf16, rows, k, q, d, dev_status, static_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+bool page_size_ok(int32_t p) { return p == 16 || p == 32 || p == 64 || p == 128 || p == 256; }
+
+// a cache that calls may address: rows of `stride` elements from 16-byte
+// aligned bases
+sss_status_t check_cache(const sss_kv_cache_t* c) {
+  if (c == nullptr) return SSS_E_ARG;
+  if (c->dtype != SSS_OUT_F16 && c->dtype != SSS_OUT_BF16) return SSS_E_ARG;
+  if (c->dim != 64 && c->dim != 128) return c->dim < 1 ? SSS_E_ARG : SSS_E_UNSUPPORTED;
+  if (c->heads < 1 || c->heads > kMaxHeads || c->slots < 0 || c->slots > INT32_MAX)
+    return SSS_E_ARG;
+  if (c->stride < static_cast<int64_t>(c->heads) * c->dim || c->stride > kMaxDim ||
+      c->stride % 8 != 0)
+    return SSS_E_ARG;
+  if (c->slots > 0 && (c->k == nullptr || c->v == nullptr)) return SSS_E_ARG;
+  if (!aligned(c->k, 16) || !aligned(c->v, 16)) return SSS_E_ALIGN;
+  return SSS_OK;
+}
+}  // namespace
+
+sss_status_t sss_page_plan(const int32_t* past, const int32_t* fresh, int32_t batch,
+                           int32_t page_size, const int32_t* free_pages, int32_t free_count,
+                           int32_t* block_table, int32_t table_width, int32_t* cu_q,
+                           int32_t* kv_len, int32_t* positions, int32_t* slots, int64_t tokens,
+                           int32_t* used, uint32_t* dev_status, void* stream) {
+  if (batch < 0 || free_count < 0 || table_width < 0 || tokens < 0 || tokens > kMaxTokens)
+    return SSS_E_ARG;
+  if (!page_size_ok(page_size)) return SSS_E_ARG;
+  if (cu_q == nullptr || used == nullptr) return SSS_E_ARG;
+  if (batch > 0 && (past == nullptr || fresh == nullptr || kv_len == nullptr)) return SSS_E_ARG;
+  if (batch > 0 && table_width > 0 && block_table == nullptr) return SSS_E_ARG;
+  if (free_count > 0 && free_pages == nullptr) return SSS_E_ARG;
+  if (tokens > 0 && (positions == nullptr || slots == nullptr)) return SSS_E_ARG;
+  for (const void* p : {static_cast<const void*>(past), static_cast<const void*>(fresh),
+                        static_cast<const void*>(free_pages), static_cast<const void*>(block_table),
+                        static_cast<const void*>(cu_q), static_cast<const void*>(kv_len),
+                        static_cast<const void*>(positions), static_cast<const void*>(slots),
+                        static_cast<const void*>(used), static_cast<const void*>(dev_status)})
+    if (!aligned(p, 4)) return SSS_E_ALIGN;
+  return finish("sss_page_plan",
+                launch_page_plan(past, fresh, batch, page_size, free_pages, free_count, block_table,
+                                 table_width, cu_q, kv_len, positions, slots, tokens, used,
+                                 dev_status, static_cast<cudaStream_t>(stream)));
+}
+
+sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                              const void* v, int64_t v_stride, int32_t in_dtype, int64_t tokens,
+                              int32_t heads, const sss_rope_t* rope, const int32_t* positions,
+                              void* q_out, const sss_kv_cache_t* cache, const int32_t* slots,
+                              uint32_t* dev_status, void* stream) {
+  sss_status_t st = check_cache(cache);
+  if (st != SSS_OK) return st;
+  if (rope == nullptr || in_dtype < SSS_OUT_F32 || in_dtype > SSS_OUT_BF16) return SSS_E_ARG;
+  if (tokens < 0 || tokens > kMaxTokens || heads < 1 || heads > kMaxHeads) return SSS_E_ARG;
+  const int64_t kvw = static_cast<int64_t>(cache->heads) * cache->dim;
+  if (q_stride < static_cast<int64_t>(heads) * cache->dim || k_stride < kvw || v_stride < kvw)
+    return SSS_E_ARG;
+  if (q_stride > kMaxDim || k_stride > kMaxDim || v_stride > kMaxDim) return SSS_E_ARG;
+  if (q_stride % 4 != 0 || k_stride % 4 != 0 || v_stride % 4 != 0) return SSS_E_ARG;
+  if (rope->rot_dim < 0 || rope->rot_dim > cache->dim || rope->rot_dim % 8 != 0) return SSS_E_ARG;
+  if (rope->style != SSS_ROPE_HALF && rope->style != SSS_ROPE_PAIRS) return SSS_E_ARG;
+  if (!(rope->eps >= 0.0f) || rope->max_pos < 0 || rope->max_pos > kMaxDim) return SSS_E_ARG;
+  if (tokens == 0) return SSS_OK;
+  if (rope->rot_dim > 0 && (rope->cos == nullptr || rope->sin == nullptr || positions == nullptr ||
+                            rope->max_pos == 0))
+    return SSS_E_ARG;
+  if (q == nullptr || k == nullptr || v == nullptr || q_out == nullptr) return SSS_E_ARG;
+  const size_t in_align = in_dtype == SSS_OUT_F32 ? 16 : 8;
+  if (!aligned(q, in_align) || !aligned(k, in_align) || !aligned(v, in_align) ||
+      !aligned(q_out, 16) || !aligned(rope->cos, 16) || !aligned(rope->sin, 16) ||
+      !aligned(rope->q_norm, 16) || !aligned(rope->k_norm, 16) || !aligned(positions, 4) ||
+      !aligned(slots, 4) || !aligned(dev_status, 4))
+    return SSS_E_ALIGN;
+  return finish("sss_qk_norm_rope",
+                launch_qk_norm_rope(q, q_stride, k, k_stride, v, v_stride, in_dtype, tokens, heads,
+                                    *rope, positions, q_out, *cache, slots, dev_status,
+                                    static_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+// the sizes of an attention that is not empty
+sss_status_t check_attention(int64_t tokens, int32_t heads, const sss_kv_cache_t* cache,
+                             int32_t batch, int32_t max_q, int64_t max_kv) {
+  sss_status_t st = check_cache(cache);
+  if (st != SSS_OK) return st;
+  if (heads < 1 || heads > kMaxHeads || heads % cache->heads != 0) return SSS_E_ARG;
+  if (batch < 0 || batch > kMaxBatch || tokens < 0 || tokens > kMaxTokens) return SSS_E_ARG;
+  if (max_q < 0 || max_kv < 0 || max_kv > INT32_MAX / 2) return SSS_E_ARG;
+  return SSS_OK;
+}
+}  // namespace
+
+size_t sss_attention_workspace_bytes(int64_t tokens, int32_t heads, const sss_kv_cache_t* cache,
+                                     int32_t batch, int32_t max_q, int64_t max_kv) {
+  if (check_attention(tokens, heads, cache, batch, max_q, max_kv) != SSS_OK) return 0;
+  if (tokens == 0 || batch == 0 || max_q == 0) return 0;
+  return plan_attention(tokens, heads, *cache, batch, max_q, max_kv).ws_bytes;
+}
+
+sss_status_t sss_attention(const void* q, int64_t q_stride, int32_t heads,
+                           const sss_kv_cache_t* cache, const int32_t* cu_q, const int32_t* kv_len,
+                           const int32_t* block_table, int32_t table_width, int32_t batch,
+                           int64_t tokens, int32_t max_q, int64_t max_kv, float scale, void* out,
+                           void* workspace, size_t ws_bytes, uint32_t* dev_status, void* stream) {
+  sss_status_t st = check_attention(tokens, heads, cache, batch, max_q, max_kv);
+  if (st != SSS_OK) return st;
+  if (!(scale > 0.0f) || !(scale <= 3.0e38f)) return SSS_E_ARG;
+  if (q_stride < static_cast<int64_t>(heads) * cache->dim || q_stride > kMaxDim ||
+      q_stride % 8 != 0)
+    return SSS_E_ARG;
+  if (block_table != nullptr &&
+      (table_width < 1 || !page_size_ok(cache->page_size) || kv_len == nullptr))
+    return SSS_E_ARG;
+  if (tokens == 0 || batch == 0 || max_q == 0) return SSS_OK;
+  if (q == nullptr || out == nullptr || cu_q == nullptr) return SSS_E_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(cu_q, 4) || !aligned(kv_len, 4) ||
+      !aligned(block_table, 4) || !aligned(dev_status, 4) || !aligned(workspace, 16))
+    return SSS_E_ALIGN;
+  const AttnPlan p = plan_attention(tokens, heads, *cache, batch, max_q, max_kv);
+  if (p.ws_bytes > 0 && (workspace == nullptr || ws_bytes < p.ws_bytes)) return SSS_E_WORKSPACE;
+  return finish("sss_attention",
+                launch_attention(p, q, q_stride, heads, *cache, cu_q, kv_len, block_table,
+                                 table_width, batch, tokens, max_q, max_kv, scale, out, workspace,
+                                 dev_status, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -74,6 +74,34 @@ cudaError_t launch_sign_diagnostics(const float* w, int64_t n, int64_t k, int q,
                                     int16_t* margin, double* gain, unsigned long long* hist,
                                     uint32_t* status, cudaStream_t stream);
 
+cudaError_t launch_page_plan(const int32_t* past, const int32_t* fresh, int batch, int page_size,
+                             const int32_t* free_pages, int nfree, int32_t* table, int width,
+                             int32_t* cu_q, int32_t* kv_len, int32_t* positions, int32_t* slots,
+                             int64_t tokens, int32_t* used, uint32_t* status, cudaStream_t stream);
+
+cudaError_t launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                                const void* v, int64_t v_stride, int in_dtype, int64_t tokens,
+                                int heads, const sss_rope_t& rope, const int32_t* positions,
+                                void* q_out, const sss_kv_cache_t& cache, const int32_t* slots,
+                                uint32_t* status, cudaStream_t stream);
+
+// How a call of sss_attention is laid out (from its sizes alone).
+struct AttnPlan {
+  int row_tiles16;           // the row form's tiles are 16 or 32 rows
+  int hpt, hchunks, tpt;     // heads and tokens of a tile, tiles of a group of heads
+  bool one_tile;             // a request is one tile
+  int64_t tiles;             // an upper bound of the token tiles
+  int64_t chunk, nsplit;     // keys per split
+  size_t part_bytes, ws_bytes;
+};
+AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& cache, int batch,
+                        int max_q, int64_t max_kv);
+cudaError_t launch_attention(const AttnPlan& plan, const void* q, int64_t q_stride, int heads,
+                             const sss_kv_cache_t& cache, const int32_t* cu_q,
+                             const int32_t* kv_len, const int32_t* table, int width, int batch,
+                             int64_t tokens, int max_q, int64_t max_kv, float scale, void* out,
+                             void* workspace, uint32_t* status, cudaStream_t stream);
+
 // The kernel families whose next launches skip one barrier arrive
 // (sss_test_set_stall; 0 in normal use).
 uint32_t test_stall_mask();

@@ -25,6 +25,8 @@ OP_GEMV, OP_GEMM = 0, 1
 FLAG_NONFINITE = 0x1
 FLAG_RANGE = 0x2
 FLAG_TIMEOUT = 0x4
+FLAG_INDEX = 0x8
+FLAG_PAGES = 0x10
 
 SSS_OK = 0
 STATUS_NAMES = {0: "SSS_OK", 1: "SSS_E_ARG", 2: "SSS_E_UNSUPPORTED", 3: "SSS_E_ALIGN",
@@ -35,13 +37,17 @@ EXPORTS = ("sss_codes_bytes", "sss_status_string", "sss_last_error", "sss_quanti
            "sss_gemm_noalloc", "sss_gemm_noalloc_max_scratch_bytes", "sss_test_set_stall",
            "sss_gemm_multi", "sss_gemm_multi_workspace_bytes",
            "sss_gemm_q8", "sss_quantize_act_q8", "sss_sign_diagnostics", "sss_hadamard",
-           "sss_quantize_rotated", "sss_quantize_lsq")
+           "sss_quantize_rotated", "sss_quantize_lsq",
+           "sss_page_plan", "sss_qk_norm_rope", "sss_attention",
+           "sss_attention_workspace_bytes")
 
 GEMV_PDL = 0x1
 GEMV_WEIGHTS_READY = 0x2
 GEMV_ACT_Q8 = 0x4
 
 ROTATE_INPUT, ROTATE_OUTPUT = 0, 1
+
+ROPE_HALF, ROPE_PAIRS = 0, 1
 
 TEST_STALL_GEMV = 0x1
 TEST_STALL_GEMV_BATCH = 0x2
@@ -67,6 +73,34 @@ class QTensorDesc(ctypes.Structure):
         ("codes", ctypes.c_void_p),
         ("scales", ctypes.c_void_p),
         ("mins", ctypes.c_void_p),
+    ]
+
+
+class KVCacheDesc(ctypes.Structure):
+    """Mirror of sss_kv_cache_t."""
+    _fields_ = [
+        ("k", ctypes.c_void_p),
+        ("v", ctypes.c_void_p),
+        ("slots", ctypes.c_int64),
+        ("stride", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
+class RopeDesc(ctypes.Structure):
+    """Mirror of sss_rope_t."""
+    _fields_ = [
+        ("cos", ctypes.c_void_p),
+        ("sin", ctypes.c_void_p),
+        ("q_norm", ctypes.c_void_p),
+        ("k_norm", ctypes.c_void_p),
+        ("max_pos", ctypes.c_int64),
+        ("rot_dim", ctypes.c_int32),
+        ("style", ctypes.c_int32),
+        ("eps", ctypes.c_float),
     ]
 
 
@@ -133,6 +167,18 @@ def load(build_if_needed: bool = True):
         L.sss_quantize_rotated.restype = i32
         L.sss_quantize_lsq.argtypes = [vp, P, i32, ctypes.c_float, vp, vp]
         L.sss_quantize_lsq.restype = i32
+        C, R, f32 = ctypes.POINTER(KVCacheDesc), ctypes.POINTER(RopeDesc), ctypes.c_float
+        L.sss_page_plan.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, i64, vp,
+                                    vp, vp]
+        L.sss_page_plan.restype = i32
+        L.sss_qk_norm_rope.argtypes = [vp, i64, vp, i64, vp, i64, i32, i64, i32, R, vp, vp, C, vp,
+                                       vp, vp]
+        L.sss_qk_norm_rope.restype = i32
+        L.sss_attention.argtypes = [vp, i64, i32, C, vp, vp, vp, i32, i32, i64, i32, i64, f32, vp,
+                                    vp, sz, vp, vp]
+        L.sss_attention.restype = i32
+        L.sss_attention_workspace_bytes.argtypes = [i64, i32, C, i32, i32, i64]
+        L.sss_attention_workspace_bytes.restype = sz
         L.sss_test_set_stall.argtypes = [ctypes.c_uint32]
         L.sss_test_set_stall.restype = None
         _lib = L
@@ -587,5 +633,240 @@ def sss_quantize_lsq(w, q: int, group: int, grid: int, steps: int, lr: float,
     d = out.desc()
     st = load().sss_quantize_lsq(_ptr(w), ctypes.byref(d), int(steps), float(lr),
                                  _ptr(dev_status), _stream(stream))
+    _check(fn, st)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# the attention step: pages, head norm and rotation, attention
+# ---------------------------------------------------------------------------
+
+def _dtype_code(dtype):
+    import torch
+
+    return {torch.float32: OUT_F32, torch.float16: OUT_F16, torch.bfloat16: OUT_BF16}.get(dtype)
+
+
+@dataclass
+class KVCache:
+    """Keys and values [slots, heads, dim] (fp16 or bf16) in pages of page_size
+    slots.  The heads of a slot are dense; slots may be further apart (k and v as
+    columns of one matrix)."""
+    k: "object"
+    v: "object"
+    page_size: int = 16
+
+    def __post_init__(self):
+        fn, k, v = "KVCache", self.k, self.v
+        if k.dim() != 3 or k.shape != v.shape:
+            raise SssError(fn, 1, "k and v must be [slots, heads, dim] of one shape")
+        if _dtype_code(k.dtype) not in (OUT_F16, OUT_BF16) or k.dtype != v.dtype:
+            raise SssError(fn, 1, "k and v must be float16 or bfloat16")
+        slots, heads, dim = k.shape
+        strides = [(t.stride(0) if slots > 1 else heads * dim) for t in (k, v)]
+        for t in (k, v):
+            if t.numel() and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != dim)):
+                raise SssError(fn, 1, "the heads of a slot must be contiguous")
+        if strides[0] != strides[1]:
+            raise SssError(fn, 1, "k and v must have the same stride")
+        _on_device(fn, k=k, v=v)
+        # (the pointers are read at every call: the tensors may be refilled, not moved)
+        self._desc = KVCacheDesc(_ptr(k), _ptr(v), slots, strides[0], self.page_size, heads, dim,
+                                 _dtype_code(k.dtype))
+        self._ref = ctypes.byref(self._desc)
+
+
+def empty_kv_cache(pages: int, page_size: int, heads: int, dim: int, dtype=None,
+                   device="cuda") -> KVCache:
+    import torch
+
+    dtype = torch.bfloat16 if dtype is None else dtype
+    k, v = (torch.empty((pages * page_size, heads, dim), dtype=dtype, device=device)
+            for _ in range(2))
+    return KVCache(k, v, page_size)
+
+
+@dataclass
+class Rope:
+    """The rotation of a model's heads: fp32 cos and sin [max_pos, rot_dim / 2]
+    (None: no rotation), the pairs' style, and the fp32 weights [dim] of the query
+    and key heads' norm (None: none)."""
+    cos: Optional["object"] = None
+    sin: Optional["object"] = None
+    style: int = ROPE_HALF
+    q_norm: Optional["object"] = None
+    k_norm: Optional["object"] = None
+    eps: float = 1e-6
+
+    def __post_init__(self):
+        import torch
+
+        fn = "Rope"
+        if (self.cos is None) != (self.sin is None):
+            raise SssError(fn, 1, "cos and sin are given together")
+        max_pos, half = 0, 0
+        if self.cos is not None:
+            if self.cos.dim() != 2 or self.cos.shape != self.sin.shape:
+                raise SssError(fn, 1, "cos and sin must be [max_pos, rot_dim / 2]")
+            max_pos, half = self.cos.shape
+        for name in ("cos", "sin", "q_norm", "k_norm"):
+            _need(fn, name, getattr(self, name), torch.float32, optional=True)
+        _on_device(fn, cos=self.cos, sin=self.sin, q_norm=self.q_norm, k_norm=self.k_norm)
+        self._desc = RopeDesc(_ptr(self.cos), _ptr(self.sin), _ptr(self.q_norm), _ptr(self.k_norm),
+                              max_pos, 2 * half, self.style, self.eps)
+        self._ref = ctypes.byref(self._desc)
+
+
+def _int32(t, numel) -> bool:
+    import torch
+
+    return (t is not None and t.dtype is torch.int32 and t.is_cuda and t.is_contiguous()
+            and t.numel() == numel)
+
+
+def _need_int32(fn, **tensors):
+    """name=(tensor, elements or None): device int32, contiguous."""
+    import torch
+
+    for name, (t, numel) in tensors.items():
+        _need(fn, name, t, torch.int32, numel)
+        _on_device(fn, **{name: t})
+
+
+def sss_page_plan(past, fresh, page_size: int, free_pages, block_table, cu_q, kv_len, positions,
+                  slots, used, dev_status=None, stream=None) -> None:
+    """A step's pages and slots from its requests' lengths: int32 past and fresh
+    [batch], free_pages and the block table [batch, width] to cu_q [batch + 1],
+    kv_len [batch], positions and slots [tokens], used [1] and the table's new
+    entries."""
+    fn = "sss_page_plan"
+    batch, tokens = past.numel(), positions.numel()
+    if not (_int32(past, batch) and _int32(fresh, batch) and _int32(free_pages, free_pages.numel())
+            and block_table.dim() == 2 and _int32(block_table, batch * block_table.shape[1])
+            and _int32(cu_q, batch + 1) and _int32(kv_len, batch) and _int32(positions, tokens)
+            and _int32(slots, tokens) and _int32(used, 1) and _plain_status(dev_status)):
+        if block_table.dim() != 2 or block_table.shape[0] != batch:
+            raise SssError(fn, 1, "block_table must be [batch, width]")
+        _need_int32(fn, past=(past, batch), fresh=(fresh, batch), free_pages=(free_pages, None),
+                    block_table=(block_table, None), cu_q=(cu_q, batch + 1), kv_len=(kv_len, batch),
+                    positions=(positions, tokens), slots=(slots, tokens), used=(used, 1))
+        _need_status(fn, dev_status)
+        _on_device(fn, dev_status=dev_status)
+    st = load().sss_page_plan(past.data_ptr(), fresh.data_ptr(), batch, page_size,
+                              free_pages.data_ptr(), free_pages.numel(), block_table.data_ptr(),
+                              block_table.shape[1], cu_q.data_ptr(), kv_len.data_ptr(),
+                              positions.data_ptr(), slots.data_ptr(), tokens, used.data_ptr(),
+                              _ptr(dev_status), _stream(stream))
+    _check(fn, st)
+
+
+def _rows(fn, name, t, tokens, width):
+    """The row stride of t [tokens, width] (or [tokens, heads, dim]) whose rows
+    are dense."""
+    if t.shape[0] != tokens or t.numel() != tokens * width:
+        raise SssError(fn, 1, f"{name} must be [{tokens}, {width}]")
+    if t.is_contiguous() or t.numel() == 0:
+        return width
+    inner = t.stride()[-1] == 1 and (t.dim() == 2 or t.shape[1] == 1
+                                     or t.stride(1) == t.shape[2])
+    if not inner or t.dim() > 3:
+        raise SssError(fn, 1, f"{name}'s rows must be contiguous")
+    return t.stride(0) if tokens > 1 else width
+
+
+def sss_qk_norm_rope(q, k, v, rope: Rope, positions, cache: KVCache, slots=None, q_out=None,
+                     dev_status=None, stream=None):
+    """q [tokens, heads * dim], k and v [tokens, kv_heads * dim] (fp32 as the
+    projections write them, or 16-bit; rows may be strided): heads normalised
+    and rotated, q to q_out [tokens, heads, dim], k and v to the cache's slots."""
+    import torch
+
+    fn = "sss_qk_norm_rope"
+    d = cache._desc
+    tokens, dim = q.shape[0], d.dim
+    width = q.numel() // tokens if tokens else q.shape[-1]
+    if dim <= 0 or width % dim:
+        raise SssError(fn, 1, "q's rows must be whole heads")
+    code = _dtype_code(q.dtype)
+    if code is None or k.dtype != q.dtype or v.dtype != q.dtype:
+        raise SssError(fn, 1, "q, k and v must be of one dtype: float32, float16 or bfloat16")
+    qs = _rows(fn, "q", q, tokens, width)
+    ks, vs = (_rows(fn, n, t, tokens, d.heads * dim) for n, t in (("k", k), ("v", v)))
+    if q_out is None:
+        q_out = torch.empty((tokens, width // dim, dim), dtype=cache.k.dtype, device=q.device)
+    _need(fn, "q_out", q_out, cache.k.dtype, tokens * width)
+    _on_device(fn, q=q, k=k, v=v, q_out=q_out, dev_status=dev_status)
+    if positions is not None or d.dim and rope._desc.rot_dim:
+        _need_int32(fn, positions=(positions, tokens))
+    if slots is not None:
+        _need_int32(fn, slots=(slots, tokens))
+    for name in ("q_norm", "k_norm"):
+        _need(fn, name, getattr(rope, name), torch.float32, dim, optional=True)
+    if not _plain_status(dev_status):
+        _need_status(fn, dev_status)
+    st = load().sss_qk_norm_rope(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, code, tokens,
+                                 width // dim, rope._ref, _ptr(positions), q_out.data_ptr(),
+                                 cache._ref, _ptr(slots), _ptr(dev_status), _stream(stream))
+    _check(fn, st)
+    return q_out
+
+
+def sss_attention_workspace_bytes(tokens: int, heads: int, cache: KVCache, batch: int, max_q: int,
+                                  max_kv: int) -> int:
+    """Workspace bytes of sss_attention with these sizes."""
+    return int(load().sss_attention_workspace_bytes(tokens, heads, cache._ref, batch, max_q,
+                                                    max_kv))
+
+
+def sss_attention(q, cache: KVCache, cu_q, kv_len, max_q: int, max_kv: int, block_table=None,
+                  scale=None, out=None, workspace=None, dev_status=None, stream=None):
+    """Causal attention of q [tokens, heads, dim] over the cache: request b's
+    tokens are rows cu_q[b] .. cu_q[b + 1] - 1 of q, the last of its kv_len[b]
+    keys.  Without a block table its keys lie in slots cu_q[b] .. (kv_len may be
+    None: its new tokens).  Returns out [tokens, heads, dim]."""
+    import torch
+
+    fn = "sss_attention"
+    d = cache._desc
+    if q.dim() != 3 or q.shape[2] != d.dim:
+        raise SssError(fn, 1, "q must be [tokens, heads, dim] of the cache's dim")
+    tokens, heads, dim = q.shape
+    batch = cu_q.numel() - 1
+    if q.dtype is not cache.k.dtype:
+        raise SssError(fn, 1, f"q must be {cache.k.dtype}, as the cache")
+    qs = _rows(fn, "q", q, tokens, heads * dim)
+    if out is None:
+        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+    if scale is None:
+        scale = dim ** -0.5
+    if not (_int32(cu_q, batch + 1) and _plain(out, q.dtype, tokens * heads * dim) and q.is_cuda
+            and _plain_workspace(workspace) and _plain_status(dev_status)
+            and (kv_len is None or _int32(kv_len, batch))
+            and (block_table is None
+                 or block_table.dim() == 2 and block_table.shape[0] == batch
+                 and _int32(block_table, block_table.numel()))):
+        _need_int32(fn, cu_q=(cu_q, None))
+        if batch < 0:
+            raise SssError(fn, 1, "cu_q must be [batch + 1]")
+        if kv_len is not None:
+            _need_int32(fn, kv_len=(kv_len, batch))
+        if block_table is not None:
+            if block_table.dim() != 2 or block_table.shape[0] != batch:
+                raise SssError(fn, 1, "block_table must be [batch, width]")
+            _need_int32(fn, block_table=(block_table, None))
+        _need(fn, "out", out, q.dtype, tokens * heads * dim)
+        _need(fn, "workspace", workspace, torch.uint8, optional=True)
+        _need_status(fn, dev_status)
+        _on_device(fn, q=q, out=out, workspace=workspace, dev_status=dev_status)
+    if workspace is None:
+        need = sss_attention_workspace_bytes(tokens, heads, cache, batch, max_q, max_kv)
+        if need > 0:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    ws_bytes = 0 if workspace is None else workspace.numel()
+    width = 0 if block_table is None else block_table.shape[1]
+    st = load().sss_attention(q.data_ptr(), qs, heads, cache._ref, cu_q.data_ptr(), _ptr(kv_len),
+                              _ptr(block_table), width, batch, tokens, max_q, max_kv, scale,
+                              out.data_ptr(), _ptr(workspace), ws_bytes, _ptr(dev_status),
+                              _stream(stream))
     _check(fn, st)
     return out
