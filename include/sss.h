@@ -77,9 +77,9 @@ typedef enum {
                                    (see those calls); their outputs may then hold
                                    inf or NaN                                         */
 #define SSS_FLAG_TIMEOUT 0x4u   /* a bounded pipeline wait of sss_gemm (or
-                                   sss_gemm_noalloc), sss_quantize or
-                                   sss_quantize_rotated expired; the output is
-                                   incomplete                                         */
+                                   sss_gemm_noalloc), sss_quantize,
+                                   sss_quantize_rotated or sss_attention (of many
+                                   rows) expired; the output is incomplete                                         */
 #define SSS_FLAG_INDEX 0x8u     /* sss_page_plan, sss_qk_norm_rope, sss_attention: a length,
                                    position, slot or page lies outside what the call's
                                    arguments allow; what the calls do then is said there */
@@ -538,6 +538,7 @@ sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, in
  *                     outside what they may (a request past `tokens` is left
  *                     out, lengths are cut to max_q, max_kv, the table's width or
  *                     the request's own rows, a page that is none reads as zeros).
+ *                     SSS_FLAG_TIMEOUT: a bounded wait ran out (many rows only).
  * The result does not depend on timing, and a request's not on the others in the
  * batch but through max_q, max_kv and their number, by which the work is split.
  * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim), SSS_E_ALIGN, SSS_E_WORKSPACE,
@@ -596,7 +597,7 @@ size_t sss_gemm_noalloc_max_scratch_bytes(void);
  * sss_test_set_stall -- test hook for the bounded waits; the paper has no
  * counterpart.  While a bit below is set, every later launch of that kernel
  * family leaves one mbarrier one arrive short: the GEMM on the first
- * stage's weight tile.  The decode GEMV kernels (batch 1 and batched) have
+ * stage's weight tile, the attention of prompts on its first value tile.  The decode GEMV kernels (batch 1 and batched) have
  * no data-dependent waits (their warps meet only at CTA-wide barriers), so
  * their bits have no effect.  The wait on that barrier then runs out after
  * its bound (about one second), the kernel raises SSS_FLAG_TIMEOUT in
@@ -608,6 +609,8 @@ size_t sss_gemm_noalloc_max_scratch_bytes(void);
 #define SSS_TEST_STALL_GEMV 0x1u       /* gemv_stream_kernel: no waits, no effect               */
 #define SSS_TEST_STALL_GEMV_BATCH 0x2u /* gemv_batch_kernel: no waits, no effect                */
 #define SSS_TEST_STALL_GEMM 0x4u       /* gemm_kernel (sss_gemm, sss_gemm_noalloc)             */
+#define SSS_TEST_STALL_ATTENTION 0x8u  /* attn_prompt_kernel (sss_attention of many rows): the
+                                          first value tile is never handed on              */
 void sss_test_set_stall(uint32_t mask);
 
 #ifdef __cplusplus

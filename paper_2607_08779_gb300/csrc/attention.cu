@@ -10,19 +10,36 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
                         int64_t max_kv) {
   AttnPlan p = {};
   const int group = heads / c.heads;
-  // rows of a tile: 16 while they hold a request's tokens and heads
-  p.row_tiles16 = static_cast<int64_t>(group) * max_q <= 16 ? 1 : 2;
-  const int rows = 16 * p.row_tiles16;
-  p.hpt = std::min(group, rows);
+  const int64_t sms = device_sm_count();
+  // the row form while a request's tokens and heads are one tile of it (and without
+  // a cache to make a tensor map of)
+  p.prompt = static_cast<int64_t>(group) * max_q > 32 && max_q > 1 && c.slots > 0;
+  int64_t splits, step;
+  if (p.prompt) {
+    // two row tiles of 128 rows: `tt` tokens (a multiple of 8, as its box in swizzled
+    // shared memory needs) of up to 16 heads each
+    p.hpt = std::min(group, 16);
+    p.tpt = 2 * (128 / p.hpt / 8 * 8);
+  } else {
+    // 16 rows while they hold a request's tokens and heads
+    p.row_tiles16 = static_cast<int64_t>(group) * max_q <= 16 ? 1 : 2;
+    p.hpt = std::min(group, 16 * p.row_tiles16);
+    p.tpt = std::min(16 * p.row_tiles16 / p.hpt, max_q);
+  }
   p.hchunks = (group + p.hpt - 1) / p.hpt;
-  p.tpt = std::min(rows / p.hpt, max_q);
   p.one_tile = max_q <= p.tpt;
   p.tiles = p.one_tile ? batch : std::min(tokens / p.tpt + batch,
                                           static_cast<int64_t>(batch) * ((max_q + p.tpt - 1) / p.tpt));
   const int64_t items = std::max<int64_t>(1, p.tiles * c.heads * p.hchunks);
-  const int64_t want = std::max<int64_t>(1, 4 * device_sm_count() / items);
-  const int64_t splits = std::max<int64_t>(1, std::min(want, (max_kv + 255) / 256));
-  p.chunk = std::max<int64_t>(64, ((max_kv + splits - 1) / splits + 63) / 64 * 64);
+  if (p.prompt) {
+    step = 128;
+    splits = std::min(sms / items, (max_kv + 511) / 512);
+  } else {
+    step = 64;
+    splits = std::min(4 * sms / items, (max_kv + 255) / 256);
+  }
+  splits = std::max<int64_t>(1, splits);
+  p.chunk = std::max<int64_t>(step, ((max_kv + splits - 1) / splits + step - 1) / step * step);
   p.nsplit = std::max<int64_t>(1, (max_kv + p.chunk - 1) / p.chunk);
   if (p.nsplit > 1) {
     const size_t rowsz = static_cast<size_t>(tokens) * heads;
@@ -68,7 +85,9 @@ cudaError_t launch_attention(const AttnPlan& p, const void* q, int64_t q_stride,
   a.chunk = static_cast<int>(p.chunk);
   a.nsplit = static_cast<int>(p.nsplit);
   a.scale_log2 = scale * 1.4426950408889634f;
-  cudaError_t e = launch_attn_rows(a, c.dtype, c.dim, p.row_tiles16, stream);
+  a.stall = (test_stall_mask() & SSS_TEST_STALL_ATTENTION) ? 1 : 0;
+  cudaError_t e = p.prompt ? launch_attn_prompt(a, c.dtype, c.dim, stream)
+                           : launch_attn_rows(a, c.dtype, c.dim, p.row_tiles16, stream);
   if (e == cudaSuccess && p.nsplit > 1) e = launch_attn_join(a, c.dtype, c.dim, stream);
   return e;
 }

@@ -158,6 +158,7 @@ __device__ __forceinline__ float ex2(float x) {
 // The forms of the attention.
 cudaError_t launch_attn_rows(const AttnArgs& a, int dtype, int dim, int row_tiles16,
                              cudaStream_t stream);
+cudaError_t launch_attn_prompt(const AttnArgs& a, int dtype, int dim, cudaStream_t stream);
 cudaError_t launch_attn_join(const AttnArgs& a, int dtype, int dim, cudaStream_t stream);
 
 }  // namespace sss

@@ -140,7 +140,8 @@ const char* sss_status_string(sss_status_t s) {
 const char* sss_last_error(void) { return g_last_error; }
 
 void sss_test_set_stall(uint32_t mask) {
-  g_test_stall.store(mask & (SSS_TEST_STALL_GEMV | SSS_TEST_STALL_GEMV_BATCH | SSS_TEST_STALL_GEMM),
+  g_test_stall.store(mask & (SSS_TEST_STALL_GEMV | SSS_TEST_STALL_GEMV_BATCH | SSS_TEST_STALL_GEMM |
+                             SSS_TEST_STALL_ATTENTION),
                      std::memory_order_relaxed);
 }
 

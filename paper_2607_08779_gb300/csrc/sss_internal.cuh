@@ -87,6 +87,7 @@ cudaError_t launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, 
 
 // How a call of sss_attention is laid out (from its sizes alone).
 struct AttnPlan {
+  bool prompt;               // the form on tcgen05; else the row form
   int row_tiles16;           // the row form's tiles are 16 or 32 rows
   int hpt, hchunks, tpt;     // heads and tokens of a tile, tiles of a group of heads
   bool one_tile;             // a request is one tile

@@ -52,6 +52,7 @@ ROPE_HALF, ROPE_PAIRS = 0, 1
 TEST_STALL_GEMV = 0x1
 TEST_STALL_GEMV_BATCH = 0x2
 TEST_STALL_GEMM = 0x4
+TEST_STALL_ATTENTION = 0x8
 
 
 class SssError(RuntimeError):
