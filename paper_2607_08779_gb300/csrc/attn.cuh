@@ -42,9 +42,9 @@ struct AttnArgs {
 struct AttnRequest {
   int q0, n, kv;
 };
-__device__ __forceinline__ AttnRequest attn_request(const AttnArgs& a, int b, uint32_t& flags) {
+__device__ __forceinline__ AttnRequest attn_request(const AttnArgs& a, int64_t q0, int64_t q1,
+                                                    int64_t kv, uint32_t& flags) {
   AttnRequest r;
-  const int64_t q0 = a.cu_q[b], q1 = a.cu_q[b + 1];
   int64_t n = q1 - q0;
   if (q0 < 0 || n < 0 || q1 > a.tokens) {
     n = 0;
@@ -59,7 +59,7 @@ __device__ __forceinline__ AttnRequest attn_request(const AttnArgs& a, int b, ui
   int64_t most = a.table ? static_cast<int64_t>(a.table_width) << a.page_shift
                          : min(n, a.slots - q0);
   if (most > a.max_kv) most = a.max_kv;
-  int64_t kv = a.kv_len ? a.kv_len[b] : n;
+  if (!a.kv_len) kv = n;
   if (kv < 0 || kv > most) {
     kv = kv < 0 || most < 0 ? 0 : most;
     flags |= SSS_FLAG_INDEX;
@@ -69,6 +69,9 @@ __device__ __forceinline__ AttnRequest attn_request(const AttnArgs& a, int b, ui
   r.kv = static_cast<int>(kv);
   return r;
 }
+__device__ __forceinline__ AttnRequest attn_request(const AttnArgs& a, int b, uint32_t& flags) {
+  return attn_request(a, a.cu_q[b], a.cu_q[b + 1], a.kv_len ? a.kv_len[b] : 0, flags);
+}
 
 // keys that token i of the request sees
 __device__ __forceinline__ int attn_limit(const AttnRequest& r, int i) {
@@ -77,19 +80,26 @@ __device__ __forceinline__ int attn_limit(const AttnRequest& r, int i) {
 
 // Token tile `tile` of the launch, found by a whole warp: its request and first
 // token.  A request's tiles run from its last tokens, which see the most keys, to
-// its first.  False behind the last tile.
-__device__ __forceinline__ bool attn_tile(const AttnArgs& a, int tile, int& b, int& i0) {
+// its first.  False behind the last tile.  (Each lane brings all of a request's
+// lengths at once: where they are not in the caches, one trip to memory.)
+__device__ __forceinline__ bool attn_tile(const AttnArgs& a, int tile, int& b, int& i0,
+                                          AttnRequest& rq, uint32_t& flags) {
   if (a.one_tile) {
     b = tile;
     i0 = 0;
-    return tile < a.batch;
+    if (tile >= a.batch) return false;
+    rq = attn_request(a, b, flags);
+    return true;
   }
   const int lane = threadIdx.x & 31;
   int before = 0;
   for (int base = 0; base < a.batch; base += 32) {
-    int nt = 0;
+    int q0 = 0, q1 = 0, kv = 0, nt = 0;
     if (base + lane < a.batch) {
-      const int64_t n = static_cast<int64_t>(a.cu_q[base + lane + 1]) - a.cu_q[base + lane];
+      q0 = a.cu_q[base + lane];
+      q1 = a.cu_q[base + lane + 1];
+      kv = a.kv_len ? a.kv_len[base + lane] : 0;
+      const int64_t n = static_cast<int64_t>(q1) - q0;
       if (n > 0) nt = static_cast<int>((min(n, static_cast<int64_t>(a.max_q)) + a.tpt - 1) / a.tpt);
     }
     int sum = nt;
@@ -105,6 +115,8 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int tile, int& b, i
       const int first = before + __shfl_sync(0xffffffffu, sum - nt, w);
       const int count = __shfl_sync(0xffffffffu, nt, w);
       i0 = (count - 1 - (tile - first)) * a.tpt;
+      rq = attn_request(a, __shfl_sync(0xffffffffu, q0, w), __shfl_sync(0xffffffffu, q1, w),
+                        __shfl_sync(0xffffffffu, kv, w), flags);
       return true;
     }
     before += __shfl_sync(0xffffffffu, sum, 31);

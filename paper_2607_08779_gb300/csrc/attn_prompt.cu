@@ -14,9 +14,17 @@
 //             operand) and keeps the row's sum; at the end it scales the row's
 //             output and stores it;
 //   warp 8    issues the products: scores S = Q K^T (both from shared memory), then
-//             O += P V with P from tensor memory;
+//             O += P V with P from tensor memory.  It takes A and B in turn, which keeps
+//             them half a step apart;
 //   warp 9    TMA producer of Q, K and V (a box per page, or per 128 packed keys);
-//   warps 10-11  look through V tiles that some row does not see whole.
+//   warp 10   scheduler: says what the CTA works on next;
+//   warps 12-15  look through V tiles that some row does not see whole.
+//
+// The grid has a CTA for every item (two row tiles and a split of the keys); those
+// that run take the items of those that do not yet (cluster launch control), so
+// that an item's loads, its first scores and the search for its request run
+// while the one before is finished.  Within a request the items with the most keys
+// come first.
 // Rows are tokens x the heads that share a key/value head (head-major, so that a TMA
 // box brings a head's tokens): all heads of a group see almost the same keys, a
 // tile spans few tokens, and little of the last key tile is masked.
@@ -44,10 +52,11 @@
 namespace sss {
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 512;
 constexpr int kKeys = 128;      // of a tile
 constexpr float kRaise = 8.0f;  // powers of two
 constexpr int kTmemCols = 512;  // one CTA per SM
+constexpr int kConsumers = 14;  // warps that read an item
 
 struct AttnMaps {
   CUtensorMap q, k, v;
@@ -60,12 +69,15 @@ struct PromptSmem {
   static constexpr int Q_TILE = HALVES * PART;
   static constexpr int KV_TILE = HALVES * PART;
   static constexpr int KS = D == 128 ? 2 : 4;       // key and value tiles in flight
-  static constexpr int VS = D == 128 ? 3 : 4;
+  // (a stage is asked for 2T - 1536 cycles before its use, T = 2048 at best: two do)
+  static constexpr int VS = KS;
   static constexpr int K_OFF = 2 * Q_TILE;
   static constexpr int V_OFF = K_OFF + KS * KV_TILE;
-  static constexpr int FIRST_OFF = V_OFF + VS * KV_TILE;  // int [3][D]
-  static constexpr int BAR_OFF = FIRST_OFF + 3 * D * 4;
-  static constexpr int NBAR = 2 + 2 * KS + 3 * VS + 3 * 2 + 1;
+  static constexpr int OUT_OFF = V_OFF + VS * KV_TILE;    // 32 rows of 128 bytes per warp
+  static constexpr int WORK_OFF = OUT_OFF + 8 * 4096;     // two items, and a 16-byte answer
+  static constexpr int FIRST_OFF = WORK_OFF + 2 * 64 + 16;  // uint32 [2][D]
+  static constexpr int BAR_OFF = FIRST_OFF + 2 * D * 4;
+  static constexpr int NBAR = 4 + 2 * KS + 3 * VS + 4 * 2 + 4 + 2;
   static constexpr int TOTAL = BAR_OFF + NBAR * 8 + 16 + 1024;  // + align slack
   static_assert(TOTAL <= 227 * 1024, "shared memory per CTA");
 };
@@ -79,31 +91,45 @@ constexpr uint32_t idesc_of(int n, bool b_mn) {
          (static_cast<uint32_t>(n >> 3) << 17) | (8u << 24);
 }
 
-// V as a B operand: 64 values of d are one 128-byte row of a swizzled part, 8 keys an
-// atom of 1024 bytes; the next 64 values lie a part further.
-__device__ __forceinline__ uint64_t mn_desc(uint32_t saddr, uint32_t part) {
-  uint64_t d = 0;
-  d |= static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4);
-  d |= static_cast<uint64_t>(part >> 4) << 16;
-  d |= static_cast<uint64_t>(1024 >> 4) << 32;
-  d |= static_cast<uint64_t>(1) << 46;
-  d |= static_cast<uint64_t>(2) << 61;
-  return d;
+// Shared-memory operands.  All have 128-byte swizzled rows in atoms of 8 rows, 1024
+// bytes apart, so the upper words of their descriptors are the same: only the lower
+// word is handed about.  Q and K are K-major (d contiguous).  V is MN-major: 64 values of
+// d are one row of an atom of 8 keys, and the next 64 values lie a part further.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t saddr, uint32_t part) {
+  return ((saddr & 0x3FFFFu) >> 4) | (part >> 4) << 16;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t acc) {
+// Four products of 16 deep in one block, the first of them from zero unless acc.  A and
+// B from shared memory, 32 bytes further along d each.
+__device__ __forceinline__ void mma4_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                        uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n .reg .pred p;\n .reg .b32 x, y;\n .reg .b64 a, b;\n setp.ne.b32 p, %4, 0;\n"
+      " mov.b64 a, {%1, %5};\n mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n"
+      " add.u32 x, %1, 2;\n add.u32 y, %2, 2;\n mov.b64 a, {x, %5};\n mov.b64 b, {y, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n"
+      " add.u32 x, %1, 4;\n add.u32 y, %2, 4;\n mov.b64 a, {x, %5};\n mov.b64 b, {y, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n"
+      " add.u32 x, %1, 6;\n add.u32 y, %2, 6;\n mov.b64 a, {x, %5};\n mov.b64 b, {y, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, 1;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(kDescHigh)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc,
-                                       uint32_t acc) {
+// A from tensor memory, 8 columns further each; B 16 keys (2048 bytes) further.
+__device__ __forceinline__ void mma4_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc,
+                                        uint32_t acc) {
   asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n .reg .pred p;\n .reg .b32 x, y;\n .reg .b64 b;\n setp.ne.b32 p, %4, 0;\n"
+      " mov.b64 b, {%2, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n"
+      " add.u32 x, %1, 8;\n add.u32 y, %2, 128;\n mov.b64 b, {y, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %3, 1;\n"
+      " add.u32 x, %1, 16;\n add.u32 y, %2, 256;\n mov.b64 b, {y, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %3, 1;\n"
+      " add.u32 x, %1, 24;\n add.u32 y, %2, 384;\n mov.b64 b, {y, %5};\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], [x], b, %3, 1;\n}\n" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(kDescHigh)
       : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() {
@@ -111,6 +137,11 @@ __device__ __forceinline__ void tmem_wait_ld() {
 }
 __device__ __forceinline__ void tmem_wait_st() {
   asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
 }
 // (x0, x1) * s + t
 __device__ __forceinline__ float2 fma2(float x0, float x1, float s, float t) {
@@ -130,14 +161,46 @@ __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   return r;
 }
 
-// What the CTA works on: two row tiles of `tt` tokens each.
-struct PromptWork {
-  AttnRequest rq;
-  int b, kh, g0, nh, i0, tt, z;
+// An item, as the scheduler leaves it in shared memory.
+struct __align__(16) Work {
+  int live;      // 0: there is no further item
+  int b;         // request
+  int q0, n, kv; // its AttnRequest
+  int kh, g0, nh;  // key/value head; first head of the group and number of heads
+  int i0;        // first token of row tile A (row tile B's: i0 + tt)
   int k0;        // first key of the split
   int lim0;      // keys that the first token sees
-  int n[2];      // key tiles of A, B
+  int n0, n1;    // key tiles of A, B
+  int z;
+  int alone;     // no other split has keys
+  int pad;
 };
+static_assert(sizeof(Work) == 64, "");
+
+// The grid's next CTA that has not started, kept from starting: its index in x (-1:
+// all have).  To be called by one thread; not again after -1.
+__device__ __forceinline__ void next_cta_ask(uint32_t answer, uint64_t* bar) {
+  mbar_arrive_expect_tx(bar, 16);
+  asm volatile(
+      "clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 "
+      "[%0], [%1];" ::"r"(answer),
+      "r"(smem_u32(bar))
+      : "memory");
+}
+__device__ __forceinline__ int next_cta(uint32_t answer) {
+  uint32_t ok, x;
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b128 h;\n ld.shared.b128 h, [%2];\n"
+      " clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, h;\n"
+      " selp.u32 %0, 1, 0, p;\n mov.u32 %1, 0;\n"
+      " @p clusterlaunchcontrol.query_cancel.get_first_ctaid.v4.b32.b128 {%1, _, _, _}, h;\n}\n"
+      : "=r"(ok), "=r"(x)
+      : "r"(answer)
+      : "memory");
+  // (the answer has been read before the next one is written)
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  return ok ? static_cast<int>(x) : -1;
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -147,76 +210,64 @@ __global__ void __launch_bounds__(kThreads, 1)
   // 1024-byte alignment for the swizzle atoms
   unsigned char* smem = reinterpret_cast<unsigned char*>(
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  int* first = reinterpret_cast<int*>(smem + S::FIRST_OFF);  // [+inf, -inf, NaN][D]
+  Work* works = reinterpret_cast<Work*>(smem + S::WORK_OFF);
+  // By item parity and column, ten bits each: the first key (from the first tile that
+  // some row does not see whole) whose value is +inf, -inf, NaN.
+  uint32_t* first = reinterpret_cast<uint32_t*>(smem + S::FIRST_OFF);
+  constexpr uint32_t kNone = 0x3FFFFFFFu;
+  const uint32_t answer = smem_u32(smem + S::WORK_OFF + 2 * sizeof(Work));
   uint64_t* full_q = reinterpret_cast<uint64_t*>(smem + S::BAR_OFF);
-  uint64_t* full_k = full_q + 2;
+  uint64_t* empty_q = full_q + 2;
+  uint64_t* full_k = empty_q + 2;
   uint64_t* empty_k = full_k + S::KS;
   uint64_t* full_v = empty_k + S::KS;
-  uint64_t* seen_v = full_v + S::VS;   // looked through
-  uint64_t* empty_v = seen_v + S::VS;
-  uint64_t* full_s = empty_v + S::VS;  // scores are there (and earlier products done)
+  // the value tile has been looked through, and the next key tile of the item is there
+  uint64_t* seen = full_v + S::VS;
+  uint64_t* empty_v = seen + S::VS;
+  uint64_t* full_s = empty_v + S::VS;   // scores are there (and earlier products done)
   uint64_t* full_p = full_s + 2;
-  uint64_t* done = full_p + 2;         // the row tile's output is complete
-  uint64_t* retired = done + 2;        // used when a wait has run out
+  uint64_t* done = full_p + 2;          // the row tile's output is complete
+  uint64_t* free_o = done + 2;          // it has been read
+  uint64_t* full_w = free_o + 2;        // an item
+  uint64_t* empty_w = full_w + 2;
+  uint64_t* asked = empty_w + 2;
+  uint64_t* retired = asked + 1;        // used when a wait has run out
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(retired + 1);
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* odd = reinterpret_cast<int*>(tmem_slot + 2);  // `first` holds something
+  volatile int* odd = reinterpret_cast<volatile int*>(tmem_slot + 2);  // [2]: `first` holds something
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-
-  // this CTA's work
-  uint32_t flags = 0;
-  PromptWork w;
-  const int hx = (blockIdx.x / a.nsplit) % (a.kv_heads * a.hchunks);
-  w.z = blockIdx.x % a.nsplit;
-  w.kh = hx / a.hchunks;
-  w.g0 = hx % a.hchunks * a.hpt;
-  w.nh = min(a.hpt, a.group - w.g0);
-  w.tt = a.tpt / 2;
-  if (!attn_tile(a, blockIdx.x / (a.nsplit * a.kv_heads * a.hchunks), w.b, w.i0)) return;
-  w.rq = attn_request(a, w.b, flags);
-  if (flags && a.status && threadIdx.x == 0) atomicOr(a.status, flags);
-  flags = 0;
-  if (w.i0 >= w.rq.n) return;
-  w.k0 = w.z * a.chunk;
-  w.lim0 = attn_limit(w.rq, w.i0);
-  int lim1 = w.lim0;  // keys that the last token sees
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int i = w.i0 + s * w.tt, last = min(i + w.tt, w.rq.n) - 1;
-    w.n[s] = 0;
-    if (last < i) continue;
-    lim1 = attn_limit(w.rq, last);
-    w.n[s] = max(0, (min(lim1, w.k0 + a.chunk) - w.k0 + kKeys - 1) / kKeys);
+  if (warp == 9 && lane < 3) {
+    const CUtensorMap* m = lane == 0 ? &maps.q : lane == 1 ? &maps.k : &maps.v;
+    asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
   }
-  const bool alone = lim1 <= a.chunk;  // no other split has keys
-  const int nt = max(w.n[0], w.n[1]);
-  if (nt == 0 && w.z > 0) return;
-
   if (threadIdx.x == 0) {
     for (int s = 0; s < 2; ++s) {
       mbar_init(&full_q[s], 1);
+      mbar_init(&empty_q[s], 1);
       mbar_init(&full_s[s], 1);
       mbar_init(&full_p[s], 4);
       mbar_init(&done[s], 1);
+      mbar_init(&free_o[s], 4);
+      mbar_init(&full_w[s], 1);
+      mbar_init(&empty_w[s], kConsumers);
+      odd[s] = 0;
     }
     for (int s = 0; s < S::KS; ++s) {
       mbar_init(&full_k[s], 1);
-      mbar_init(&empty_k[s], 1);
+      mbar_init(&empty_k[s], 2);  // the issuer's, and the warp's that sees every key tile
     }
     for (int s = 0; s < S::VS; ++s) {
       mbar_init(&full_v[s], 1);
-      mbar_init(&seen_v[s], 2);
+      mbar_init(&seen[s], 4);
       mbar_init(&empty_v[s], 1);
     }
+    mbar_init(asked, 1);
     mbar_init(retired, 1);
     *abort = 0;
-    *odd = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  for (int i = threadIdx.x; i < 3 * D; i += kThreads) first[i] = INT32_MAX;
+  for (int i = threadIdx.x; i < 2 * D; i += kThreads) first[i] = kNone;
   if (warp == 8) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(
                      smem_u32(tmem_slot)),
@@ -228,150 +279,281 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int tt = a.tpt / 2;  // tokens of a row tile
+
+  // A wait of the roles whose work is safe to go on with whatever it finds (a wait
+  // that ran out raised *abort, and all later ones give up at once).
+  auto wait = [&](uint64_t* bar, uint32_t parity) {
+    if (!mbar_try_wait(bar, parity)) (void)mbar_wait(bar, parity, abort);
+    __syncwarp();
+  };
+
+  // The next item, into w: false where there is none (or a wait ran out, ok).  The
+  // softmax warps give its place back when they have finished it: an item reaches the
+  // others when all is done with the one before the last.
+  auto take = [&](int item, Work& w, bool& ok) -> bool {
+    ok = __all_sync(0xffffffffu, mbar_wait(&full_w[item & 1], (item >> 1) & 1, abort));
+    if (!ok) return false;
+    const int4* src = reinterpret_cast<const int4*>(&works[item & 1]);
+    int4* dst = reinterpret_cast<int4*>(&w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) dst[i] = src[i];
+    __syncwarp();
+    if (lane == 0 && warp >= 8) mbar_arrive(&empty_w[item & 1]);
+    return __reduce_or_sync(0xffffffffu, w.live) != 0;  // (a uniform register)
+  };
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 9) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp == 10) {
+      // ---------------- scheduler ----------------
+      int x = blockIdx.x, item = 0, asks = 0;
+      const int per = a.kv_heads * a.hchunks;
+      bool ok = true;
+      while (ok) {
+        if (x >= 0 && lane == 0) next_cta_ask(answer, asked);
+        Work w = {};
+        bool live = false;
+        uint32_t flags = 0;
+        if (x >= 0) {
+          w.z = x % a.nsplit;
+          const int hx = x / a.nsplit % per;
+          w.kh = hx / a.hchunks;
+          w.g0 = hx % a.hchunks * a.hpt;
+          w.nh = min(a.hpt, a.group - w.g0);
+          AttnRequest rq;
+          if (attn_tile(a, x / (a.nsplit * per), w.b, w.i0, rq, flags)) {
+            w.q0 = rq.q0;
+            w.n = rq.n;
+            w.kv = rq.kv;
+            if (w.i0 < rq.n) {
+              w.k0 = w.z * a.chunk;
+              w.lim0 = attn_limit(rq, w.i0);
+              int lim1 = w.lim0, n[2] = {0, 0};  // lim1: keys that the last token sees
+#pragma unroll
+              for (int s = 0; s < 2; ++s) {
+                const int i = w.i0 + s * tt, last = min(i + tt, rq.n) - 1;
+                if (last < i) continue;
+                lim1 = attn_limit(rq, last);
+                n[s] = max(0, (min(lim1, w.k0 + a.chunk) - w.k0 + kKeys - 1) / kKeys);
+              }
+              w.n0 = n[0];
+              w.n1 = n[1];
+              w.alone = lim1 <= a.chunk;
+              live = n[0] + n[1] > 0 || w.z == 0;
+            }
+          }
+        }
+        if (flags && a.status && lane == 0) atomicOr(a.status, flags);
+        if (live || x < 0) {
+          ok = __all_sync(0xffffffffu,
+                          mbar_wait(&empty_w[item & 1], ((item >> 1) & 1) ^ 1, abort));
+          if (!ok) break;
+          w.live = live;
+          if (lane == 0) {
+            works[item & 1] = w;
+            mbar_arrive(&full_w[item & 1]);
+          }
+          __syncwarp();
+          ++item;
+        }
+        if (x < 0) break;
+        ok = __all_sync(0xffffffffu, mbar_wait(asked, asks & 1, abort));
+        if (!ok) break;
+        ++asks;
+        x = next_cta(answer);
+        __syncwarp();
+      }
+      if (!ok && x >= 0) {  // the answer in flight lands before the CTA's memory goes
+        int drain = 0;
+        (void)mbar_wait(asked, asks & 1, &drain);
+      }
+    } else if (warp == 9) {
       // ---------------- TMA producer ----------------
       const int box = a.table ? min(kKeys, 1 << a.page_shift) : kKeys;  // keys of a box
       const int boxes = kKeys / box * S::HALVES;
       const int my = lane / S::HALVES, half = lane % S::HALVES;
-      const int32_t* table =
-          a.table ? a.table + static_cast<int64_t>(w.b) * a.table_width : nullptr;
-      // Lane l brings box l of a tile: its first slot.  Boxes behind the keys, or of
-      // a page that is none, lie past the cache and read as zeros.
-      auto entry = [&](int j) -> int {
-        const int key = w.k0 + kKeys * j + my * box;
-        return table && lane < boxes && j < nt && key < w.rq.kv
-                   ? __ldg(table + (key >> a.page_shift))
-                   : -1;
-      };
-      auto slot_of = [&](int page, int j) -> int {
-        const int key = w.k0 + kKeys * j + my * box;
-        if (key >= w.rq.kv || lane >= boxes) return static_cast<int>(a.slots);
-        if (!table) return w.rq.q0 + key;
-        const int64_t s = attn_slot(a, page, key);
-        if (s < 0) flags |= SSS_FLAG_INDEX;
-        return static_cast<int>(s < 0 ? a.slots : s);
-      };
-      if (elect_one()) {
-        for (int s = 0; s < 2; ++s) {
-          if (w.n[s] == 0) continue;
-          mbar_arrive_expect_tx(&full_q[s], w.nh * w.tt * 128 * S::HALVES);
-          for (int g = 0; g < w.nh; ++g)
-            for (int h = 0; h < S::HALVES; ++h)
-              tma_load_2d(&maps.q, &full_q[s],
-                          smem + s * S::Q_TILE + h * S::PART + g * w.tt * 128,
-                          (w.kh * a.group + w.g0 + g) * D + 64 * h, w.rq.q0 + w.i0 + s * w.tt);
-        }
-      }
-      __syncwarp();
-      int page = entry(0), j = 0;
-      bool ok = true;
-      for (; j < nt; ++j) {
-        const int slot = slot_of(page, j);
-        page = entry(j + 1);
-#pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          const int stages = kv ? S::VS : S::KS, st = j % stages;
-          uint64_t* full = (kv ? full_v : full_k) + st;
-          ok = ok && __all_sync(0xffffffffu, mbar_wait((kv ? empty_v : empty_k) + st,
-                                                       ((j / stages) & 1) ^ 1, abort));
-          if (!ok) break;
-          if (lane == 0) mbar_arrive_expect_tx(full, S::KV_TILE);
+      uint32_t flags = 0;
+      int kc = 0, vc = 0, qc[2] = {0, 0};  // tiles asked for
+      Work w;
+      bool ok;
+      for (int item = 0; take(item, w, ok); ++item) {
+        const int n[2] = {w.n0, w.n1}, nt = max(w.n0, w.n1);
+        const int32_t* table =
+            a.table ? a.table + static_cast<int64_t>(w.b) * a.table_width : nullptr;
+        // Lane l brings box l of a tile: its first slot.  Boxes behind the keys, or of
+        // a page that is none, lie past the cache and read as zeros.
+        auto entry = [&](int j) -> int {
+          const int key = w.k0 + kKeys * j + my * box;
+          return table && lane < boxes && j < nt && key < w.kv
+                     ? __ldg(table + (key >> a.page_shift))
+                     : -1;
+        };
+        auto slot_of = [&](int page, int j) -> int {
+          const int key = w.k0 + kKeys * j + my * box;
+          if (key >= w.kv || lane >= boxes) return static_cast<int>(a.slots);
+          if (!table) return w.q0 + key;
+          const int64_t s = attn_slot(a, page, key);
+          if (s < 0) flags |= SSS_FLAG_INDEX;
+          return static_cast<int>(s < 0 ? a.slots : s);
+        };
+        auto put = [&](const CUtensorMap* map, uint64_t* full, uint64_t* empty, int off, int stages,
+                       int& count, int slot) {
+          const int st = count % stages;
+          ok = ok && __all_sync(0xffffffffu,
+                                mbar_wait(empty + st, ((count / stages) & 1) ^ 1, abort));
+          if (!ok) return;
+          if (lane == 0) mbar_arrive_expect_tx(full + st, S::KV_TILE);
           __syncwarp();
           if (lane < boxes)
-            tma_load_2d(kv ? &maps.v : &maps.k, full,
-                        smem + (kv ? S::V_OFF : S::K_OFF) + st * S::KV_TILE + half * S::PART +
-                            my * box * 128,
+            tma_load_2d(map, full + st,
+                        smem + off + st * S::KV_TILE + half * S::PART + my * box * 128,
                         w.kh * D + 64 * half, slot);
           __syncwarp();
+          ++count;
+        };
+        int page = entry(0);
+        for (int j = 0; j < nt && ok; ++j) {
+          const int slot = slot_of(page, j);
+          page = entry(j + 1);
+          put(&maps.k, full_k, empty_k, S::K_OFF, S::KS, kc, slot);
+          if (j == 0) {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              if (n[s] == 0 || !ok) continue;
+              ok = __all_sync(0xffffffffu, mbar_wait(&empty_q[s], (qc[s] & 1) ^ 1, abort));
+              if (!ok) continue;
+              if (lane == 0) mbar_arrive_expect_tx(&full_q[s], w.nh * tt * 128 * S::HALVES);
+              __syncwarp();
+              if (lane < w.nh * S::HALVES)  // at most 16 heads
+                tma_load_2d(&maps.q, &full_q[s], smem + s * S::Q_TILE + half * S::PART + my * tt * 128,
+                            (w.kh * a.group + w.g0 + my) * D + 64 * half, w.q0 + w.i0 + s * tt);
+              __syncwarp();
+              ++qc[s];
+            }
+          }
+          put(&maps.v, full_v, empty_v, S::V_OFF, S::VS, vc, slot);
         }
         if (!ok) break;
       }
       if (flags && a.status) atomicOr(a.status, flags);
-      if (!ok) {
-        // let this CTA's copies still in flight land (of a barrier never used, the
-        // phase before its first counts as completed); tile j may have its keys only
+      if (!ok) {  // let this CTA's copies still in flight land
         int drain = 0;
         for (int s = 0; s < 2; ++s)
-          if (w.n[s] > 0) (void)mbar_wait(&full_q[s], 0, &drain);
-        for (int i = max(0, j - S::KS + 1); i <= j; ++i) {
-          const uint32_t par = (i / S::KS) & 1;
-          // (tile j's keys, where they were not asked for, are the stage's last ones)
-          if (i < j || mbar_test_wait(&empty_k[i % S::KS], par ^ 1u))
-            (void)mbar_wait(&full_k[i % S::KS], par, &drain);
-        }
-        for (int i = max(0, j - S::VS); i < j; ++i)
+          if (qc[s] > 0) (void)mbar_wait(&full_q[s], (qc[s] - 1) & 1, &drain);
+        for (int i = max(0, kc - S::KS); i < kc; ++i)
+          (void)mbar_wait(&full_k[i % S::KS], (i / S::KS) & 1, &drain);
+        for (int i = max(0, vc - S::VS); i < vc; ++i)
           (void)mbar_wait(&full_v[i % S::VS], (i / S::VS) & 1, &drain);
       }
     } else if (warp == 8) {
       // ---------------- issuer of the products ----------------
+      // What it costs beside the products is its waits (a few dependent instructions
+      // each, beside two softmax warps on the same scheduler): three a step.  Its
+      // control flow and operands are kept in uniform registers: a product then issues
+      // in the 64 cycles that it takes, else in 80 to 110.
       constexpr uint32_t id_s = idesc_of<T>(kKeys, false), id_o = idesc_of<T>(D, true);
       const uint32_t tm = __reduce_or_sync(0xffffffffu, tmem);
       const uint32_t base = smem_u32(smem);
-      auto wait = [&](uint64_t* bar, uint32_t parity) -> bool {
-        return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort));
-      };
-      auto scores = [&](int s, int j) {  // S_s = Q_s K_j^T
-        if (elect_one()) {
+      const uint32_t q_desc = desc_low(base, 0), k_desc = desc_low(base + S::K_OFF, 0);
+      const uint32_t v_desc = desc_low(base + S::V_OFF, S::PART);
+      constexpr uint32_t kStage = S::KV_TILE >> 4, kQ = S::Q_TILE >> 4, kPart = S::PART >> 4;
+      uint32_t count = 0;  // key tiles before
+      uint32_t qph = 0, pph = 0, oph = 3;  // bit s: the parities of row tile s
+      auto scores = [&](int s, uint32_t st) {  // S_s = Q_s K^T of stage st
 #pragma unroll
-          for (int h = 0; h < S::HALVES; ++h) {
-            const uint64_t qd = sw128_desc(base + s * S::Q_TILE + h * S::PART);
-            const uint64_t kd =
-                sw128_desc(base + S::K_OFF + (j % S::KS) * S::KV_TILE + h * S::PART);
-#pragma unroll
-            for (int kk = 0; kk < 4; ++kk)
-              mma_ss(tm + s * kKeys, qd + 2 * kk, kd + 2 * kk, id_s, h + kk > 0);
-          }
-          umma_commit(&full_s[s]);
-        }
-        __syncwarp();
+        for (int h = 0; h < S::HALVES; ++h)
+          mma4_ss(tm + s * kKeys, q_desc + s * kQ + h * kPart, k_desc + st * kStage + h * kPart,
+                  id_s, h > 0);
+        umma_commit(&full_s[s]);
       };
-      bool go = true;
-      for (int s = 0; s < 2; ++s)
-        if (w.n[s] > 0) go = go && wait(&full_q[s], 0);
-      if (nt > 0) go = go && wait(&full_k[0], 0);
-      tc_fence_after();
-      if (go && nt > 0) {
-        for (int s = 0; s < 2; ++s)
-          if (w.n[s] > 0) scores(s, 0);
-        if (elect_one()) umma_commit(&empty_k[0]);
+      auto outputs = [&](int s, uint32_t st, uint32_t acc) {  // O_s += P_s V
+        mma4_ts(tm + 2 * kKeys + s * D, tm + s * kKeys, v_desc + st * kStage, id_o, acc);
+        mma4_ts(tm + 2 * kKeys + s * D, tm + s * kKeys + 32, v_desc + st * kStage + 512, id_o, 1);
+      };
+      for (uint32_t item = 0;; ++item) {
+        if (!__all_sync(0xffffffffu, mbar_wait(&full_w[item & 1], item >> 1 & 1, abort))) break;
+        const volatile Work* w = &works[item & 1];
+        const uint32_t n0 = __reduce_or_sync(0xffffffffu, w->n0);
+        const uint32_t n1 = __reduce_or_sync(0xffffffffu, w->n1);
+        const uint32_t live = __reduce_or_sync(0xffffffffu, w->live);
+        if (lane == 0) mbar_arrive(&empty_w[item & 1]);
         __syncwarp();
-      }
-      for (int j = 0; j < nt && go; ++j) {
-        go = wait(&seen_v[j % S::VS], (j / S::VS) & 1);
-        const uint32_t vbase = base + S::V_OFF + (j % S::VS) * S::KV_TILE;
-        bool have_k = false;
-        for (int s = 0; s < 2 && go; ++s) {
-          if (j >= w.n[s]) continue;
-          go = wait(&full_p[s], j & 1);
-          if (!go) break;
+        if (live == 0) break;
+        const uint32_t nt = max(n0, n1);
+        if (nt == 0) continue;
+        wait(&full_k[count % S::KS], count / S::KS & 1);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint32_t n = s ? n1 : n0;
+          if (n == 0) continue;
+          wait(&full_q[s], qph >> s & 1);
+          qph ^= 1u << s;
           tc_fence_after();
           if (elect_one()) {
-#pragma unroll
-            for (int kk = 0; kk < kKeys / 16; ++kk)  // O_s += P_s V_j
-              mma_ts(tm + 2 * kKeys + s * D, tm + s * kKeys + 8 * kk,
-                     mn_desc(vbase + kk * 2048, S::PART), id_o, j + kk > 0);
-            if (j + 1 == w.n[s]) umma_commit(&done[s]);
+            scores(s, count % S::KS);
+            if (n == 1) umma_commit(&empty_q[s]);
           }
           __syncwarp();
-          if (j + 1 < w.n[s]) {
-            if (!have_k) {
-              go = wait(&full_k[(j + 1) % S::KS], ((j + 1) / S::KS) & 1);
-              if (!go) break;
-              tc_fence_after();
-              have_k = true;
-            }
-            scores(s, j + 1);
-          }
         }
-        if (!go) break;
-        if (elect_one()) {
-          umma_commit(&empty_v[j % S::VS]);
-          if (j + 1 < nt) umma_commit(&empty_k[(j + 1) % S::KS]);
-        }
+        if (elect_one()) umma_commit(&empty_k[count % S::KS]);
         __syncwarp();
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {  // the outputs of the item before have been read
+          if ((s ? n1 : n0) == 0) continue;
+          wait(&free_o[s], oph >> s & 1);
+          oph ^= 1u << s;
+        }
+        // while both row tiles have at least two key tiles ahead
+        const uint32_t both = min(n0, n1) > 2 ? min(n0, n1) - 2 : 0;
+        uint32_t j = 0;
+#pragma unroll 1
+        for (; j < both; ++j, ++count) {
+          const uint32_t st = count % S::KS, st1 = (count + 1) % S::KS;
+          wait(&seen[st], count / S::KS & 1);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            wait(&full_p[s], pph >> s & 1);
+            tc_fence_after();
+            if (elect_one()) {
+              outputs(s, st, j > 0);
+              scores(s, st1);
+              if (s == 1) {
+                umma_commit(&empty_v[st]);
+                umma_commit(&empty_k[st1]);
+              }
+            }
+            __syncwarp();
+          }
+          pph ^= 3;
+        }
+#pragma unroll 1
+        for (; j < nt; ++j, ++count) {
+          const uint32_t st = count % S::KS, st1 = (count + 1) % S::KS;
+          wait(&seen[st], count / S::KS & 1);
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const uint32_t n = s ? n1 : n0;
+            if (j >= n) continue;
+            wait(&full_p[s], pph >> s & 1);
+            pph ^= 1u << s;
+            tc_fence_after();
+            if (elect_one()) {
+              outputs(s, st, j > 0);
+              if (j + 1 == n) umma_commit(&done[s]);
+              if (j + 1 < n) scores(s, st1);
+              if (j + 2 == n) umma_commit(&empty_q[s]);
+            }
+            __syncwarp();
+          }
+          if (elect_one()) {
+            umma_commit(&empty_v[st]);
+            if (j + 1 < nt) umma_commit(&empty_k[st1]);
+          }
+          __syncwarp();
+        }
       }
       if (*abort) {  // products still in flight must retire before the memory goes
         int drain = 0;
@@ -379,154 +561,220 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         (void)mbar_wait(retired, 0u, &drain);
       }
-    } else {
+    } else if (warp >= 12) {
       // ---------------- values that are infinite or NaN ----------------
       // (also with nothing to look for these warps see every tile's phase in turn)
       constexpr uint32_t kExp2 = Pair<T>::kExp * 0x10001u;
       constexpr uint32_t kOne2 = (Pair<T>::kExp & (~Pair<T>::kExp + 1)) * 0x10001u;
-      const int t64 = threadIdx.x - 320;
-      for (int j = 0; j < nt; ++j) {
-        const int st = j % S::VS;
-        if (!__all_sync(0xffffffffu, mbar_wait(&full_v[st], (j / S::VS) & 1, abort))) break;
-        const int key0 = w.k0 + kKeys * j;
-        if (key0 + kKeys > w.lim0) {
-          unsigned char* tile = smem + S::V_OFF + st * S::KV_TILE;
-          constexpr int PIECES = S::KV_TILE / 16 / 64;  // of a thread
-          uint32_t found = 0;
-#pragma unroll 8
-          for (int i = 0; i < PIECES; ++i) {
-            const uint4 u = *reinterpret_cast<const uint4*>(tile + (t64 + 64 * i) * 16);
-            // an exponent of all ones carries into the sign's place
-            found |= ((u.x & kExp2) + kOne2) | ((u.y & kExp2) + kOne2) |
-                     ((u.z & kExp2) + kOne2) | ((u.w & kExp2) + kOne2);
-          }
-          if (found & 0x80008000u) {
-            for (int i = 0; i < PIECES; ++i) {
-              const int p = t64 + 64 * i, row = p / 8 % kKeys, half = p / (8 * kKeys);
-              uint16_t* v16 = reinterpret_cast<uint16_t*>(tile + p * 16);
-              for (int e = 0; e < 8; ++e) {
-                const uint16_t x = v16[e];
-                if ((x & Pair<T>::kExp) != Pair<T>::kExp) continue;
-                const int d = 64 * half + 8 * ((p & 7) ^ (row & 7)) + e;
-                const bool nan = (x & 0x7FFFu) != Pair<T>::kExp;
-                atomicMin(&first[(nan ? 2 : x >> 15) * D + d], key0 + row);
-                v16[e] = 0;
-              }
-            }
-            *odd = 1;
-            __threadfence_block();
-          }
-          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      const int t128 = threadIdx.x - 384;
+      int vs = 0;
+      uint32_t vph = 0;
+      bool ok = true;
+      Work w;
+      for (int item = 0;; ++item) {
+        const bool live = ok && take(item, w, ok);
+        // (the four warps leave together, and clear together the notes of the item
+        // before the last)
+        uint32_t stop;
+        asm volatile(
+            "{\n .reg .pred p, q;\n setp.eq.u32 q, %1, 0;\n bar.red.or.pred p, 1, 128, q;\n"
+            " selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(stop)
+            : "r"(live ? 1u : 0u)
+            : "memory");
+        if (stop) break;
+        const int used = odd[item & 1];
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (used) {
+          if (t128 < D) first[(item & 1) * D + t128] = kNone;
+          odd[item & 1] = 0;
         }
-        __syncwarp();
-        if (lane == 0 && !(a.stall && j == 0 && warp == 11)) mbar_arrive(&seen_v[st]);
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        const int nt = max(w.n0, w.n1), from = max(w.lim0 - w.k0, 0) / kKeys;
+        for (int j = 0; j < nt && ok; ++j) {
+          ok = __all_sync(0xffffffffu, mbar_wait(&full_v[vs], vph, abort));
+          // (one warp also sees every key tile)
+          if (warp == 12 && ok) {
+            if (j == 0) {
+              ok = __all_sync(0xffffffffu, mbar_wait(&full_k[vs], vph, abort));
+              if (lane == 0) mbar_arrive(&empty_k[vs]);
+            }
+            const int vs1 = vs + 1 == S::VS ? 0 : vs + 1;
+            if (j + 1 < nt && ok) {
+              ok = __all_sync(0xffffffffu,
+                              mbar_wait(&full_k[vs1], vph ^ (vs1 == 0 ? 1 : 0), abort));
+              if (lane == 0) mbar_arrive(&empty_k[vs1]);
+            }
+          }
+          if (!ok) break;
+          if (j >= from) {
+            unsigned char* tile = smem + S::V_OFF + vs * S::KV_TILE;
+            constexpr int PIECES = S::KV_TILE / 16 / 128;  // of a thread
+            uint32_t found = 0;
+#pragma unroll 4
+            for (int i = 0; i < PIECES; ++i) {
+              const uint4 u = *reinterpret_cast<const uint4*>(tile + (t128 + 128 * i) * 16);
+              // an exponent of all ones carries into the sign's place
+              found |= ((u.x & kExp2) + kOne2) | ((u.y & kExp2) + kOne2) |
+                       ((u.z & kExp2) + kOne2) | ((u.w & kExp2) + kOne2);
+            }
+            if (found & 0x80008000u) {
+              for (int i = 0; i < PIECES; ++i) {
+                const int p = t128 + 128 * i, row = p / 8 % kKeys, half = p / (8 * kKeys);
+                uint16_t* v16 = reinterpret_cast<uint16_t*>(tile + p * 16);
+                for (int e = 0; e < 8; ++e) {
+                  const uint16_t x = v16[e];
+                  if ((x & Pair<T>::kExp) != Pair<T>::kExp) continue;
+                  const int d = 64 * half + 8 * ((p & 7) ^ (row & 7)) + e;
+                  const bool nan = (x & 0x7FFFu) != Pair<T>::kExp;
+                  const uint32_t key = kKeys * (j - from) + row;  // < 128 + 256 + 128
+                  const int at = nan ? 20 : 10 * (x >> 15);
+                  uint32_t* word = &first[(item & 1) * D + d];
+                  uint32_t old = *word;
+                  while (key < ((old >> at) & 1023u)) {
+                    const uint32_t have =
+                        atomicCAS(word, old, (old & ~(1023u << at)) | key << at);
+                    if (have == old) break;
+                    old = have;
+                  }
+                  v16[e] = 0;
+                }
+              }
+              odd[item & 1] = 1;
+              __threadfence_block();
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          __syncwarp();
+          if (lane == 0 && !(a.stall && item == 0 && j == 0 && warp == 15)) mbar_arrive(&seen[vs]);
+          if (++vs == S::VS) {
+            vs = 0;
+            vph ^= 1;
+          }
+        }
       }
     }
   } else {
     // ---------------- softmax ----------------
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     const int s = warp >> 2;  // row tile
     const int row = 32 * (warp & 3) + lane;
-    const int g = row / w.tt, i = w.i0 + s * w.tt + row - g * w.tt;
-    const bool in = g < w.nh && i < w.rq.n;
-    const int lim = in ? attn_limit(w.rq, i) : 0;
-    // keys that all rows of the row tile see
-    const int whole = attn_limit(w.rq, min(w.i0 + s * w.tt, w.rq.n - 1));
+    const int g = row / tt;   // head, and token of the row tile
+    const int ti = s * tt + row - g * tt;
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
     const uint32_t sc_col = lanes + s * kKeys, o_col = lanes + 2 * kKeys + s * D;
-    float mx = -INFINITY;
-    float2 sum = make_float2(0.f, 0.f);
-    bool ok = true;
-    const int n = w.n[s];
-    for (int j = 0; j < n; ++j) {
-      ok = __all_sync(0xffffffffu, mbar_wait(&full_s[s], j & 1, abort));
-      if (!ok) break;
-      tc_fence_after();
-      uint32_t v[4][32];
+    uint32_t sph = 0, dph = 0;
+    bool ok;
+    Work w;
+    for (int item = 0; take(item, w, ok); ++item) {
+      const AttnRequest rq = {w.q0, w.n, w.kv};
+      const int i = w.i0 + ti;
+      const bool in = g < w.nh && i < w.n;
+      const int lim = in ? attn_limit(rq, i) : 0;
+      // keys that all rows of the row tile see
+      const int whole = attn_limit(rq, min(w.i0 + s * tt, w.n - 1));
+      const int n = s ? w.n1 : w.n0;
+      float mx = -INFINITY;
+      float2 sum[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) tmem_ld_async<32>(sc_col + 32 * c, v[c]);
-      tmem_wait_ld();
+      for (int x = 0; x < 4; ++x) sum[x] = make_float2(0.f, 0.f);
+      for (int j = 0; j < n; ++j) {
+        wait(&full_s[s], sph);
+        sph ^= 1;
+        tc_fence_after();
+        uint32_t v[4][32];
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int x = 0; x < 32; ++x) asm volatile("" : "+r"(v[c][x]));  // (not before the wait)
-      const int key0 = w.k0 + kKeys * j;
-      if (key0 + kKeys > whole) {
+        for (int c = 0; c < 4; ++c) tmem_ld_async<32>(sc_col + 32 * c, v[c]);
+        tmem_wait_ld();
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int x = 0; x < 32; ++x)
-            if (key0 + 32 * c + x >= lim) v[c][x] = 0xFF800000u;
-      }
-      float t[4];
+          for (int x = 0; x < 32; ++x) asm volatile("" : "+r"(v[c][x]));  // (not before the wait)
+        const int key0 = w.k0 + kKeys * j;
+        if (key0 + kKeys > whole) {
+          const int left = lim - key0;
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        t[c] = __uint_as_float(v[c][0]);
+          for (int c = 0; c < 4; ++c) {
+            if (key0 + 32 * c + 32 <= whole) continue;
 #pragma unroll
-        for (int x = 1; x < 32; ++x) t[c] = fmaxf(t[c], __uint_as_float(v[c][x]));
-      }
-      const float top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
-      if (__any_sync(0xffffffffu, (top - mx) * a.scale_log2 > kRaise)) {
-        const float to = fmaxf(mx, top);
-        const float f = to == -INFINITY ? 1.f : ex2((mx - to) * a.scale_log2);
-        mx = to;
-        sum.x *= f;
-        sum.y *= f;
-        if (j > 0) {
-#pragma unroll
-          for (int c = 0; c < D / 16; ++c) {
-            uint32_t o[16];
-            tmem_ld_async<16>(o_col + 16 * c, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              asm volatile("" : "+r"(o[x]));
-              o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
-            }
-            tmem_st16(o_col + 16 * c, o);
+            for (int x = 0; x < 32; ++x)
+              if (32 * c + x >= left) v[c][x] = 0xFF800000u;
           }
         }
-      }
-      const float neg = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
+        float t[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
+        for (int c = 0; c < 4; ++c) {
+          t[c] = __uint_as_float(v[c][0]);
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint32_t p[8];
+          for (int x = 1; x < 31; x += 2)
+            t[c] = max3(t[c], __uint_as_float(v[c][x]), __uint_as_float(v[c][x + 1]));
+          t[c] = fmaxf(t[c], __uint_as_float(v[c][31]));
+        }
+        const float top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
+        if (__any_sync(0xffffffffu, (top - mx) * a.scale_log2 > kRaise)) {
+          const float to = fmaxf(mx, top);
+          const float f = to == -INFINITY ? 1.f : ex2((mx - to) * a.scale_log2);
+          mx = to;
 #pragma unroll
-          for (int x = 0; x < 8; ++x) {
-            float2 y = fma2(__uint_as_float(v[c][16 * hf + 2 * x]),
-                            __uint_as_float(v[c][16 * hf + 2 * x + 1]), a.scale_log2, neg);
+          for (int x = 0; x < 4; ++x) sum[x] = make_float2(sum[x].x * f, sum[x].y * f);
+          if (j > 0) {
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t o[16];
+              tmem_ld_async<16>(o_col + 16 * c, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int x = 0; x < 16; ++x) {
+                asm volatile("" : "+r"(o[x]));
+                o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+              }
+              tmem_st16(o_col + 16 * c, o);
+            }
+          }
+        }
+        const float neg = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t p[16];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            float2 y = fma2(__uint_as_float(v[c][2 * x]), __uint_as_float(v[c][2 * x + 1]),
+                            a.scale_log2, neg);
             y.x = ex2(y.x);
             y.y = ex2(y.y);
-            sum = add2(sum, y);
+            sum[x & 3] = add2(sum[x & 3], y);
             p[x] = Pair<T>::pack(y.x, y.y);
           }
-#pragma unroll
-          for (int x = 0; x < 8; ++x) v[c][8 * hf + x] = p[x];
+          tmem_st16(sc_col + 16 * c, p);
         }
-        uint32_t st[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) st[x] = v[c][x];
-        tmem_st16(sc_col + 16 * c, st);
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full_p[s]);
       }
-      tmem_wait_st();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&full_p[s]);
-    }
-    // the row's output
-    if (n > 0 && ok) ok = __all_sync(0xffffffffu, mbar_wait(&done[s], 0, abort));
-    if (ok) {
-      tc_fence_after();
-      const float total = sum.x + sum.y;
+      // the row's output
+      if (n > 0) {
+        wait(&done[s], dph);
+        dph ^= 1;
+        tc_fence_after();
+      }
+      const float2 s01 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+      const float total = s01.x + s01.y;
       const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
-      const int64_t at = static_cast<int64_t>(w.rq.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
+      const int64_t at = static_cast<int64_t>(w.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
       const int64_t zat = static_cast<int64_t>(w.z) * a.tokens * a.heads + at;
-      const bool mark = *reinterpret_cast<volatile int*>(odd) != 0;
-#pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
+      const bool mark = odd[item & 1] != 0;
+      const uint32_t* notes = first + (item & 1) * D;
+      const int seen = lim - w.k0 - max(w.lim0 - w.k0, 0) / kKeys * kKeys;
+      // 128 bytes of each of the warp's rows at a time: through shared memory (swizzled
+      // in 16-byte pieces), so that a store writes whole rows of four
+      unsigned char* stage = smem + S::OUT_OFF + warp * 4096;
+      const uint32_t mine = smem_u32(stage) + lane * 128;
+      const uint32_t from = smem_u32(stage) + (lane >> 3) * 128;
+      const uint32_t rows_in = __ballot_sync(0xffffffffu, in);
+      char* base = w.alone ? static_cast<char*>(a.out) + at * (D * 2)
+                           : reinterpret_cast<char*>(a.part) + zat * (D * 4);
+      auto fetch = [&](int c, uint32_t (&o)[32]) {  // 32 columns of the output
         if (n > 0) {
           tmem_ld32(o_col + 32 * c, o);
 #pragma unroll
@@ -535,39 +783,71 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int x = 0; x < 32; ++x) o[x] = 0;
         }
-        if (in) {
+        if (n > 0 && c == D / 32 - 1) {
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&free_o[s]);
+        }
+#pragma unroll
+        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * r);
+        if (mark) {
 #pragma unroll
           for (int x = 0; x < 32; ++x) {
-            float y = __uint_as_float(o[x]) * r;
-            if (mark) {
-              const int d = 32 * c + x;
-              if (first[d] < lim) y += INFINITY;
-              if (first[D + d] < lim) y -= INFINITY;
-              if (first[2 * D + d] < lim) y = NAN;
-            }
+            float y = __uint_as_float(o[x]);
+            const uint32_t f = notes[32 * c + x];
+            if (static_cast<int>(f & 1023u) < seen) y += INFINITY;
+            if (static_cast<int>((f >> 10) & 1023u) < seen) y -= INFINITY;
+            if (static_cast<int>(f >> 20) < seen) y = NAN;
             o[x] = __float_as_uint(y);
           }
-          if (alone) {
-            uint4* dst = reinterpret_cast<uint4*>(static_cast<T*>(a.out) + at * D + 32 * c);
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const uint32_t* y = o + 8 * x;
-              dst[x] = make_uint4(Pair<T>::pack(__uint_as_float(y[0]), __uint_as_float(y[1])),
-                                  Pair<T>::pack(__uint_as_float(y[2]), __uint_as_float(y[3])),
-                                  Pair<T>::pack(__uint_as_float(y[4]), __uint_as_float(y[5])),
-                                  Pair<T>::pack(__uint_as_float(y[6]), __uint_as_float(y[7])));
-            }
-          } else {
-            uint4* dst = reinterpret_cast<uint4*>(a.part + zat * D + 32 * c);
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-              dst[x] = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
-          }
         }
+      };
+      auto flush = [&](const uint32_t (&o)[32], int off) {
         __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 8; ++x)
+          asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(mine + ((x ^ (lane & 7)) * 16)),
+                       "r"(o[4 * x]), "r"(o[4 * x + 1]), "r"(o[4 * x + 2]), "r"(o[4 * x + 3])
+                       : "memory");
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 8; ++x) {
+          const int row = 4 * x + (lane >> 3);
+          uint4 u;
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
+                       : "r"(from + x * 512 + (((lane & 7) ^ (row & 7)) * 16))
+                       : "memory");
+          char* dst = reinterpret_cast<char*>(
+              __shfl_sync(0xffffffffu, reinterpret_cast<uintptr_t>(base), row));
+          if (rows_in >> row & 1) *reinterpret_cast<uint4*>(dst + off + (lane & 7) * 16) = u;
+        }
+      };
+      if (w.alone) {
+#pragma unroll 1
+        for (int c = 0; c < D / 64; ++c) {
+          uint32_t o[32], lo[32];
+          fetch(2 * c, lo);
+          fetch(2 * c + 1, o);
+          uint32_t p[32];
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            p[x] = Pair<T>::pack(__uint_as_float(lo[2 * x]), __uint_as_float(lo[2 * x + 1]));
+            p[16 + x] = Pair<T>::pack(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
+          }
+          flush(p, 128 * c);
+        }
+      } else {
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32];
+          fetch(c, o);
+          flush(o, 128 * c);
+        }
+        if (in) a.part_lse[zat] = total == 0.f ? -INFINITY : mx * a.scale_log2 + log2f(total);
       }
-      if (in && !alone)
-        a.part_lse[zat] = total == 0.f ? -INFINITY : mx * a.scale_log2 + log2f(total);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&empty_w[item & 1]);
     }
   }
   tc_fence_before();

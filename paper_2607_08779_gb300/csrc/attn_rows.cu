@@ -91,9 +91,9 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
   const int kh = hx / a.hchunks, g0 = hx % a.hchunks * a.hpt;
   const int nh = min(a.hpt, a.group - g0);  // heads of the tile
   int b, i0;
-  if (!attn_tile(a, tile, b, i0)) return;
   uint32_t flags = 0;
-  const AttnRequest rq = attn_request(a, b, flags);
+  AttnRequest rq;
+  if (!attn_tile(a, tile, b, i0, rq, flags)) return;
   const int nt = min(a.tpt, rq.n - i0);  // tokens of the tile
   if (nt <= 0) {
     if (flags && a.status && threadIdx.x == 0) atomicOr(a.status, flags);

@@ -34,3 +34,20 @@ def test_single_tokens_have_no_waits_to_stall():
         sss.sss_test_set_stall(0)
     assert int(status) == 0
     check(c, got)
+
+
+def test_short_items_in_a_row_never_wait_in_vain():
+    # requests of one to sixteen key tiles, many to a CTA: whatever role is late, no
+    # wait runs out and the bits are the same every time
+    fresh = [264, 271, 151, 374, 1200, 164, 36, 32, 342, 26, 129, 128, 257]
+    c = make(fresh, fresh, 64, 8, 128, BF, 0, seed=32)
+    cache = sss.KVCache(c["k"].cuda(), c["v"].cuda())
+    q = c["q"].cuda()
+    cu = torch.tensor(c["cu"], dtype=torch.int32, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    first = sss.sss_attention(q, cache, cu, None, 1200, 1200, dev_status=status)
+    for _ in range(200):
+        out = sss.sss_attention(q, cache, cu, None, 1200, 1200, dev_status=status)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    assert torch.equal(out, first)
