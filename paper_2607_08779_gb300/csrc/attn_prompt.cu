@@ -152,6 +152,14 @@ __device__ __forceinline__ float2 fma2(float x0, float x1, float s, float t) {
       : "f"(x0), "f"(x1), "f"(s), "f"(t));
   return r;
 }
+__device__ __forceinline__ float2 mul2(float x0, float x1, float s) {
+  float2 r;
+  asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %4};\n"
+      " mul.rn.f32x2 d, a, b;\n mov.b64 {%0, %1}, d;\n}\n"
+      : "=f"(r.x), "=f"(r.y)
+      : "f"(x0), "f"(x1), "f"(s));
+  return r;
+}
 __device__ __forceinline__ float2 add2(float2 x, float2 y) {
   float2 r;
   asm("{\n .reg .b64 a, b, d;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
@@ -763,9 +771,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
       const int64_t at = static_cast<int64_t>(w.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
       const int64_t zat = static_cast<int64_t>(w.z) * a.tokens * a.heads + at;
-      const bool mark = odd[item & 1] != 0;
-      const uint32_t* notes = first + (item & 1) * D;
-      const int seen = lim - w.k0 - max(w.lim0 - w.k0, 0) / kKeys * kKeys;
       // 128 bytes of each of the warp's rows at a time: through shared memory (swizzled
       // in 16-byte pieces), so that a store writes whole rows of four
       unsigned char* stage = smem + S::OUT_OFF + warp * 4096;
@@ -782,24 +787,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         } else {
 #pragma unroll
           for (int x = 0; x < 32; ++x) o[x] = 0;
-        }
-        if (n > 0 && c == D / 32 - 1) {
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&free_o[s]);
-        }
-#pragma unroll
-        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * r);
-        if (mark) {
-#pragma unroll
-          for (int x = 0; x < 32; ++x) {
-            float y = __uint_as_float(o[x]);
-            const uint32_t f = notes[32 * c + x];
-            if (static_cast<int>(f & 1023u) < seen) y += INFINITY;
-            if (static_cast<int>((f >> 10) & 1023u) < seen) y -= INFINITY;
-            if (static_cast<int>(f >> 20) < seen) y = NAN;
-            o[x] = __float_as_uint(y);
-          }
         }
       };
       auto flush = [&](const uint32_t (&o)[32], int off) {
@@ -823,17 +810,22 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (rows_in >> row & 1) *reinterpret_cast<uint4*>(dst + off + (lane & 7) * 16) = u;
         }
       };
+      // (Compact code, each path in a loop of its own: it runs once an item, out of
+      // the instruction caches.  Unrolled, with the rare path below inlined for every
+      // value, it took 4500 to 6000 cycles.)
       if (w.alone) {
 #pragma unroll 1
         for (int c = 0; c < D / 64; ++c) {
-          uint32_t o[32], lo[32];
-          fetch(2 * c, lo);
-          fetch(2 * c + 1, o);
           uint32_t p[32];
 #pragma unroll
-          for (int x = 0; x < 16; ++x) {
-            p[x] = Pair<T>::pack(__uint_as_float(lo[2 * x]), __uint_as_float(lo[2 * x + 1]));
-            p[16 + x] = Pair<T>::pack(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]));
+          for (int h = 0; h < 2; ++h) {
+            uint32_t o[32];
+            fetch(2 * c + h, o);
+#pragma unroll
+            for (int x = 0; x < 16; ++x) {
+              const float2 y = mul2(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]), r);
+              p[16 * h + x] = Pair<T>::pack(y.x, y.y);
+            }
           }
           flush(p, 128 * c);
         }
@@ -842,9 +834,41 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
           fetch(c, o);
+#pragma unroll
+          for (int x = 0; x < 16; ++x) {
+            const float2 y = mul2(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]), r);
+            o[2 * x] = __float_as_uint(y.x);
+            o[2 * x + 1] = __float_as_uint(y.y);
+          }
           flush(o, 128 * c);
         }
         if (in) a.part_lse[zat] = total == 0.f ? -INFINITY : mx * a.scale_log2 + log2f(total);
+      }
+      if (n > 0) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&free_o[s]);
+      }
+      if (odd[item & 1]) {  // infinite and NaN values that the row sees
+        const uint32_t* notes = first + (item & 1) * D;
+        const int seen_keys = lim - w.k0 - max(w.lim0 - w.k0, 0) / kKeys * kKeys;
+        __syncwarp();
+#pragma unroll 1
+        for (int d = 0; d < D && in; ++d) {
+          const uint32_t f = notes[d];
+          float y = 0.f;
+          if (static_cast<int>(f & 1023u) < seen_keys) y += INFINITY;
+          if (static_cast<int>((f >> 10) & 1023u) < seen_keys) y -= INFINITY;
+          if (static_cast<int>(f >> 20) < seen_keys) y = NAN;
+          if (y == 0.f) continue;
+          if (w.alone) {
+            uint16_t* at16 = reinterpret_cast<uint16_t*>(base) + d;
+            *at16 = static_cast<uint16_t>(Pair<T>::pack(y + Pair<T>::value(*at16), 0.f));
+          } else {
+            reinterpret_cast<float*>(base)[d] += y;
+          }
+        }
+        __syncwarp();
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty_w[item & 1]);
