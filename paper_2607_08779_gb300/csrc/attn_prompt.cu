@@ -60,6 +60,7 @@ constexpr int kConsumers = 14;  // warps that read an item
 
 struct AttnMaps {
   CUtensorMap q, k, v;
+  CUtensorMap out;  // boxes of 64 columns of 8 tokens
 };
 
 template <int D>
@@ -245,8 +246,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   volatile int* odd = reinterpret_cast<volatile int*>(tmem_slot + 2);  // [2]: `first` holds something
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (warp == 9 && lane < 3) {
-    const CUtensorMap* m = lane == 0 ? &maps.q : lane == 1 ? &maps.k : &maps.v;
+  if (warp == 9 && lane < 4) {
+    const CUtensorMap* m = &maps.q + lane;
     asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
   }
   if (threadIdx.x == 0) {
@@ -326,13 +327,19 @@ __global__ void __launch_bounds__(kThreads, 1)
         bool live = false;
         uint32_t flags = 0;
         if (x >= 0) {
-          w.z = x % a.nsplit;
-          const int hx = x / a.nsplit % per;
-          w.kh = hx / a.hchunks;
-          w.g0 = hx % a.hchunks * a.hpt;
+          int tile = x / per, hx = x - tile * per;
+          if (a.nsplit > 1) {
+            w.z = tile % a.nsplit;
+            tile /= a.nsplit;
+          }
+          w.kh = hx;
+          if (a.hchunks > 1) {
+            w.kh = hx / a.hchunks;
+            w.g0 = (hx - w.kh * a.hchunks) * a.hpt;
+          }
           w.nh = min(a.hpt, a.group - w.g0);
           AttnRequest rq;
-          if (attn_tile(a, x / (a.nsplit * per), w.b, w.i0, rq, flags)) {
+          if (attn_tile(a, tile, w.b, w.i0, rq, flags)) {
             w.q0 = rq.q0;
             w.n = rq.n;
             w.kv = rq.kv;
@@ -771,33 +778,42 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
       const int64_t at = static_cast<int64_t>(w.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
       const int64_t zat = static_cast<int64_t>(w.z) * a.tokens * a.heads + at;
-      // 128 bytes of each of the warp's rows at a time: through shared memory (swizzled
-      // in 16-byte pieces), so that a store writes whole rows of four
+      // 128 bytes of each of the warp's rows at a time, through shared memory (rows in
+      // swizzled atoms of eight).  Eight rows are eight tokens of a head: a TMA store
+      // takes them while the warp goes on; those at a request's end, and partial
+      // results, are stored by the warp, four rows at a time.
       unsigned char* stage = smem + S::OUT_OFF + warp * 4096;
       const uint32_t mine = smem_u32(stage) + lane * 128;
-      const uint32_t from = smem_u32(stage) + (lane >> 3) * 128;
       const uint32_t rows_in = __ballot_sync(0xffffffffu, in);
       char* base = w.alone ? static_cast<char*>(a.out) + at * (D * 2)
                            : reinterpret_cast<char*>(a.part) + zat * (D * 4);
-      auto fetch = [&](int c, uint32_t (&o)[32]) {  // 32 columns of the output
-        if (n > 0) {
-          tmem_ld32(o_col + 32 * c, o);
-#pragma unroll
-          for (int x = 0; x < 32; ++x) asm volatile("" : "+r"(o[x]));
-        } else {
-#pragma unroll
-          for (int x = 0; x < 32; ++x) o[x] = 0;
-        }
-      };
-      auto flush = [&](const uint32_t (&o)[32], int off) {
+      auto put = [&](const uint32_t (&o)[32], int off, int c, bool boxes) {
+        asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (of this stage)
         __syncwarp();
 #pragma unroll
         for (int x = 0; x < 8; ++x)
           asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(mine + ((x ^ (lane & 7)) * 16)),
                        "r"(o[4 * x]), "r"(o[4 * x + 1]), "r"(o[4 * x + 2]), "r"(o[4 * x + 3])
                        : "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-#pragma unroll
+        uint32_t left = rows_in;
+        if (boxes) {
+          // lane 8 k: rows 8 k .. 8 k + 7, if all are tokens of the request
+          const bool whole = (rows_in >> (lane & 24) & 255u) == 255u;
+          if ((lane & 7) == 0 && whole)
+            asm volatile(
+                "cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                    reinterpret_cast<uint64_t>(&maps.out)),
+                "r"((w.kh * a.group + w.g0 + g) * D + 64 * c), "r"(w.q0 + i), "r"(mine)
+                : "memory");
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          const uint32_t some = __ballot_sync(0xffffffffu, !whole);
+          left &= some;
+          if (left == 0) return;
+        }
+        const uint32_t from = smem_u32(stage) + (lane >> 3) * 128;
+#pragma unroll 1
         for (int x = 0; x < 8; ++x) {
           const int row = 4 * x + (lane >> 3);
           uint4 u;
@@ -807,51 +823,61 @@ __global__ void __launch_bounds__(kThreads, 1)
                        : "memory");
           char* dst = reinterpret_cast<char*>(
               __shfl_sync(0xffffffffu, reinterpret_cast<uintptr_t>(base), row));
-          if (rows_in >> row & 1) *reinterpret_cast<uint4*>(dst + off + (lane & 7) * 16) = u;
+          if (left >> row & 1) *reinterpret_cast<uint4*>(dst + off + (lane & 7) * 16) = u;
         }
       };
+      const uint32_t keep = n > 0 ? 0xFFFFFFFFu : 0u;  // (else nothing was added up there)
       // (Compact code, each path in a loop of its own: it runs once an item, out of
-      // the instruction caches.  Unrolled, with the rare path below inlined for every
-      // value, it took 4500 to 6000 cycles.)
+      // the instruction caches.)
       if (w.alone) {
 #pragma unroll 1
         for (int c = 0; c < D / 64; ++c) {
+          uint32_t o[2][32];
+          tmem_ld_async<32>(o_col + 64 * c, o[0]);
+          tmem_ld_async<32>(o_col + 64 * c + 32, o[1]);
+          tmem_wait_ld();
           uint32_t p[32];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t o[32];
-            fetch(2 * c + h, o);
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int x = 0; x < 16; ++x) {
-              const float2 y = mul2(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]), r);
-              p[16 * h + x] = Pair<T>::pack(y.x, y.y);
+              asm volatile("" : "+r"(o[h][2 * x]), "+r"(o[h][2 * x + 1]));
+              const float2 y = mul2(__uint_as_float(o[h][2 * x]), __uint_as_float(o[h][2 * x + 1]), r);
+              p[16 * h + x] = Pair<T>::pack(y.x, y.y) & keep;
             }
+          if (n > 0 && c == D / 64 - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&free_o[s]);
           }
-          flush(p, 128 * c);
+          put(p, 128 * c, c, true);
         }
       } else {
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
           uint32_t o[32];
-          fetch(c, o);
+          tmem_ld32(o_col + 32 * c, o);
 #pragma unroll
           for (int x = 0; x < 16; ++x) {
+            asm volatile("" : "+r"(o[2 * x]), "+r"(o[2 * x + 1]));
             const float2 y = mul2(__uint_as_float(o[2 * x]), __uint_as_float(o[2 * x + 1]), r);
-            o[2 * x] = __float_as_uint(y.x);
-            o[2 * x + 1] = __float_as_uint(y.y);
+            o[2 * x] = __float_as_uint(y.x) & keep;
+            o[2 * x + 1] = __float_as_uint(y.y) & keep;
           }
-          flush(o, 128 * c);
+          if (n > 0 && c == D / 32 - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&free_o[s]);
+          }
+          put(o, 128 * c, c, false);
         }
         if (in) a.part_lse[zat] = total == 0.f ? -INFINITY : mx * a.scale_log2 + log2f(total);
-      }
-      if (n > 0) {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&free_o[s]);
       }
       if (odd[item & 1]) {  // infinite and NaN values that the row sees
         const uint32_t* notes = first + (item & 1) * D;
         const int seen_keys = lim - w.k0 - max(w.lim0 - w.k0, 0) / kKeys * kKeys;
+        asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // (the rows are stored)
+        asm volatile("fence.proxy.async;" ::: "memory");
         __syncwarp();
 #pragma unroll 1
         for (int d = 0; d < D && in; ++d) {
@@ -873,6 +899,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty_w[item & 1]);
     }
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   tc_fence_before();
   __syncthreads();
@@ -910,7 +937,9 @@ cudaError_t run_prompt(const AttnArgs& a, cudaStream_t stream) {
       encode(enc, &maps.k, type, a.k, static_cast<int64_t>(a.kv_heads) * D, a.slots, a.kv_stride,
              box) != CUDA_SUCCESS ||
       encode(enc, &maps.v, type, a.v, static_cast<int64_t>(a.kv_heads) * D, a.slots, a.kv_stride,
-             box) != CUDA_SUCCESS)
+             box) != CUDA_SUCCESS ||
+      encode(enc, &maps.out, type, a.out, static_cast<int64_t>(a.heads) * D, a.tokens,
+             static_cast<int64_t>(a.heads) * D, 8) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   auto kern = attn_prompt_kernel<T, D>;
   cudaError_t e = ensure_smem(kern, PromptSmem<D>::TOTAL);
