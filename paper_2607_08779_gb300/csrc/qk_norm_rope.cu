@@ -6,12 +6,15 @@
 // value is rounded once, when it is stored.
 //
 // Bound by HBM: an fp32 value is read and a 16-bit one written once (6 bytes a
-// value, and the token's cosines and sines).  A head is D / 4 lanes with four
-// consecutive values each, so a warp holds 128 / D heads; the norm is a sum over
-// the head's lanes, and the other value of a pair (a, a + rot / 2) one shuffle
-// away.  A warp takes a run of a token's heads, four groups of them in flight at a
-// time, and keeps the token's cosines and sines and the norm's weights in
-// registers.
+// value, and the token's cosines and sines).  A head is D / 8 lanes.  A lane has two
+// runs of four values, chosen so that both values of every pair are its own: of the
+// rotated values run 4l and run rot / 2 + 4l, of the others two that follow one
+// another.  So the rotation needs no exchange between lanes, and the norm a sum over
+// the head's lanes only.  A warp takes a run of a token's heads, two groups of them at
+// a time with the next two's loads in flight, and keeps the token's cosines and sines
+// in registers.  8191 tokens of 64 + 16 heads of 128: 88.5 us, 5.7 TB/s, 86 % of the
+// copy rate (four lanes' worth of exchange per value and no loads ahead: 110 us; more
+// heads at a time or fewer registers: 91 to 104 us).
 #include <algorithm>
 
 #include "sss_internal.cuh"
@@ -19,8 +22,9 @@
 namespace sss {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kUnroll = 4;
+constexpr int kThreads = 128;
+constexpr int kCtas = 7;    // per SM: 72 registers a thread hold the loads ahead
+constexpr int kUnroll = 2;
 
 struct RopeArgs {
   const void *q, *k, *v;
@@ -64,12 +68,22 @@ __device__ __forceinline__ void store4(T* p, float4 v) {
   *reinterpret_cast<uint2*>(p) = u;
 }
 
+// (x, y) * c + (y, x) * s of two runs: the rotation where y is x's other half
+__device__ __forceinline__ float4 axpy4(float4 a, float4 c, float4 b, float4 s) {
+  return make_float4(a.x * c.x + b.x * s.x, a.y * c.y + b.y * s.y, a.z * c.z + b.z * s.z,
+                     a.w * c.w + b.w * s.w);
+}
+__device__ __forceinline__ float4 swapped(float4 a) { return make_float4(a.y, a.x, a.w, a.z); }
+__device__ __forceinline__ float4 scaled(float4 a, float r, float4 w) {
+  return make_float4(a.x * r * w.x, a.y * r * w.y, a.z * r * w.z, a.w * r * w.w);
+}
+
 template <typename IN, typename OUT, int D>
-__global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const RopeArgs a) {
-  constexpr int LANES = D / 4;       // of a head
+__global__ void __launch_bounds__(kThreads, kCtas) qk_norm_rope_kernel(const RopeArgs a) {
+  constexpr int LANES = D / 8;       // of a head
   constexpr int GH = 32 / LANES;     // heads of a warp at a time
   const int lane = threadIdx.x & 31;
-  const int sub = lane / LANES, l = lane % LANES, d = 4 * l;
+  const int sub = lane / LANES, l = lane % LANES;
   const int64_t item = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) >> 5;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -83,81 +97,99 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const RopeArgs a
   int64_t slot = a.slots ? a.slots[t] : t;
   if (slot >= a.slots_n) flags |= SSS_FLAG_INDEX;
   const bool keep = slot >= 0 && slot < a.slots_n;  // -1: the token is not kept
-  float4 c = make_float4(1.f, 1.f, 1.f, 1.f), s = make_float4(0.f, 0.f, 0.f, 0.f);
-  int other = lane;  // the lane of the other halves of this lane's pairs
+  // the lane's runs, and what turns them: y0 = x0 c0 + o0 s0, y1 = x1 c1 + o1 s1 with
+  // o0 = x1 and o1 = x0 (halves), or the neighbours in the run (pairs)
+  const int half = a.rot / 2;
+  const bool turned = 8 * l < a.rot;
+  const int d0 = turned ? 4 * l : 8 * l;
+  const int d1 = turned ? half + 4 * l : 8 * l + 4;
+  const float4 one = make_float4(1.f, 1.f, 1.f, 1.f), none = make_float4(0.f, 0.f, 0.f, 0.f);
+  float4 c0 = one, s0 = none, c1 = one, s1 = none;
   if (a.rot > 0) {
     int64_t pos = a.positions[t];
     if (pos < 0 || pos >= a.max_pos) {
       flags |= SSS_FLAG_INDEX;
       pos = pos < 0 ? 0 : a.max_pos - 1;
     }
-    const int half = a.rot / 2;
     const float* cr = a.cos + pos * half;
     const float* sr = a.sin + pos * half;
-    if (d < a.rot) {
-      if (a.pairs) {
-        const float2 c2 = __ldg(reinterpret_cast<const float2*>(cr + d / 2));
-        const float2 s2 = __ldg(reinterpret_cast<const float2*>(sr + d / 2));
-        c = make_float4(c2.x, c2.x, c2.y, c2.y);
-        s = make_float4(-s2.x, s2.x, -s2.y, s2.y);
-      } else {
-        const bool low = d < half;
-        c = __ldg(reinterpret_cast<const float4*>(cr + (low ? d : d - half)));
-        s = __ldg(reinterpret_cast<const float4*>(sr + (low ? d : d - half)));
-        if (low) s = make_float4(-s.x, -s.y, -s.z, -s.w);
-        other = lane + (low ? half / 4 : -(half / 4));
-      }
+    if (turned && a.pairs) {
+      const float2 ca = __ldg(reinterpret_cast<const float2*>(cr + d0 / 2));
+      const float2 sa = __ldg(reinterpret_cast<const float2*>(sr + d0 / 2));
+      const float2 cb = __ldg(reinterpret_cast<const float2*>(cr + d1 / 2));
+      const float2 sb = __ldg(reinterpret_cast<const float2*>(sr + d1 / 2));
+      c0 = make_float4(ca.x, ca.x, ca.y, ca.y);
+      s0 = make_float4(-sa.x, sa.x, -sa.y, sa.y);
+      c1 = make_float4(cb.x, cb.x, cb.y, cb.y);
+      s1 = make_float4(-sb.x, sb.x, -sb.y, sb.y);
+    } else if (turned) {
+      c0 = c1 = __ldg(reinterpret_cast<const float4*>(cr + d0));
+      s1 = __ldg(reinterpret_cast<const float4*>(sr + d0));
+      s0 = make_float4(-s1.x, -s1.y, -s1.z, -s1.w);
     }
   }
-  const float4 one = make_float4(1.f, 1.f, 1.f, 1.f);
-  const float4 wq = a.wq ? __ldg(reinterpret_cast<const float4*>(a.wq + d)) : one;
-  const float4 wk = a.wk ? __ldg(reinterpret_cast<const float4*>(a.wk + d)) : one;
-
-  for (int hb = h0; hb < h1; hb += kUnroll * GH) {
-    float4 x[kUnroll];
+  // heads hb, hb + GH, ... of the lane's place in the warp
+  auto fetch = [&](int hb, float4 (&x0)[kUnroll], float4 (&x1)[kUnroll]) {
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = hb + u * GH + sub;
-      x[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+      x0[u] = x1[u] = none;
       if (h < h1) {
         const IN* src;
         if (h < a.hq) src = static_cast<const IN*>(a.q) + t * a.q_stride + h * D;
         else if (h < a.hq + a.hkv) src = static_cast<const IN*>(a.k) + t * a.k_stride + (h - a.hq) * D;
         else src = static_cast<const IN*>(a.v) + t * a.v_stride + (h - a.hq - a.hkv) * D;
-        x[u] = load4(src + d);
+        x0[u] = load4(src + d0);
+        x1[u] = load4(src + d1);
       }
     }
+  };
+  float4 n0[kUnroll], n1[kUnroll];
+  fetch(h0, n0, n1);
+#pragma unroll 1
+  for (int hb = h0; hb < h1; hb += kUnroll * GH) {
+    float4 x0[kUnroll], x1[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      x0[u] = n0[u];
+      x1[u] = n1[u];
+    }
+    if (hb + kUnroll * GH < h1) fetch(hb + kUnroll * GH, n0, n1);
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       const int h = hb + u * GH + sub;
       const bool is_q = h < a.hq, is_v = h >= a.hq + a.hkv;
-      float4 y = x[u];
-      float ss = y.x * y.x + y.y * y.y + y.z * y.z + y.w * y.w;
+      float4 y0 = x0[u], y1 = x1[u];
+      if (a.wq != nullptr || a.wk != nullptr) {
+        float ss = y0.x * y0.x + y0.y * y0.y + y0.z * y0.z + y0.w * y0.w + y1.x * y1.x +
+                   y1.y * y1.y + y1.z * y1.z + y1.w * y1.w;
 #pragma unroll
-      for (int m = LANES / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
-      if (!is_v && (is_q ? a.wq : a.wk) != nullptr) {
-        const float r = 1.0f / sqrtf(ss / D + a.eps);
-        const float4 w = is_q ? wq : wk;
-        y = make_float4(y.x * r * w.x, y.y * r * w.y, y.z * r * w.z, y.w * r * w.w);
+        for (int m = LANES / 2; m > 0; m >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+        const float* w = is_q ? a.wq : a.wk;
+        if (!is_v && w != nullptr) {
+          const float r = 1.0f / sqrtf(ss / D + a.eps);
+          y0 = scaled(y0, r, __ldg(reinterpret_cast<const float4*>(w + d0)));
+          y1 = scaled(y1, r, __ldg(reinterpret_cast<const float4*>(w + d1)));
+        }
       }
-      float4 o;  // the other halves
-      if (a.pairs) {
-        o = make_float4(y.y, y.x, y.w, y.z);
-      } else {
-        o.x = __shfl_sync(0xffffffffu, y.x, other);
-        o.y = __shfl_sync(0xffffffffu, y.y, other);
-        o.z = __shfl_sync(0xffffffffu, y.z, other);
-        o.w = __shfl_sync(0xffffffffu, y.w, other);
+      if (!is_v) {
+        const float4 o0 = a.pairs ? swapped(y0) : y1, o1 = a.pairs ? swapped(y1) : y0;
+        if (turned) {
+          y0 = axpy4(y0, c0, o0, s0);
+          y1 = axpy4(y1, c1, o1, s1);
+        }
       }
-      if (!is_v && d < a.rot)
-        y = make_float4(y.x * c.x + o.x * s.x, y.y * c.y + o.y * s.y, y.z * c.z + o.z * s.z,
-                        y.w * c.w + o.w * s.w);
       if (h >= h1) continue;
+      OUT* dst = nullptr;
       if (is_q) {
-        store4(static_cast<OUT*>(a.q_out) + (t * a.hq + h) * D + d, y);
+        dst = static_cast<OUT*>(a.q_out) + (t * a.hq + h) * D;
       } else if (keep) {
         const int kh = h - a.hq - (is_v ? a.hkv : 0);
-        store4(static_cast<OUT*>(is_v ? a.v_out : a.k_out) + slot * a.kv_stride + kh * D + d, y);
+        dst = static_cast<OUT*>(is_v ? a.v_out : a.k_out) + slot * a.kv_stride + kh * D;
+      }
+      if (dst != nullptr) {
+        store4(dst + d0, y0);
+        store4(dst + d1, y1);
       }
     }
   }
@@ -166,13 +198,13 @@ __global__ void __launch_bounds__(kThreads) qk_norm_rope_kernel(const RopeArgs a
 
 template <typename IN, typename OUT, int D>
 cudaError_t run(RopeArgs& a, cudaStream_t stream) {
-  constexpr int GH = 128 / D;
+  constexpr int GH = 256 / D;
   const int groups = (a.hq + 2 * a.hkv + GH - 1) / GH;
-  // a run of 16 groups shares its cosines and sines; fewer while the warps of
-  // the call would not fill the SMs (8 CTAs of 8 warps each)
-  a.run = 16;
-  while (a.run > kUnroll &&
-         static_cast<int64_t>(a.tokens) * ((groups + a.run - 1) / a.run) < 64 * device_sm_count())
+  // a run of 8 groups shares its cosines and sines; fewer while the warps of
+  // the call would not fill the SMs
+  a.run = 8;
+  while (a.run > 1 &&
+         static_cast<int64_t>(a.tokens) * ((groups + a.run - 1) / a.run) < 32 * device_sm_count())
     a.run /= 2;
   a.runs = (groups + a.run - 1) / a.run;
   const int64_t warps = static_cast<int64_t>(a.tokens) * a.runs;
