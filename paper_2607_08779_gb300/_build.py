@@ -1,4 +1,5 @@
-"""Build the CUDA library libsss.so in-tree with nvcc (sm_103a only).
+"""Build the CUDA library libsss.so in-tree with nvcc (sm_103a only), and with g++
+_binding.so, the compiled part of the Python binding.
 
 Each translation unit under csrc/ is compiled in parallel to an object file
 under _build/, then linked into paper_2607_08779_gb300/libsss.so.  The CUDA
@@ -18,6 +19,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libsss.so")
+BINDING_SRC = os.path.join(CSRC, "binding.cpp")
+BINDING = os.path.join(PKG, "_binding.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
@@ -37,16 +40,40 @@ def sources():
 
 def _deps():
     files = sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")]
+    files.append(BINDING_SRC)
     files.append(os.path.join(INCLUDE, "sss.h"))
     files.append(os.path.abspath(__file__))
     return files
 
 
 def up_to_date() -> bool:
-    if not os.path.exists(LIB):
+    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
         return False
-    t = os.path.getmtime(LIB)
+    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
     return all(os.path.getmtime(f) <= t for f in _deps())
+
+
+def build_binding() -> None:
+    """_binding.so, against the torch that this interpreter imports."""
+    import sysconfig
+
+    import torch
+
+    home = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
+    include = [INCLUDE, os.path.join(home, "include"),
+               os.path.join(home, "include", "torch", "csrc", "api", "include"), cuda,
+               sysconfig.get_paths()["include"]]
+    tmp = BINDING + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           *[x for d in include for x in ("-isystem", d)], BINDING_SRC, "-o", tmp,
+           "-L", os.path.join(home, "lib"), "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python",
+           f"-Wl,-rpath,{os.path.join(home, 'lib')}"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for {BINDING_SRC}:\n{r.stderr}")
+    os.replace(tmp, BINDING)
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
@@ -66,8 +93,10 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return obj
 
     srcs = sources()
-    with cf.ThreadPoolExecutor(max_workers=min(len(srcs), os.cpu_count() or 4)) as ex:
+    with cf.ThreadPoolExecutor(max_workers=min(len(srcs) + 1, os.cpu_count() or 4)) as ex:
+        binding = ex.submit(build_binding)
         objs = list(ex.map(compile_one, srcs))
+        binding.result()
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [cc, *ARCH, "-shared", "-Xcompiler", "-fPIC", "-o", tmp, *objs,
            "-cudart", "static"]

@@ -186,6 +186,32 @@ def load(build_if_needed: bool = True):
         return L
 
 
+_fast = None
+
+
+def _binding():
+    """The compiled part of the binding: it checks and makes the attention step's
+    calls that are in order."""
+    global _fast
+    if _fast is None:
+        import importlib.machinery
+        import importlib.util
+
+        import torch  # noqa: F401  (its libraries come first)
+
+        L = load()
+        with _lock:
+            if _fast is None:
+                loader = importlib.machinery.ExtensionFileLoader("_binding", _build.BINDING)
+                spec = importlib.util.spec_from_loader("_binding", loader)
+                m = importlib.util.module_from_spec(spec)
+                loader.exec_module(m)
+                m.init(*[ctypes.cast(f, ctypes.c_void_p).value
+                         for f in (L.sss_page_plan, L.sss_qk_norm_rope, L.sss_attention)])
+                _fast = m
+    return _fast
+
+
 def _ptr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
@@ -675,6 +701,7 @@ class KVCache:
         self._desc = KVCacheDesc(_ptr(k), _ptr(v), slots, strides[0], self.page_size, heads, dim,
                                  _dtype_code(k.dtype))
         self._ref = ctypes.byref(self._desc)
+        self._address = ctypes.addressof(self._desc)
 
 
 def empty_kv_cache(pages: int, page_size: int, heads: int, dim: int, dtype=None,
@@ -716,13 +743,9 @@ class Rope:
         self._desc = RopeDesc(_ptr(self.cos), _ptr(self.sin), _ptr(self.q_norm), _ptr(self.k_norm),
                               max_pos, 2 * half, self.style, self.eps)
         self._ref = ctypes.byref(self._desc)
-
-
-def _int32(t, numel) -> bool:
-    import torch
-
-    return (t is not None and t.dtype is torch.int32 and t.is_cuda and t.is_contiguous()
-            and t.numel() == numel)
+        self._address = ctypes.addressof(self._desc)
+        sizes = {w.numel() for w in (self.q_norm, self.k_norm) if w is not None}
+        self._weights = 0 if not sizes else sizes.pop() if len(sizes) == 1 else -1
 
 
 def _need_int32(fn, **tensors):
@@ -741,18 +764,19 @@ def sss_page_plan(past, fresh, page_size: int, free_pages, block_table, cu_q, kv
     kv_len [batch], positions and slots [tokens], used [1] and the table's new
     entries."""
     fn = "sss_page_plan"
+    if stream is None:
+        st = (_fast or _binding()).page_plan(past, fresh, page_size, free_pages, block_table, cu_q,
+                                             kv_len, positions, slots, used, dev_status)
+        if st >= 0:
+            return _check(fn, st)
     batch, tokens = past.numel(), positions.numel()
-    if not (_int32(past, batch) and _int32(fresh, batch) and _int32(free_pages, free_pages.numel())
-            and block_table.dim() == 2 and _int32(block_table, batch * block_table.shape[1])
-            and _int32(cu_q, batch + 1) and _int32(kv_len, batch) and _int32(positions, tokens)
-            and _int32(slots, tokens) and _int32(used, 1) and _plain_status(dev_status)):
-        if block_table.dim() != 2 or block_table.shape[0] != batch:
-            raise SssError(fn, 1, "block_table must be [batch, width]")
-        _need_int32(fn, past=(past, batch), fresh=(fresh, batch), free_pages=(free_pages, None),
-                    block_table=(block_table, None), cu_q=(cu_q, batch + 1), kv_len=(kv_len, batch),
-                    positions=(positions, tokens), slots=(slots, tokens), used=(used, 1))
-        _need_status(fn, dev_status)
-        _on_device(fn, dev_status=dev_status)
+    if block_table.dim() != 2 or block_table.shape[0] != batch:
+        raise SssError(fn, 1, "block_table must be [batch, width]")
+    _need_int32(fn, past=(past, batch), fresh=(fresh, batch), free_pages=(free_pages, None),
+                block_table=(block_table, None), cu_q=(cu_q, batch + 1), kv_len=(kv_len, batch),
+                positions=(positions, tokens), slots=(slots, tokens), used=(used, 1))
+    _need_status(fn, dev_status)
+    _on_device(fn, dev_status=dev_status)
     st = load().sss_page_plan(past.data_ptr(), fresh.data_ptr(), batch, page_size,
                               free_pages.data_ptr(), free_pages.numel(), block_table.data_ptr(),
                               block_table.shape[1], cu_q.data_ptr(), kv_len.data_ptr(),
@@ -780,9 +804,15 @@ def sss_qk_norm_rope(q, k, v, rope: Rope, positions, cache: KVCache, slots=None,
     """q [tokens, heads * dim], k and v [tokens, kv_heads * dim] (fp32 as the
     projections write them, or 16-bit; rows may be strided): heads normalised
     and rotated, q to q_out [tokens, heads, dim], k and v to the cache's slots."""
+    fn = "sss_qk_norm_rope"
+    if stream is None and q_out is not None:
+        st = (_fast or _binding()).qk_norm_rope(q, k, v, rope._address, rope._weights, positions,
+                                                cache._address, slots, q_out, dev_status)
+        if st >= 0:
+            _check(fn, st)
+            return q_out
     import torch
 
-    fn = "sss_qk_norm_rope"
     d = cache._desc
     tokens, dim = q.shape[0], d.dim
     width = q.numel() // tokens if tokens else q.shape[-1]
@@ -803,8 +833,7 @@ def sss_qk_norm_rope(q, k, v, rope: Rope, positions, cache: KVCache, slots=None,
         _need_int32(fn, slots=(slots, tokens))
     for name in ("q_norm", "k_norm"):
         _need(fn, name, getattr(rope, name), torch.float32, dim, optional=True)
-    if not _plain_status(dev_status):
-        _need_status(fn, dev_status)
+    _need_status(fn, dev_status)
     st = load().sss_qk_norm_rope(q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs, code, tokens,
                                  width // dim, rope._ref, _ptr(positions), q_out.data_ptr(),
                                  cache._ref, _ptr(slots), _ptr(dev_status), _stream(stream))
@@ -825,9 +854,18 @@ def sss_attention(q, cache: KVCache, cu_q, kv_len, max_q: int, max_kv: int, bloc
     tokens are rows cu_q[b] .. cu_q[b + 1] - 1 of q, the last of its kv_len[b]
     keys.  Without a block table its keys lie in slots cu_q[b] .. (kv_len may be
     None: its new tokens).  Returns out [tokens, heads, dim]."""
+    fn = "sss_attention"
+    if scale is None:
+        scale = cache._desc.dim ** -0.5
+    if stream is None and out is not None:
+        st = (_fast or _binding()).attention(q, cache._address, cu_q, kv_len, max_q, max_kv,
+                                             block_table, scale, out, workspace, dev_status)
+        # (a workspace that was not given is allocated below)
+        if st >= 0 and not (st == 5 and workspace is None):
+            _check(fn, st)
+            return out
     import torch
 
-    fn = "sss_attention"
     d = cache._desc
     if q.dim() != 3 or q.shape[2] != d.dim:
         raise SssError(fn, 1, "q must be [tokens, heads, dim] of the cache's dim")
@@ -838,27 +876,19 @@ def sss_attention(q, cache: KVCache, cu_q, kv_len, max_q: int, max_kv: int, bloc
     qs = _rows(fn, "q", q, tokens, heads * dim)
     if out is None:
         out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
-    if scale is None:
-        scale = dim ** -0.5
-    if not (_int32(cu_q, batch + 1) and _plain(out, q.dtype, tokens * heads * dim) and q.is_cuda
-            and _plain_workspace(workspace) and _plain_status(dev_status)
-            and (kv_len is None or _int32(kv_len, batch))
-            and (block_table is None
-                 or block_table.dim() == 2 and block_table.shape[0] == batch
-                 and _int32(block_table, block_table.numel()))):
-        _need_int32(fn, cu_q=(cu_q, None))
-        if batch < 0:
-            raise SssError(fn, 1, "cu_q must be [batch + 1]")
-        if kv_len is not None:
-            _need_int32(fn, kv_len=(kv_len, batch))
-        if block_table is not None:
-            if block_table.dim() != 2 or block_table.shape[0] != batch:
-                raise SssError(fn, 1, "block_table must be [batch, width]")
-            _need_int32(fn, block_table=(block_table, None))
-        _need(fn, "out", out, q.dtype, tokens * heads * dim)
-        _need(fn, "workspace", workspace, torch.uint8, optional=True)
-        _need_status(fn, dev_status)
-        _on_device(fn, q=q, out=out, workspace=workspace, dev_status=dev_status)
+    _need_int32(fn, cu_q=(cu_q, None))
+    if batch < 0:
+        raise SssError(fn, 1, "cu_q must be [batch + 1]")
+    if kv_len is not None:
+        _need_int32(fn, kv_len=(kv_len, batch))
+    if block_table is not None:
+        if block_table.dim() != 2 or block_table.shape[0] != batch:
+            raise SssError(fn, 1, "block_table must be [batch, width]")
+        _need_int32(fn, block_table=(block_table, None))
+    _need(fn, "out", out, q.dtype, tokens * heads * dim)
+    _need(fn, "workspace", workspace, torch.uint8, optional=True)
+    _need_status(fn, dev_status)
+    _on_device(fn, q=q, out=out, workspace=workspace, dev_status=dev_status)
     if workspace is None:
         need = sss_attention_workspace_bytes(tokens, heads, cache, batch, max_q, max_kv)
         if need > 0:
