@@ -14,7 +14,6 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
   // the row form while a request's tokens and heads are one tile of it (and without
   // a cache to make a tensor map of)
   p.prompt = static_cast<int64_t>(group) * max_q > 32 && max_q > 1 && c.slots > 0;
-  int64_t splits, step;
   if (p.prompt) {
     // two row tiles of 128 rows: `tt` tokens (a multiple of 8, as its box in swizzled
     // shared memory needs) of up to 16 heads each
@@ -22,30 +21,40 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
     p.tpt = 2 * (128 / p.hpt / 8 * 8);
   } else {
     // 16 rows while they hold a request's tokens and heads
-    p.row_tiles16 = static_cast<int64_t>(group) * max_q <= 16 ? 1 : 2;
-    p.hpt = std::min(group, 16 * p.row_tiles16);
-    p.tpt = std::min(16 * p.row_tiles16 / p.hpt, max_q);
+    p.rows = static_cast<int64_t>(group) * max_q <= 16 ? 16 : 32;
+    p.hpt = std::min(group, p.rows);
+    p.tpt = std::min(p.rows / p.hpt, max_q);
   }
   p.hchunks = (group + p.hpt - 1) / p.hpt;
   p.one_tile = max_q <= p.tpt;
   p.tiles = p.one_tile ? batch : std::min(tokens / p.tpt + batch,
                                           static_cast<int64_t>(batch) * ((max_q + p.tpt - 1) / p.tpt));
-  const int64_t items = std::max<int64_t>(1, p.tiles * c.heads * p.hchunks);
+  const int64_t per_tile = static_cast<int64_t>(c.heads) * p.hchunks;
+  const int64_t items = std::max<int64_t>(1, p.tiles * per_tile);
   if (p.prompt) {
-    step = 128;
-    splits = std::min(sms / items, (max_kv + 511) / 512);
-  } else {
-    step = 64;
-    splits = std::min(4 * sms / items, (max_kv + 255) / 256);
+    const int64_t splits = std::max<int64_t>(1, std::min(sms / items, (max_kv + 511) / 512));
+    p.chunk = std::max<int64_t>(128, ((max_kv + splits - 1) / splits + 127) / 128 * 128);
+    p.nsplit = std::max<int64_t>(1, (max_kv + p.chunk - 1) / p.chunk);
+    p.join = p.nsplit > 1;
+    if (p.join) {
+      const size_t rows = static_cast<size_t>(p.nsplit) * tokens * heads;
+      p.lse_at = rows * c.dim * 4;
+      p.ws_bytes = p.lse_at + rows * 4;
+    }
+    return p;
   }
-  splits = std::max<int64_t>(1, splits);
-  p.chunk = std::max<int64_t>(step, ((max_kv + splits - 1) / splits + step - 1) / step * step);
-  p.nsplit = std::max<int64_t>(1, (max_kv + p.chunk - 1) / p.chunk);
-  if (p.nsplit > 1) {
-    const size_t rowsz = static_cast<size_t>(tokens) * heads;
-    p.part_bytes = (p.nsplit * rowsz * c.dim * 4 + 255) / 256 * 256;
-    p.ws_bytes = p.part_bytes + p.nsplit * rowsz * 4;
-  }
+  // Few rows: a cluster of as many CTAs as run at a time (two an SM, and whole
+  // clusters in a cluster of SMs: 8 of 16 CTAs, 32 of 8), of 128 keys each at least.  A
+  // second wave costs more than it evens out (32 requests of 512 keys: 14.2 us whole,
+  // 19.3 in pairs; 8 of 125 to 1000: 8.4 us in fours, 16.2 in eights), but where keys
+  // are many (16 requests of 130 to 16384: 89 us in pairs, 59 in fours; 64 of 12000 to
+  // 16384: 534 us whole, 516 in fours).
+  constexpr int64_t kLeast = 128, kMany = 4096;
+  const int64_t fit = items <= 8 ? 16 : items <= 32 ? 8 : items <= 2 * sms / 4 ? 4 : items <= sms ? 2 : 1;
+  int64_t cluster = max_kv >= kMany ? std::max<int64_t>(fit, 4) : fit;
+  while (cluster > 1 && cluster * kLeast > max_kv) cluster /= 2;
+  p.nsplit = cluster;
+  p.chunk = kLeast;
   return p;
 }
 
@@ -66,7 +75,7 @@ cudaError_t launch_attention(const AttnPlan& p, const void* q, int64_t q_stride,
   a.slots = c.slots;
   a.kv_stride = c.stride;
   a.part = static_cast<float*>(workspace);
-  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes);
+  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.lse_at);
   a.status = status;
   a.batch = batch;
   a.tokens = static_cast<int>(tokens);
@@ -77,6 +86,7 @@ cudaError_t launch_attention(const AttnPlan& p, const void* q, int64_t q_stride,
   a.group = heads / c.heads;
   a.hpt = p.hpt;
   a.hchunks = p.hchunks;
+  a.hpt_inverse = 65536 / p.hpt + 1;
   a.tpt = p.tpt;
   a.tiles = static_cast<int>(p.tiles);
   a.one_tile = p.one_tile ? 1 : 0;
@@ -84,11 +94,12 @@ cudaError_t launch_attention(const AttnPlan& p, const void* q, int64_t q_stride,
   while (table && (1 << a.page_shift) < c.page_size) ++a.page_shift;
   a.chunk = static_cast<int>(p.chunk);
   a.nsplit = static_cast<int>(p.nsplit);
+  a.rows = p.rows;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.stall = (test_stall_mask() & SSS_TEST_STALL_ATTENTION) ? 1 : 0;
   cudaError_t e = p.prompt ? launch_attn_prompt(a, c.dtype, c.dim, stream)
-                           : launch_attn_rows(a, c.dtype, c.dim, p.row_tiles16, stream);
-  if (e == cudaSuccess && p.nsplit > 1) e = launch_attn_join(a, c.dtype, c.dim, stream);
+                           : launch_attn_rows(a, c.dtype, c.dim, stream);
+  if (e == cudaSuccess && p.join) e = launch_attn_join(a, c.dtype, c.dim, stream);
   return e;
 }
 

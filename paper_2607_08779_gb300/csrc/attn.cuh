@@ -8,9 +8,10 @@
 // of one key/value head (a group of more heads than a tile takes goes in
 // `hchunks` tiles).
 //
-// Keys.  A tile's keys are cut into splits of `chunk`.  A tile of more than one
-// leaves each split's normalised fp32 rows and log2 of their sums in the
-// workspace, and attn_join_kernel adds them.
+// Keys.  A tile's keys may be cut into splits.  With few rows they are the CTAs of a
+// cluster of nsplit, which join there (`chunk` is then the least length of a split); with
+// many rows each split of `chunk` keys leaves its normalised fp32 rows and the log2 of
+// their sums in the workspace, and attn_join_kernel adds them.
 #pragma once
 
 #include "sss_internal.cuh"
@@ -29,10 +30,12 @@ struct AttnArgs {
   int batch, tokens, max_q, max_kv;
   int heads, kv_heads, group;
   int hpt, hchunks, tpt;
+  int hpt_inverse;  // row * hpt_inverse >> 16 = row / hpt for rows < 32
   int tiles;        // an upper bound of the launch's token tiles
   int one_tile;     // max_q <= tpt: tile b is request b's only one
   int table_width, page_shift;
   int chunk, nsplit;
+  int rows;         // of the row form's tiles: 16 or 32
   int stall;        // test hook
   float scale_log2;  // scale * log2(e)
 };
@@ -168,8 +171,7 @@ __device__ __forceinline__ float ex2(float x) {
 }
 
 // The forms of the attention.
-cudaError_t launch_attn_rows(const AttnArgs& a, int dtype, int dim, int row_tiles16,
-                             cudaStream_t stream);
+cudaError_t launch_attn_rows(const AttnArgs& a, int dtype, int dim, cudaStream_t stream);
 cudaError_t launch_attn_prompt(const AttnArgs& a, int dtype, int dim, cudaStream_t stream);
 cudaError_t launch_attn_join(const AttnArgs& a, int dtype, int dim, cudaStream_t stream);
 

@@ -27,11 +27,13 @@ constexpr int kStep = 16;   // keys of a warp's step
 constexpr int kStages = 3;  // steps in a warp's ring
 constexpr float kRaise = 8.0f;
 
-template <int D>
+template <int D, int R, bool CL>
 struct RowsSmem {
   static constexpr int TILE = kStep * D * 2;             // 16 keys (or values)
   static constexpr int RING = kStages * 2 * TILE;        // of a warp
-  static constexpr int TOTAL = kWarps * RING;
+  static constexpr int RINGS = kWarps * RING;
+  // the splits' pieces of the values that this one joins (their number rounded up)
+  static constexpr int TOTAL = RINGS + (CL ? (R * D / 4 + 16) * 16 : 0);
 };
 
 __device__ __forceinline__ uint32_t smem_addr(const void* p) {
@@ -71,58 +73,76 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// MT tiles of 16 rows
-template <typename T, int D, int MT>
+// Stores into the shared memory of another CTA of the cluster, at the address that
+// addr is in this one's.
+__device__ __forceinline__ uint32_t of_peer(uint32_t addr, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void peer_store(uint32_t addr, float v) {
+  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void peer_store(uint32_t addr, float4 v) {
+  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y),
+               "f"(v.z), "f"(v.w)
+               : "memory");
+}
+
+// MT tiles of 16 rows.  CL: the splits of a tile's keys are the CTAs of a cluster, of
+// equal length whatever the request's, and join through its shared memory: each adds up
+// a share of the values (16 bytes at a time), and the others store their partial results
+// there.
+template <typename T, int D, int MT, bool CL>
 __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_constant__ AttnArgs a) {
-  using S = RowsSmem<D>;
   constexpr int R = 16 * MT;
+  using S = RowsSmem<D, R, CL>;
   constexpr int CH = D / 8;       // 16-byte pieces of a row
   constexpr int KD = D / 16;      // mma steps along d
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float wmax[kWarps][R], wsum[kWarps][R];
+  __shared__ float split_lse[CL ? 16 : 1][R];  // of every split
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // another CTA's shared memory exists only once that CTA has started: waited for
+  // before the first store into a peer
+  if constexpr (CL) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
-  // this CTA's work
-  const int z = blockIdx.x % a.nsplit;
-  const int hx = (blockIdx.x / a.nsplit) % (a.kv_heads * a.hchunks);
-  const int tile = blockIdx.x / (a.nsplit * a.kv_heads * a.hchunks);
-  const int kh = hx / a.hchunks, g0 = hx % a.hchunks * a.hpt;
+  // this CTA's work; the heads of a tile are neighbours in the grid's order, as their
+  // keys are in memory (heads outermost: 61 -> 70 us for 16 requests of 130 to 16384 keys)
+  const int z = blockIdx.x, hx = blockIdx.y;
+  const int kh = a.hchunks == 1 ? hx : hx / a.hchunks;
+  const int g0 = (hx - kh * a.hchunks) * a.hpt;
   const int nh = min(a.hpt, a.group - g0);  // heads of the tile
+  // (the tokens of rows < 32, without a division)
+  const auto token_of = [&](int row) { return row * a.hpt_inverse >> 16; };
+  const auto leave = [&]() {
+    if constexpr (CL) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  };
   int b, i0;
   uint32_t flags = 0;
   AttnRequest rq;
-  if (!attn_tile(a, tile, b, i0, rq, flags)) return;
+  if (!attn_tile(a, blockIdx.z, b, i0, rq, flags)) return leave();
   const int nt = min(a.tpt, rq.n - i0);  // tokens of the tile
   if (nt <= 0) {
     if (flags && a.status && threadIdx.x == 0) atomicOr(a.status, flags);
-    return;
+    return leave();
   }
-  const int lim0 = attn_limit(rq, i0), lim1 = attn_limit(rq, i0 + nt - 1);
-  const int k0 = z * a.chunk, k1 = min(lim1, k0 + a.chunk);
-  if (k0 >= k1 && z > 0) return;
+  const int lim1 = attn_limit(rq, i0 + nt - 1);
+  int k0 = 0, k1 = lim1, chunk = 0;
+  bool alone = true;  // the tile has no other split
+  if constexpr (CL) {
+    constexpr int kAll = kWarps * kStep;
+    chunk = max(a.chunk,
+                ((lim1 + a.nsplit - 1 >> (31 - __clz(a.nsplit))) + kAll - 1) / kAll * kAll);
+    k0 = min(z * chunk, lim1);
+    k1 = min(lim1, k0 + chunk);
+    alone = lim1 <= chunk;
+    if (k0 >= k1 && z > 0 && alone) return leave();
+  }
+  const int lim0 = attn_limit(rq, i0);
   const int steps = (max(k1 - k0, 0) + kStep - 1) / kStep;
-
-  // the rows' queries as mma operands, and how many keys each row sees
-  uint32_t qf[MT][KD][4];
-  int lim[MT][2];
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int row = 16 * m + 8 * e + (lane >> 2);
-      const int i = row / a.hpt, g = row - i * a.hpt;
-      const bool in = i < nt && g < nh;
-      lim[m][e] = in ? attn_limit(rq, i0 + i) : 0;
-      const T* src = static_cast<const T*>(a.q) + (rq.q0 + i0 + (in ? i : 0)) * a.q_stride +
-                     (kh * a.group + g0 + (in ? g : 0)) * D + 2 * (lane & 3);
-#pragma unroll
-      for (int kk = 0; kk < KD; ++kk) {
-        qf[m][kk][e] = in ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * kk)) : 0u;
-        qf[m][kk][2 + e] = in ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * kk + 8)) : 0u;
-      }
-    }
 
   // The warp's steps: warp, warp + 4, ... of the split's.  Lane l keeps the table
   // entry of the warp's step 32 n + l.
@@ -159,23 +179,45 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
+  for (int s = 0; s < kStages - 1; ++s) issue(s);
 
+  // the rows' queries as mma operands, and how many keys each row sees
+  uint32_t qf[MT][KD][4];
+  int lim[MT][2];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int row = 16 * m + 8 * e + (lane >> 2);
+      const int i = token_of(row), g = row - i * a.hpt;
+      const bool in = i < nt && g < nh;
+      lim[m][e] = in ? attn_limit(rq, i0 + i) : 0;
+      const T* src = static_cast<const T*>(a.q) + (rq.q0 + i0 + (in ? i : 0)) * a.q_stride +
+                     (kh * a.group + g0 + (in ? g : 0)) * D + 2 * (lane & 3);
+#pragma unroll
+      for (int kk = 0; kk < KD; ++kk) {
+        qf[m][kk][e] = in ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * kk)) : 0u;
+        qf[m][kk][2 + e] = in ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * kk + 8)) : 0u;
+      }
+    }
+
+  // The sums are those of the rounded p, by one more product with ones: what
+  // rounding takes off all of a row's p alike then cancels.
+  constexpr uint32_t kOnes = std::is_same<T, __half>::value ? 0x3C003C00u : 0x3F803F80u;
   float o[MT][D / 8][4];
-  float mx[MT][2], sum[MT][2];
+  float mx[MT][2], sum[MT][4];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      mx[m][e] = -INFINITY;
-      sum[m][e] = 0.f;
-    }
+    for (int e = 0; e < 2; ++e) mx[m][e] = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[m][i] = 0.f;
 #pragma unroll
     for (int n = 0; n < D / 8; ++n)
 #pragma unroll
       for (int i = 0; i < 4; ++i) o[m][n][i] = 0.f;
   }
 
-  for (int s = 0; s < kStages - 1; ++s) issue(s);
   for (int s = 0; s < mine; ++s) {
     issue(s + kStages - 1);
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
@@ -183,14 +225,14 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     const uint32_t kt = ring_addr + (s % kStages) * 2 * S::TILE, vt = kt + S::TILE;
     const int key0 = k0 + kStep * (warp + kWarps * s);
 
-    // scores: two tiles of 8 keys
-    float sc[MT][2][4];
+    // scores: two tiles of 8 keys, each in two sums (shorter chains of products)
+    float sc[MT][2][4], odd_sc[MT][2][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int n = 0; n < 2; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[m][n][i] = 0.f;
+        for (int i = 0; i < 4; ++i) sc[m][n][i] = odd_sc[m][n][i] = 0.f;
 #pragma unroll
     for (int kk = 0; kk < KD; ++kk) {
       const int row = (lane & 7) + ((lane >> 4) << 3), c = 2 * kk + ((lane >> 3) & 1);
@@ -198,8 +240,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
       ldsm4(kf, kt + row * (D * 2) + ((c ^ (row & 7)) * 16));
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        mma16816<T>(sc[m][0], qf[m][kk], kf[0], kf[1]);
-        mma16816<T>(sc[m][1], qf[m][kk], kf[2], kf[3]);
+        mma16816<T>(kk & 1 ? odd_sc[m][0] : sc[m][0], qf[m][kk], kf[0], kf[1]);
+        mma16816<T>(kk & 1 ? odd_sc[m][1] : sc[m][1], qf[m][kk], kf[2], kf[3]);
       }
     }
     // scale, mask, and raise the maxima where a score passes them by much
@@ -211,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
       for (int n = 0; n < 2; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          float x = sc[m][n][i] * a.scale_log2;
+          float x = (sc[m][n][i] + odd_sc[m][n][i]) * a.scale_log2;
           if (cut && key0 + 8 * n + 2 * (lane & 3) + (i & 1) >= lim[m][i >> 1]) x = -INFINITY;
           sc[m][n][i] = x;
           raise = raise || x > mx[m][i >> 1] + kRaise;
@@ -228,7 +270,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
           t = fmaxf(t, mx[m][e]);
           const float f = t == -INFINITY ? 1.f : ex2(mx[m][e] - t);
           mx[m][e] = t;
-          sum[m][e] *= f;
+          sum[m][2 * e] *= f;
+          sum[m][2 * e + 1] *= f;
 #pragma unroll
           for (int n = 0; n < D / 8; ++n) {
             o[m][n][2 * e] *= f;
@@ -246,12 +289,12 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
           const float ref = mx[m][i >> 1];
           const float p = ex2(sc[m][n][i] - (ref == -INFINITY ? 0.f : ref));
           sc[m][n][i] = p;
-          sum[m][i >> 1] += p;
         }
       pf[m][0] = Pair<T>::pack(sc[m][0][0], sc[m][0][1]);
       pf[m][1] = Pair<T>::pack(sc[m][0][2], sc[m][0][3]);
       pf[m][2] = Pair<T>::pack(sc[m][1][0], sc[m][1][1]);
       pf[m][3] = Pair<T>::pack(sc[m][1][2], sc[m][1][3]);
+      mma16816<T>(sum[m], pf[m], kOnes, kOnes);
     }
     // A value that is infinite or NaN reaches the rows that see its key and no
     // other: 0 x NaN would reach all.  Where a step's keys are not seen by every
@@ -326,20 +369,19 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
 
   // join the warps
   constexpr int LD = D + 4;  // (rows' lanes in distinct banks)
-  static_assert(kWarps * R * LD * 4 <= S::TOTAL, "the partial outputs reuse the rings");
+  static_assert(kWarps * R * LD * 4 <= S::RINGS, "the partial outputs reuse the rings");
   float* part = reinterpret_cast<float*>(smem);
+  const int rows = nt * a.hpt;  // (with those of heads that a last group of heads lacks)
   __syncthreads();
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      if (16 * m + 8 * e >= rows) continue;
       const int row = 16 * m + 8 * e + (lane >> 2);
-      float t = sum[m][e];
-      t += __shfl_xor_sync(0xffffffffu, t, 1);
-      t += __shfl_xor_sync(0xffffffffu, t, 2);
       if ((lane & 3) == 0) {
         wmax[warp][row] = mx[m][e];
-        wsum[warp][row] = t;
+        wsum[warp][row] = sum[m][2 * e];
       }
       float* dst = part + (warp * R + row) * LD + 2 * (lane & 3);
 #pragma unroll
@@ -347,11 +389,14 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
         *reinterpret_cast<float2*>(dst + 8 * n) = make_float2(o[m][n][2 * e], o[m][n][2 * e + 1]);
     }
   __syncthreads();
-  const bool alone = lim1 <= a.chunk;  // the tile has no other split
-  for (int x = threadIdx.x; x < R * (D / 4); x += kThreads) {
-    const int row = x / (D / 4), d = 4 * (x % (D / 4));
-    const int i = row / a.hpt, g = row - i * a.hpt;
-    if (i >= nt || g >= nh) continue;
+  const int n = CL ? (lim1 + chunk - 1) / chunk : 1;  // splits with keys
+  // pieces of 16 bytes; with CL those of a split follow one another in `gather`
+  constexpr int PIECES = D / 4;
+  const uint32_t gather = smem_addr(smem + S::RINGS), lse0 = smem_addr(&split_lse[0][0]);
+  if (CL && !alone) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  for (int x = threadIdx.x; x < rows * PIECES; x += kThreads) {
+    const int row = x / PIECES, d = 4 * (x % PIECES);
+    const int i = token_of(row), g = row - i * a.hpt;
     float top = -INFINITY;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) top = fmaxf(top, wmax[w][row]);
@@ -371,29 +416,67 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     }
     const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
     acc = make_float4(acc.x * r, acc.y * r, acc.z * r, acc.w * r);
-    const int64_t at =
-        static_cast<int64_t>(rq.q0 + i0 + i) * a.heads + kh * a.group + g0 + g;
+    const float lse = total == 0.f ? -INFINITY : top + log2f(total);
+    const int64_t at = static_cast<int64_t>(rq.q0 + i0 + i) * a.heads + kh * a.group + g0 + g;
     if (alone) {
       const uint2 u = make_uint2(Pair<T>::pack(acc.x, acc.y), Pair<T>::pack(acc.z, acc.w));
+      if (g < nh) *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
+    } else if constexpr (CL) {
+      if (z < n) {
+        const int per = (rows * PIECES + n - 1) / n, to = x / per;
+        peer_store(of_peer(gather + (z * per + x - to * per) * 16, to), acc);
+        // (the row's pieces belong to a few of the splits: each gets its sum)
+        if (d == 0 || x == to * per) peer_store(of_peer(lse0 + (z * R + row) * 4, to), lse);
+      }
+    }
+  }
+  if constexpr (CL) {
+    if (alone) return leave();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    const int per = (rows * PIECES + n - 1) / n;
+    if (z >= n) return;
+    // a lane per split and piece (a cluster is a power of two)
+    const int cl = a.nsplit, w = threadIdx.x & (cl - 1);
+    for (int y0 = 0; y0 < per; y0 += kThreads / cl) {
+      const int y = y0 + threadIdx.x / cl, x = z * per + y, row = x / PIECES, d = 4 * (x % PIECES);
+      const int i = token_of(row), g = row - i * a.hpt;
+      const bool in = y < per && row < rows;
+      const float l = in && w < n ? split_lse[w][row] : -INFINITY;
+      float top = l;
+      for (int m = cl / 2; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+      float total = l == -INFINITY ? 0.f : ex2(l - top);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (total != 0.f) {
+        v = *reinterpret_cast<const float4*>(smem + S::RINGS + (w * per + y) * 16);
+        v = make_float4(v.x * total, v.y * total, v.z * total, v.w * total);
+      }
+      for (int m = cl / 2; m > 0; m >>= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, m);
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, m);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, m);
+        v.z += __shfl_xor_sync(0xffffffffu, v.z, m);
+        v.w += __shfl_xor_sync(0xffffffffu, v.w, m);
+      }
+      if (!in || w != 0 || g >= nh) continue;
+      const float r = total == 0.f ? 0.f : 1.f / total;
+      const int64_t at = static_cast<int64_t>(rq.q0 + i0 + i) * a.heads + kh * a.group + g0 + g;
+      const uint2 u = make_uint2(Pair<T>::pack(v.x * r, v.y * r), Pair<T>::pack(v.z * r, v.w * r));
       *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
-    } else {
-      const int64_t zat = static_cast<int64_t>(z) * a.tokens * a.heads + at;
-      *reinterpret_cast<float4*>(a.part + zat * D + d) = acc;
-      if (d == 0) a.part_lse[zat] = total == 0.f ? -INFINITY : top + log2f(total);
     }
   }
 }
 
 // The rows whose tile has more than one split: the splits' outputs, weighted by
-// 2^lse, in split order.  A warp per row.
+// 2^lse, in split order.  A CTA per row; its warps take every fourth split.
 template <typename T, int D>
 __global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ AttnArgs a) {
+  __shared__ float4 sums[4][D / 4];
+  __shared__ float totals[4];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int lane = threadIdx.x & 31;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 5);
-  const int64_t rows = static_cast<int64_t>(a.tokens) * a.heads;
-  if (row >= rows) return;
+  const int64_t row = blockIdx.x, rows = static_cast<int64_t>(a.tokens) * a.heads;
   const int t = static_cast<int>(row / a.heads);
   // the token's request: the last whose first token is not behind it
   int lo = 0, hi = a.batch;
@@ -415,68 +498,95 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ 
 #pragma unroll
   for (int m = 16; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
   const float ref = top == -INFINITY ? 0.f : top;
-  constexpr int PER = D / 32;
-  float acc[PER], total = 0.f;
-#pragma unroll
-  for (int j = 0; j < PER; ++j) acc[j] = 0.f;
-  for (int z = 0; z < n; ++z) {
+  constexpr int LANES = D / 4;  // that hold the row
+  float total = 0.f;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int z = warp; z < n; z += 4) {
     const float lse = a.part_lse[z * rows + row];
-    if (lse == -INFINITY) continue;
+    const float4 v = lane < LANES ? reinterpret_cast<const float4*>(a.part + (z * rows + row) * D)[lane]
+                                  : make_float4(0.f, 0.f, 0.f, 0.f);
     const float f = ex2(lse - ref);
+    if (lse == -INFINITY) continue;
     total += f;
-    const float* src = a.part + (z * rows + row) * D + lane * PER;
+    acc.x += f * v.x;
+    acc.y += f * v.y;
+    acc.z += f * v.z;
+    acc.w += f * v.w;
+  }
+  if (lane < LANES) sums[warp][lane] = acc;
+  if (lane == 0) totals[warp] = total;
+  __syncthreads();
+  if (warp != 0 || lane >= LANES) return;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) acc[j] += f * src[j];
+  for (int w = 1; w < 4; ++w) {
+    const float4 v = sums[w][lane];
+    total += totals[w];
+    acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
   }
   const float r = total == 0.f ? 0.f : 1.f / total;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<T*>(a.out) + row * D + lane * PER);
-#pragma unroll
-  for (int j = 0; j < PER; j += 2) dst[j / 2] = Pair<T>::pack(acc[j] * r, acc[j + 1] * r);
+  reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * D)[lane] =
+      make_uint2(Pair<T>::pack(acc.x * r, acc.y * r), Pair<T>::pack(acc.z * r, acc.w * r));
 }
 
 template <typename K>
-cudaError_t launch(K kern, const AttnArgs& a, int64_t blocks, int threads, int smem,
-                   cudaStream_t stream) {
-  if (blocks > INT32_MAX) return cudaErrorNotSupported;
+cudaError_t launch(K kern, const AttnArgs& a, dim3 grid, int threads, int smem,
+                   cudaStream_t stream, int cluster = 1) {
+  if (grid.y > 65535 || grid.z > 65535) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
-template <typename T, int D, int MT>
+template <typename T, int D, int MT, bool CL>
 cudaError_t run_rows(const AttnArgs& a, cudaStream_t stream) {
-  auto kern = attn_rows_kernel<T, D, MT>;
-  cudaError_t e = ensure_smem(kern, RowsSmem<D>::TOTAL);
+  auto kern = attn_rows_kernel<T, D, MT, CL>;
+  constexpr int smem = RowsSmem<D, 16 * MT, CL>::TOTAL;
+  cudaError_t e = ensure_smem(kern, smem);
   if (e != cudaSuccess) return e;
-  const int64_t blocks = static_cast<int64_t>(a.tiles) * a.kv_heads * a.hchunks * a.nsplit;
-  return launch(kern, a, blocks, kThreads, RowsSmem<D>::TOTAL, stream);
+  if (CL && a.nsplit > 8) {
+    e = ensure_large_cluster(kern);
+    if (e != cudaSuccess) return e;
+  }
+  return launch(kern, a, dim3(a.nsplit, a.kv_heads * a.hchunks, a.tiles), kThreads, smem, stream,
+                a.nsplit);
+}
+template <typename T, int D, int MT>
+cudaError_t rows_mode(const AttnArgs& a, cudaStream_t stream) {
+  return a.nsplit > 1 ? run_rows<T, D, MT, true>(a, stream) : run_rows<T, D, MT, false>(a, stream);
 }
 template <typename T>
-cudaError_t rows_dim(const AttnArgs& a, int dim, int mt, cudaStream_t stream) {
-  if (dim == 64) return mt == 1 ? run_rows<T, 64, 1>(a, stream) : run_rows<T, 64, 2>(a, stream);
-  return mt == 1 ? run_rows<T, 128, 1>(a, stream) : run_rows<T, 128, 2>(a, stream);
+cudaError_t rows_dim(const AttnArgs& a, int dim, cudaStream_t stream) {
+  if (dim == 64)
+    return a.rows == 16 ? rows_mode<T, 64, 1>(a, stream) : rows_mode<T, 64, 2>(a, stream);
+  return a.rows == 16 ? rows_mode<T, 128, 1>(a, stream) : rows_mode<T, 128, 2>(a, stream);
 }
 template <typename T>
 cudaError_t join_dim(const AttnArgs& a, int dim, cudaStream_t stream) {
-  const int64_t blocks = (static_cast<int64_t>(a.tokens) * a.heads + 3) / 4;
-  return dim == 64 ? launch(attn_join_kernel<T, 64>, a, blocks, 128, 0, stream)
-                   : launch(attn_join_kernel<T, 128>, a, blocks, 128, 0, stream);
+  const int64_t blocks = static_cast<int64_t>(a.tokens) * a.heads;
+  if (blocks > INT32_MAX) return cudaErrorNotSupported;
+  const dim3 grid(static_cast<unsigned>(blocks));
+  return dim == 64 ? launch(attn_join_kernel<T, 64>, a, grid, 128, 0, stream)
+                   : launch(attn_join_kernel<T, 128>, a, grid, 128, 0, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_attn_rows(const AttnArgs& a, int dtype, int dim, int row_tiles16,
-                             cudaStream_t stream) {
-  return dtype == SSS_OUT_F16 ? rows_dim<__half>(a, dim, row_tiles16, stream)
-                              : rows_dim<__nv_bfloat16>(a, dim, row_tiles16, stream);
+cudaError_t launch_attn_rows(const AttnArgs& a, int dtype, int dim, cudaStream_t stream) {
+  return dtype == SSS_OUT_F16 ? rows_dim<__half>(a, dim, stream)
+                              : rows_dim<__nv_bfloat16>(a, dim, stream);
 }
 cudaError_t launch_attn_join(const AttnArgs& a, int dtype, int dim, cudaStream_t stream) {
   return dtype == SSS_OUT_F16 ? join_dim<__half>(a, dim, stream)

@@ -25,9 +25,9 @@ void set_error(const char* what, cudaError_t e) {
 // GEMM's token-tile grid dimension inside its 65535 limit
 constexpr int64_t kMaxDim = int64_t{1} << 31;
 constexpr int64_t kMaxTokens = int64_t{1} << 24;
-// the most heads and requests of an attention: its grid stays far inside int64
-constexpr int32_t kMaxHeads = 1 << 16;
-constexpr int32_t kMaxBatch = 1 << 20;
+// the most heads and requests of an attention (its grid's y and z)
+constexpr int32_t kMaxHeads = 1 << 14;
+constexpr int32_t kMaxBatch = 65535;
 
 bool aligned(const void* p, size_t a) {
   return (reinterpret_cast<uintptr_t>(p) % a) == 0;
@@ -72,6 +72,20 @@ cudaError_t ensure_smem_impl(const void* kernel, int bytes) {
   if (have >= bytes) return cudaSuccess;
   e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
   if (e == cudaSuccess) have = bytes;
+  return e;
+}
+
+cudaError_t ensure_large_cluster_impl(const void* kernel) {
+  static std::mutex mu;
+  static std::map<std::pair<const void*, int>, bool> configured;
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  std::lock_guard<std::mutex> lock(mu);
+  bool& have = configured[std::make_pair(kernel, dev)];
+  if (have) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+  if (e == cudaSuccess) have = true;
   return e;
 }
 

@@ -85,15 +85,16 @@ cudaError_t launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, 
                                 void* q_out, const sss_kv_cache_t& cache, const int32_t* slots,
                                 uint32_t* status, cudaStream_t stream);
 
-// How a call of sss_attention is laid out (from its sizes alone).
+// How a call of sss_attention is laid out (from its sizes alone; see attn.cuh).
 struct AttnPlan {
   bool prompt;               // the form on tcgen05; else the row form
-  int row_tiles16;           // the row form's tiles are 16 or 32 rows
+  int rows;                  // of the row form's tiles: 16 or 32
   int hpt, hchunks, tpt;     // heads and tokens of a tile, tiles of a group of heads
   bool one_tile;             // a request is one tile
   int64_t tiles;             // an upper bound of the token tiles
-  int64_t chunk, nsplit;     // keys per split
-  size_t part_bytes, ws_bytes;
+  int64_t chunk, nsplit;     // keys per split, and splits
+  bool join;                 // a second kernel joins what is in the workspace
+  size_t lse_at, ws_bytes;   // the workspace: partial rows, then their sums
 };
 AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& cache, int batch,
                         int max_q, int64_t max_kv);
@@ -117,6 +118,13 @@ cudaError_t ensure_smem_impl(const void* kernel, int bytes);
 template <typename K>
 cudaError_t ensure_smem(K kernel, int bytes) {
   return ensure_smem_impl(reinterpret_cast<const void*>(kernel), bytes);
+}
+
+// Allow a kernel clusters of up to 16 CTAs, once per (kernel, device).
+cudaError_t ensure_large_cluster_impl(const void* kernel);
+template <typename K>
+cudaError_t ensure_large_cluster(K kernel) {
+  return ensure_large_cluster_impl(reinterpret_cast<const void*>(kernel));
 }
 
 // ---------------------------------------------------------------------------

@@ -25,6 +25,7 @@ def attention(c=None, **kw):
 
 
 full = dict(batch=1, tokens=1)
+many = dict(batch=1, tokens=64, max_q=64)
 
 
 @pytest.mark.parametrize("kw,want", [
@@ -36,8 +37,8 @@ full = dict(batch=1, tokens=1)
     (dict(width=0), 1), (dict(kv=None), 1),
     (dict(full, q=None), 1), (dict(full, out=None), 1), (dict(full, cu=None), 1),
     (dict(full, q=P + 8), 3), (dict(full, out=P + 2), 3), (dict(full, cu=P + 2), 3), (dict(full, table=P + 1), 3),
-    (dict(full, max_kv=100000), 5), (dict(full, max_kv=100000, ws=P, ws_bytes=100), 5),
-    (dict(full, max_kv=100000, ws=P + 8, ws_bytes=1 << 30), 3),
+    (dict(many, max_kv=100000), 5), (dict(many, max_kv=100000, ws=P, ws_bytes=100), 5),
+    (dict(many, max_kv=100000, ws=P + 8, ws_bytes=1 << 30), 3),
 ])
 def test_attention_arguments(kw, want):
     assert attention(**kw) == want
@@ -62,9 +63,9 @@ def test_attention_workspace():
     c = cache(heads=8, stride=1024)
     size = lambda *a: L.sss_attention_workspace_bytes(a[0], a[1], ctypes.byref(c), *a[2:])  # noqa: E731
     assert size(1, 32, 1, 1, 16) == 0            # nothing to split
-    assert size(1, 32, 1, 1, 8192) > 32 * 128 * 4  # partial rows
-    assert size(0, 32, 1, 1, 8192) == 0 and size(1, 32, 0, 1, 8192) == 0
-    assert size(1, 31, 1, 1, 8192) == 0 and size(-1, 32, 1, 1, 8192) == 0 and size(1, 32, 1, 1, -1) == 0
+    assert size(64, 32, 1, 64, 8192) > 64 * 32 * 128 * 4  # partial rows
+    assert size(0, 32, 1, 64, 8192) == 0 and size(64, 32, 0, 64, 8192) == 0
+    assert size(64, 31, 1, 64, 8192) == 0 and size(-1, 32, 1, 64, 8192) == 0 and size(64, 32, 1, 64, -1) == 0
 
 
 def test_page_plan_arguments():

@@ -324,10 +324,10 @@ def test_empty_calls_and_python_refusals():
 
 
 def test_workspace_too_small():
-    c = make([1], [4000], 8, 2, 128, BF, 16, seed=22)
+    c = make([20], [4000], 8, 2, 128, BF, 16, seed=22)
     cache = sss.KVCache(c["k"].to(DEV), c["v"].to(DEV), 16)
-    need = sss.sss_attention_workspace_bytes(1, 8, cache, 1, 1, 4000)
-    assert need > 0  # one request of 4000 keys is split over CTAs
+    need = sss.sss_attention_workspace_bytes(20, 8, cache, 1, 20, 4000)
+    assert need > 0  # a chunk of a prompt over 4000 keys is split over CTAs
     with pytest.raises(sss.SssError, match="SSS_E_WORKSPACE"):
         call(c, workspace=torch.empty(need - 16, dtype=torch.uint8, device=DEV))
     check(c, call(c, workspace=torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV)))
