@@ -32,8 +32,13 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
   const int64_t per_tile = static_cast<int64_t>(c.heads) * p.hchunks;
   const int64_t items = std::max<int64_t>(1, p.tiles * per_tile);
   if (p.prompt) {
-    const int64_t splits = std::max<int64_t>(1, std::min(sms / items, (max_kv + 511) / 512));
-    p.chunk = std::max<int64_t>(128, ((max_kv + splits - 1) / splits + 127) / 128 * 128);
+    // Split for SMs that the tiles leave idle, down to one key tile: the join costs about
+    // as much as three, so not below four (30 tokens of 8 heads after 1000: 16.6 us
+    // whole, 10.0 in eight; 30 of 32 heads after 500: 14.0 whole, 12.4 in two; 1500 of 8
+    // heads: 28.8 whole, 20.5 in six).
+    const int64_t kt = (max_kv + 127) / 128;
+    const int64_t splits = kt < 4 ? 1 : std::max<int64_t>(1, std::min(sms / items, kt));
+    p.chunk = std::max<int64_t>(1, (kt + splits - 1) / splits) * 128;
     p.nsplit = std::max<int64_t>(1, (max_kv + p.chunk - 1) / p.chunk);
     p.join = p.nsplit > 1;
     if (p.join) {
@@ -47,11 +52,11 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
   // clusters in a cluster of SMs: 8 of 16 CTAs, 32 of 8), of 128 keys each at least.  A
   // second wave costs more than it evens out (32 requests of 512 keys: 14.2 us whole,
   // 19.3 in pairs; 8 of 125 to 1000: 8.4 us in fours, 16.2 in eights), but where keys
-  // are many (16 requests of 130 to 16384: 89 us in pairs, 59 in fours; 64 of 12000 to
-  // 16384: 534 us whole, 516 in fours).
-  constexpr int64_t kLeast = 128, kMany = 4096;
+  // are many (20 requests of 400 to 3000: 31 us whole, 23.4 in pairs; 16 of 130 to 16384:
+  // 89 us in pairs, 59 in fours; 64 of 12000 to 16384: 534 us whole, 516 in fours).
+  constexpr int64_t kLeast = 128;
   const int64_t fit = items <= 8 ? 16 : items <= 32 ? 8 : items <= 2 * sms / 4 ? 4 : items <= sms ? 2 : 1;
-  int64_t cluster = max_kv >= kMany ? std::max<int64_t>(fit, 4) : fit;
+  int64_t cluster = std::max<int64_t>(fit, max_kv >= 4096 ? 4 : max_kv >= 2048 ? 2 : 1);
   while (cluster > 1 && cluster * kLeast > max_kv) cluster /= 2;
   p.nsplit = cluster;
   p.chunk = kLeast;

@@ -468,15 +468,18 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
 }
 
 // The rows whose tile has more than one split: the splits' outputs, weighted by
-// 2^lse, in split order.  A CTA per row; its warps take every fourth split.
-template <typename T, int D>
-__global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ AttnArgs a) {
-  __shared__ float4 sums[4][D / 4];
-  __shared__ float totals[4];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+// 2^lse, in split order.  WARPS to a row, of which each takes every WARPS-th split.
+constexpr int kJoinWarps = 4;  // of a CTA
+template <typename T, int D, int WARPS>
+__global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const __grid_constant__ AttnArgs a) {
+  __shared__ float4 sums[kJoinWarps][D / 4];
+  __shared__ float totals[kJoinWarps];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, first = warp % WARPS;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int64_t row = blockIdx.x, rows = static_cast<int64_t>(a.tokens) * a.heads;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * (kJoinWarps / WARPS) + warp / WARPS;
+  const int64_t rows = static_cast<int64_t>(a.tokens) * a.heads;
+  if (row >= rows) return;
   const int t = static_cast<int>(row / a.heads);
   // the token's request: the last whose first token is not behind it
   int lo = 0, hi = a.batch;
@@ -489,8 +492,7 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ 
   const AttnRequest rq = attn_request(a, lo, flags);
   const int i = t - rq.q0;
   if (i < 0 || i >= rq.n) return;
-  const int last = min(i / a.tpt * a.tpt + a.tpt, rq.n) - 1;
-  const int lim = attn_limit(rq, last);
+  const int lim = attn_limit(rq, min(i / a.tpt * a.tpt + a.tpt, rq.n) - 1);
   if (lim <= a.chunk) return;
   const int n = (lim + a.chunk - 1) / a.chunk;
   float top = -INFINITY;
@@ -502,7 +504,7 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ 
   float total = 0.f;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-  for (int z = warp; z < n; z += 4) {
+  for (int z = first; z < n; z += WARPS) {
     const float lse = a.part_lse[z * rows + row];
     const float4 v = lane < LANES ? reinterpret_cast<const float4*>(a.part + (z * rows + row) * D)[lane]
                                   : make_float4(0.f, 0.f, 0.f, 0.f);
@@ -514,16 +516,20 @@ __global__ void __launch_bounds__(128) attn_join_kernel(const __grid_constant__ 
     acc.z += f * v.z;
     acc.w += f * v.w;
   }
-  if (lane < LANES) sums[warp][lane] = acc;
-  if (lane == 0) totals[warp] = total;
-  __syncthreads();
-  if (warp != 0 || lane >= LANES) return;
+  if constexpr (WARPS > 1) {
+    static_assert(WARPS == kJoinWarps, "a CTA's row");
+    if (lane < LANES) sums[warp][lane] = acc;
+    if (lane == 0) totals[warp] = total;
+    __syncthreads();
+    if (warp != 0) return;
 #pragma unroll
-  for (int w = 1; w < 4; ++w) {
-    const float4 v = sums[w][lane];
-    total += totals[w];
-    acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
+    for (int w = 1; w < WARPS; ++w) {
+      const float4 v = sums[w][lane % LANES];
+      total += totals[w];
+      acc = make_float4(acc.x + v.x, acc.y + v.y, acc.z + v.z, acc.w + v.w);
+    }
   }
+  if (lane >= LANES) return;
   const float r = total == 0.f ? 0.f : 1.f / total;
   reinterpret_cast<uint2*>(static_cast<T*>(a.out) + row * D)[lane] =
       make_uint2(Pair<T>::pack(acc.x * r, acc.y * r), Pair<T>::pack(acc.z * r, acc.w * r));
@@ -573,13 +579,19 @@ cudaError_t rows_dim(const AttnArgs& a, int dim, cudaStream_t stream) {
     return a.rows == 16 ? rows_mode<T, 64, 1>(a, stream) : rows_mode<T, 64, 2>(a, stream);
   return a.rows == 16 ? rows_mode<T, 128, 1>(a, stream) : rows_mode<T, 128, 2>(a, stream);
 }
-template <typename T>
-cudaError_t join_dim(const AttnArgs& a, int dim, cudaStream_t stream) {
-  const int64_t blocks = static_cast<int64_t>(a.tokens) * a.heads;
+template <typename T, int D>
+cudaError_t run_join(const AttnArgs& a, cudaStream_t stream) {
+  const bool wide = a.nsplit > 8;  // a CTA to a row
+  const int64_t rows = static_cast<int64_t>(a.tokens) * a.heads;
+  const int64_t blocks = wide ? rows : (rows + kJoinWarps - 1) / kJoinWarps;
   if (blocks > INT32_MAX) return cudaErrorNotSupported;
   const dim3 grid(static_cast<unsigned>(blocks));
-  return dim == 64 ? launch(attn_join_kernel<T, 64>, a, grid, 128, 0, stream)
-                   : launch(attn_join_kernel<T, 128>, a, grid, 128, 0, stream);
+  return wide ? launch(attn_join_kernel<T, D, kJoinWarps>, a, grid, 32 * kJoinWarps, 0, stream)
+              : launch(attn_join_kernel<T, D, 1>, a, grid, 32 * kJoinWarps, 0, stream);
+}
+template <typename T>
+cudaError_t join_dim(const AttnArgs& a, int dim, cudaStream_t stream) {
+  return dim == 64 ? run_join<T, 64>(a, stream) : run_join<T, 128>(a, stream);
 }
 
 }  // namespace
