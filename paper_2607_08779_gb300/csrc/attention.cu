@@ -32,13 +32,23 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
   const int64_t per_tile = static_cast<int64_t>(c.heads) * p.hchunks;
   const int64_t items = std::max<int64_t>(1, p.tiles * per_tile);
   if (p.prompt) {
-    // Split for SMs that the tiles leave idle, down to one key tile: the join costs about
-    // as much as three, so not below four (30 tokens of 8 heads after 1000: 16.6 us
-    // whole, 10.0 in eight; 30 of 32 heads after 500: 14.0 whole, 12.4 in two; 1500 of 8
-    // heads: 28.8 whole, 20.5 in six).
-    const int64_t kt = (max_kv + 127) / 128;
-    const int64_t splits = kt < 4 ? 1 : std::max<int64_t>(1, std::min(sms / items, kt));
-    p.chunk = std::max<int64_t>(1, (kt + splits - 1) / splits) * 128;
+    // Split for SMs that the tiles leave idle, down to one key tile, where it pays: a key
+    // tile takes about 1.4 us of an item, the join 2.7 us and what the outputs of `n`
+    // splits, written and read in fp32, take at 5 TB/s (5000 bytes in a ns).  30 tokens of
+    // 8 heads after 1000: 16.4 us whole, 10.5 in eight; 30 of 32 heads after 500: 14.2
+    // whole, 13.2 in five; 500 of 16 heads after 3000: 50.4 whole, 26.9 in five; 512 of 32
+    // heads: 12.3 whole, 19.1 in two; 700 of 8 heads: 15.2 whole, 16.3 in six.
+    const int64_t kt = std::max<int64_t>(1, (max_kv + 127) / 128);
+    const int64_t most = std::max<int64_t>(1, std::min(sms / items, kt));
+    int64_t steps = kt, least = kt * 1400;
+    for (int64_t n = 2; n <= most; ++n) {
+      const int64_t of = (kt + n - 1) / n;
+      const int64_t cost = of * 1400 + 2700 + n * tokens * heads * c.dim * 8 / 5000;
+      if (cost >= least) continue;
+      least = cost;
+      steps = of;
+    }
+    p.chunk = steps * 128;
     p.nsplit = std::max<int64_t>(1, (max_kv + p.chunk - 1) / p.chunk);
     p.join = p.nsplit > 1;
     if (p.join) {
