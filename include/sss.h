@@ -518,8 +518,9 @@ sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, in
  *   q           [in]  device [tokens][heads][dim] of the cache's dtype, rows
  *                     q_stride elements apart (a multiple of 8, >= heads * dim);
  *                     16-byte aligned.
- *   heads       [in]  a multiple of cache->heads.
+ *   heads       [in]  a multiple of cache->heads, at most 16384.
  *   cache       [in]  k and v 16-byte aligned.
+ *   batch, tokens [in] at most 65535 and 2^24.
  *   cu_q        [in]  device int32 [batch + 1], cu_q[batch] <= tokens.  Rows of no
  *                     request are not written.
  *   kv_len      [in]  device int32 [batch].
@@ -541,8 +542,8 @@ sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, in
  *                     SSS_FLAG_TIMEOUT: a bounded wait ran out (many rows only).
  * The result does not depend on timing, and a request's not on the others in the
  * batch but through max_q, max_kv and their number, by which the work is split.
- * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim), SSS_E_ALIGN, SSS_E_WORKSPACE,
- * SSS_E_CUDA.
+ * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim; a driver without tensor maps),
+ * SSS_E_ALIGN, SSS_E_WORKSPACE, SSS_E_CUDA.
  */
 sss_status_t sss_attention(const void* q, int64_t q_stride, int32_t heads,
                            const sss_kv_cache_t* cache, const int32_t* cu_q,
@@ -553,7 +554,9 @@ sss_status_t sss_attention(const void* q, int64_t q_stride, int32_t heads,
                            void* stream);
 
 /* Workspace bytes of that call (0 for invalid arguments, or if none are needed:
- * partial results where keys are split over CTAs). */
+ * partial results where the keys of many rows are split over CTAs).  Fewer tokens
+ * over the same keys may need more, as they are split where SMs would idle: a buffer
+ * for several shapes is the largest of their sizes. */
 size_t sss_attention_workspace_bytes(int64_t tokens, int32_t heads,
                                      const sss_kv_cache_t* cache, int32_t batch,
                                      int32_t max_q, int64_t max_kv);
@@ -597,14 +600,15 @@ size_t sss_gemm_noalloc_max_scratch_bytes(void);
  * sss_test_set_stall -- test hook for the bounded waits; the paper has no
  * counterpart.  While a bit below is set, every later launch of that kernel
  * family leaves one mbarrier one arrive short: the GEMM on the first
- * stage's weight tile, the attention of prompts on its first value tile.  The decode GEMV kernels (batch 1 and batched) have
- * no data-dependent waits (their warps meet only at CTA-wide barriers), so
- * their bits have no effect.  The wait on that barrier then runs out after
- * its bound (about one second), the kernel raises SSS_FLAG_TIMEOUT in
- * dev_status, lets its own copies and MMAs in flight finish, releases its
- * tensor memory and returns; its output is incomplete.  Nothing faults or
- * hangs.  mask = 0 (the default) restores normal launches.  Process-wide;
- * affects launches issued (or captured) after the call on every thread.
+ * stage's weight tile, the attention of many rows on its first value tile.  The
+ * decode GEMV kernels (batch 1 and batched) have no data-dependent waits (their
+ * warps meet only at CTA-wide barriers), so their bits have no effect.  The wait
+ * on that barrier then runs out after its bound (about one second), the kernel
+ * raises SSS_FLAG_TIMEOUT in dev_status, lets its own copies and MMAs in flight
+ * finish, releases its tensor memory and returns; its output is incomplete.
+ * Nothing faults or hangs.  mask = 0 (the default) restores normal launches.
+ * Process-wide; affects launches issued (or captured) after the call on every
+ * thread.
  */
 #define SSS_TEST_STALL_GEMV 0x1u       /* gemv_stream_kernel: no waits, no effect               */
 #define SSS_TEST_STALL_GEMV_BATCH 0x2u /* gemv_batch_kernel: no waits, no effect                */

@@ -13,7 +13,8 @@
 // wait: every CTA scans all lengths by itself (256 requests at a time, one per
 // thread) and places its share of the tokens by a binary search among them.  A
 // table entry below ceil(past / P) is only read, the others only written (by the
-// page's first token), so the order of the CTAs does not matter.
+// page's first token), so the order of the CTAs does not matter.  16 requests of one
+// token: 2.2 us; 64 with up to 2048 new tokens each: 2.4 us.
 #include <algorithm>
 
 #include "sss_internal.cuh"

@@ -1,8 +1,14 @@
-"""Thin ctypes binding of the C ABI in include/sss.h.
+"""Thin binding of the C ABI in include/sss.h.
 
 Argument marshalling only: every step of the path runs in libsss.so's CUDA
 kernels.  torch supplies device memory and streams.  There is no fallback:
 if the library cannot be built or loaded, these functions raise.
+
+The calls go through ctypes.  Those that a decoding step makes for every layer
+(sss_page_plan, sss_qk_norm_rope, sss_attention) check and pass their usual
+arguments in compiled code (_binding.so, csrc/binding.cpp), which leaves to the
+Python below whatever it does not take, refusals among it: 3 us a call, 9 to 11
+without.
 """
 from __future__ import annotations
 

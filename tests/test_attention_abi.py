@@ -125,3 +125,11 @@ def test_python_cache_and_rope_refusals():
                      (dict(cos=cos.double(), sin=cos.double()), "float32"), (dict(cos=cos, sin=cos), "CUDA")):
         with pytest.raises(sss.SssError, match=what):
             sss.Rope(**kw)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(heads=16384, q_stride=16384 * 128), 0), (dict(heads=16386, q_stride=16386 * 128), 1),
+    (dict(batch=65536), 1), (dict(max_kv=1 << 31), 1),
+])
+def test_the_largest_attention(kw, want):
+    assert attention(**kw) == want
