@@ -509,12 +509,13 @@ sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, in
  * A whole prompt (kv_len = n), a chunk of one after what the cache holds, a
  * single token (n = 1) and drafted ones are the same call, and a batch may mix
  * them.  Query head h reads key/value head h / (heads / cache->heads).  A row
- * that sees no key is zero.  Scores, sums and outputs are held in fp32; p_ij is
+ * that sees no key (or none whose score is above minus infinity) is zero.  Scores, sums and outputs are held in fp32; p_ij is
  * rounded to the cache's type for its product with v_j (relative to a maximum
  * that may lie 8 powers of two below the row's own), the output once.
  * Keys and values that a row does not see have no part in it, whatever they
  * hold (infinities and NaN among them); what lies in the cache past kv_len is
- * never used.
+ * never used.  An infinity that a row sees makes its output infinite, or NaN where
+ * its p_ij is too small for the cache's type.
  *   q           [in]  device [tokens][heads][dim] of the cache's dtype, rows
  *                     q_stride elements apart (a multiple of 8, >= heads * dim);
  *                     16-byte aligned.

@@ -83,7 +83,7 @@ __device__ __forceinline__ int attn_limit(const AttnRequest& r, int i) {
 
 // Token tile `tile` of the launch, found by a whole warp: its request and first
 // token.  A request's tiles run from its last tokens, which see the most keys, to
-// its first.  False behind the last tile.  (Each lane brings all of a request's
+// its first.  False behind the last tile.  The flags may differ by lane.  (Each lane brings all of a request's
 // lengths at once: where they are not in the caches, one trip to memory.)
 __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int tile, int& b, int& i0,
                                           AttnRequest& rq, uint32_t& flags) {
@@ -103,6 +103,7 @@ __device__ __forceinline__ bool attn_tile(const AttnArgs& a, int tile, int& b, i
       q1 = a.cu_q[base + lane + 1];
       kv = a.kv_len ? a.kv_len[base + lane] : 0;
       const int64_t n = static_cast<int64_t>(q1) - q0;
+      if (n < 0) flags |= SSS_FLAG_INDEX;
       if (n > 0) nt = static_cast<int>((min(n, static_cast<int64_t>(a.max_q)) + a.tpt - 1) / a.tpt);
     }
     int sum = nt;

@@ -373,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        if (flags && a.status && lane == 0) atomicOr(a.status, flags);
+        if (flags && a.status) atomicOr(a.status, flags);
         if (live || x < 0) {
           ok = __all_sync(0xffffffffu,
                           mbar_wait(&empty_w[item & 1], ((item >> 1) & 1) ^ 1, abort));

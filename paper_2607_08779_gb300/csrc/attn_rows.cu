@@ -133,10 +133,10 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
   int b, i0;
   uint32_t flags = 0;
   AttnRequest rq;
-  if (!attn_tile(a, blockIdx.z, b, i0, rq, flags)) return leave();
-  const int nt = min(a.tpt, rq.n - i0);  // tokens of the tile
+  const bool found = attn_tile(a, blockIdx.z, b, i0, rq, flags);
+  const int nt = found ? min(a.tpt, rq.n - i0) : 0;  // tokens of the tile
   if (nt <= 0) {
-    if (flags && a.status && threadIdx.x == 0) atomicOr(a.status, flags);
+    if (flags && a.status && warp == 0) atomicOr(a.status, flags);
     return leave();
   }
   const int lim1 = attn_limit(rq, i0 + nt - 1);

@@ -680,11 +680,11 @@ def _dtype_code(dtype):
     return {torch.float32: OUT_F32, torch.float16: OUT_F16, torch.bfloat16: OUT_BF16}.get(dtype)
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class KVCache:
     """Keys and values [slots, heads, dim] (fp16 or bf16) in pages of page_size
     slots.  The heads of a slot are dense; slots may be further apart (k and v as
-    columns of one matrix)."""
+    columns of one matrix).  The tensors may be refilled, not replaced."""
     k: "object"
     v: "object"
     page_size: int = 16
@@ -703,11 +703,15 @@ class KVCache:
         if strides[0] != strides[1]:
             raise SssError(fn, 1, "k and v must have the same stride")
         _on_device(fn, k=k, v=v)
-        # (the pointers are read at every call: the tensors may be refilled, not moved)
-        self._desc = KVCacheDesc(_ptr(k), _ptr(v), slots, strides[0], self.page_size, heads, dim,
-                                 _dtype_code(k.dtype))
-        self._ref = ctypes.byref(self._desc)
-        self._address = ctypes.addressof(self._desc)
+        _describe(self, KVCacheDesc(_ptr(k), _ptr(v), slots, strides[0], self.page_size, heads,
+                                    dim, _dtype_code(k.dtype)))
+
+
+def _describe(o, desc):
+    """The C descriptor of an object whose fields do not change, laid out once."""
+    for name, value in (("_desc", desc), ("_ref", ctypes.byref(desc)),
+                        ("_address", ctypes.addressof(desc))):
+        object.__setattr__(o, name, value)
 
 
 def empty_kv_cache(pages: int, page_size: int, heads: int, dim: int, dtype=None,
@@ -720,11 +724,11 @@ def empty_kv_cache(pages: int, page_size: int, heads: int, dim: int, dtype=None,
     return KVCache(k, v, page_size)
 
 
-@dataclass
+@dataclass(frozen=True, eq=False)
 class Rope:
     """The rotation of a model's heads: fp32 cos and sin [max_pos, rot_dim / 2]
     (None: no rotation), the pairs' style, and the fp32 weights [dim] of the query
-    and key heads' norm (None: none)."""
+    and key heads' norm (None: none).  The tensors may be refilled, not replaced."""
     cos: Optional["object"] = None
     sin: Optional["object"] = None
     style: int = ROPE_HALF
@@ -746,12 +750,20 @@ class Rope:
         for name in ("cos", "sin", "q_norm", "k_norm"):
             _need(fn, name, getattr(self, name), torch.float32, optional=True)
         _on_device(fn, cos=self.cos, sin=self.sin, q_norm=self.q_norm, k_norm=self.k_norm)
-        self._desc = RopeDesc(_ptr(self.cos), _ptr(self.sin), _ptr(self.q_norm), _ptr(self.k_norm),
-                              max_pos, 2 * half, self.style, self.eps)
-        self._ref = ctypes.byref(self._desc)
-        self._address = ctypes.addressof(self._desc)
+        _describe(self, RopeDesc(_ptr(self.cos), _ptr(self.sin), _ptr(self.q_norm),
+                                 _ptr(self.k_norm), max_pos, 2 * half, self.style, self.eps))
         sizes = {w.numel() for w in (self.q_norm, self.k_norm) if w is not None}
-        self._weights = 0 if not sizes else sizes.pop() if len(sizes) == 1 else -1
+        object.__setattr__(self, "_weights",
+                           0 if not sizes else sizes.pop() if len(sizes) == 1 else -1)
+
+
+def _empty_on(stream, shape, dtype, device):
+    """torch.empty for a call on `stream`: of that stream's memory, as its earlier
+    and later users are then in order with the call."""
+    import torch
+
+    with torch.cuda.stream(stream):  # (None: the current one)
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _need_int32(fn, **tensors):
@@ -830,7 +842,7 @@ def sss_qk_norm_rope(q, k, v, rope: Rope, positions, cache: KVCache, slots=None,
     qs = _rows(fn, "q", q, tokens, width)
     ks, vs = (_rows(fn, n, t, tokens, d.heads * dim) for n, t in (("k", k), ("v", v)))
     if q_out is None:
-        q_out = torch.empty((tokens, width // dim, dim), dtype=cache.k.dtype, device=q.device)
+        q_out = _empty_on(stream, (tokens, width // dim, dim), cache.k.dtype, q.device)
     _need(fn, "q_out", q_out, cache.k.dtype, tokens * width)
     _on_device(fn, q=q, k=k, v=v, q_out=q_out, dev_status=dev_status)
     if positions is not None or d.dim and rope._desc.rot_dim:
@@ -881,7 +893,7 @@ def sss_attention(q, cache: KVCache, cu_q, kv_len, max_q: int, max_kv: int, bloc
         raise SssError(fn, 1, f"q must be {cache.k.dtype}, as the cache")
     qs = _rows(fn, "q", q, tokens, heads * dim)
     if out is None:
-        out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+        out = _empty_on(stream, (tokens, heads, dim), q.dtype, q.device)
     _need_int32(fn, cu_q=(cu_q, None))
     if batch < 0:
         raise SssError(fn, 1, "cu_q must be [batch + 1]")
@@ -898,7 +910,7 @@ def sss_attention(q, cache: KVCache, cu_q, kv_len, max_q: int, max_kv: int, bloc
     if workspace is None:
         need = sss_attention_workspace_bytes(tokens, heads, cache, batch, max_q, max_kv)
         if need > 0:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = _empty_on(stream, need, torch.uint8, q.device)
     ws_bytes = 0 if workspace is None else workspace.numel()
     width = 0 if block_table is None else block_table.shape[1]
     st = load().sss_attention(q.data_ptr(), qs, heads, cache._ref, cu_q.data_ptr(), _ptr(kv_len),

@@ -331,3 +331,43 @@ def test_workspace_too_small():
     with pytest.raises(sss.SssError, match="SSS_E_WORKSPACE"):
         call(c, workspace=torch.empty(need - 16, dtype=torch.uint8, device=DEV))
     check(c, call(c, workspace=torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV)))
+
+
+def test_requests_that_run_backwards_raise_the_flag():
+    # request 1 ends before it begins; the others are as if it were not there
+    c = make([40, 20], [90, 60], 4, 2, 64, BF, 16, seed=23)
+    want = call(c)
+    bad = dict(c, cu=[0, 60, 40, 60], kv=[60, 60, 60])
+    bad["table"] = torch.cat([c["table"][:1], c["table"][1:], c["table"][1:]])
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = call(bad, max_q=60, status=status)
+    assert int(status) == sss.FLAG_INDEX
+    assert torch.equal(got[40:], want[40:])
+
+
+def test_a_workspace_of_the_call_is_of_its_stream():
+    # what the caller's stream does with its memory meanwhile does not matter
+    c = make([20], [6000], 8, 2, 128, BF, 16, seed=24)
+    want = call(c)
+    cache = sss.KVCache(c["k"].to(DEV), c["v"].to(DEV), 16)
+    need = sss.sss_attention_workspace_bytes(20, 8, cache, 1, 20, 6000)
+    assert need > 0
+    q, table = c["q"].to(DEV), c["table"].to(DEV)
+    cu, kv = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in (c["cu"], c["kv"]))
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for _ in range(20):
+        out = sss.sss_attention(q, cache, cu, kv, 20, 6000, block_table=table, stream=s)
+        for _ in range(10):
+            torch.empty(need, dtype=torch.uint8, device=DEV).fill_(0xFF)
+        torch.cuda.synchronize()
+        assert torch.equal(out.cpu(), want)
+
+
+def test_a_cache_keeps_its_tensors():
+    k = torch.zeros((32, 2, 64), dtype=BF, device=DEV)
+    cache = sss.KVCache(k, torch.zeros_like(k))
+    with pytest.raises(AttributeError):
+        cache.k = torch.zeros_like(k)
+    with pytest.raises(AttributeError):
+        cache.page_size = 32
