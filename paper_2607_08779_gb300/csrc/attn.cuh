@@ -37,6 +37,7 @@ struct AttnArgs {
   int chunk, nsplit;
   int rows;         // of the row form's tiles: 16 or 32
   int stall;        // test hook
+  int box_rows;     // of an output box of the prompt form
   float scale_log2;  // scale * log2(e)
 };
 

@@ -16,7 +16,9 @@
 //   warp 8    issues the products: scores S = Q K^T (both from shared memory), then
 //             O += P V with P from tensor memory.  It takes A and B in turn, which keeps
 //             them half a step apart;
-//   warp 9    TMA producer of Q, K and V (a box per page, or per 128 packed keys);
+//   warps 9, 11  TMA producers of Q and K, and of V (a box per page, or per 128 packed
+//             keys; the boxes of a warp are issued one after another, 16 of them at pages
+//             of 16 keys: one warp for both lost 5 to 10 % there);
 //   warp 10   scheduler: says what the CTA works on next;
 //   warps 12-15  look through V tiles that some row does not see whole.
 //
@@ -68,11 +70,20 @@ constexpr int kThreads = 512;
 constexpr int kKeys = 128;      // of a tile
 constexpr float kRaise = 8.0f;  // powers of two
 constexpr int kTmemCols = 512;  // one CTA per SM
-constexpr int kConsumers = 14;  // warps that read an item
+constexpr int kConsumers = 15;  // warps that read an item
+
+__device__ __forceinline__ void tma_load_3d(const CUtensorMap* map, uint64_t* bar, void* dst, int x,
+                                            int y, int z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+      "[%0], [%1, {%3, %4, %5}], [%2];" ::"r"(smem_u32(dst)),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
 
 struct AttnMaps {
   CUtensorMap q, k, v;
-  CUtensorMap out;  // boxes of 64 columns of 8 tokens
+  CUtensorMap out;  // boxes of 64 columns of what a warp's 32 rows hold of tokens x heads
 };
 
 template <int D>
@@ -397,13 +408,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         int drain = 0;
         (void)mbar_wait(asked, asks & 1, &drain);
       }
-    } else if (warp == 9) {
-      // ---------------- TMA producer ----------------
+    } else if (warp == 9 || warp == 11) {
+      // ---------------- TMA producers: of Q and K, and of V ----------------
+      const bool vals = warp == 11;
+      const CUtensorMap* const map = vals ? &maps.v : &maps.k;
+      uint64_t* const full = vals ? full_v : full_k;
+      uint64_t* const empty = vals ? empty_v : empty_k;
+      unsigned char* const tiles = smem + (vals ? S::V_OFF : S::K_OFF);
       const int box = a.table ? min(kKeys, 1 << a.page_shift) : kKeys;  // keys of a box
       const int boxes = kKeys / box * S::HALVES;
       const int my = lane / S::HALVES, half = lane % S::HALVES;
       uint32_t flags = 0;
-      int kc = 0, vc = 0, qc[2] = {0, 0};  // tiles asked for
+      int count = 0, qc[2] = {0, 0};  // tiles asked for
       Work w;
       bool ok;
       for (int item = 0; take(item, w, ok); ++item) {
@@ -426,42 +442,35 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (s < 0) flags |= SSS_FLAG_INDEX;
           return static_cast<int>(s < 0 ? a.slots : s);
         };
-        auto put = [&](const CUtensorMap* map, uint64_t* full, uint64_t* empty, int off, int stages,
-                       int& count, int slot) {
-          const int st = count % stages;
-          ok = ok && __all_sync(0xffffffffu,
-                                mbar_wait(empty + st, ((count / stages) & 1) ^ 1, abort));
-          if (!ok) return;
-          if (lane == 0) mbar_arrive_expect_tx(full + st, S::KV_TILE);
-          __syncwarp();
-          if (lane < boxes)
-            tma_load_2d(map, full + st,
-                        smem + off + st * S::KV_TILE + half * S::PART + my * box * 128,
-                        w.kh * D + 64 * half, slot);
-          __syncwarp();
-          ++count;
-        };
         int page = entry(0);
         for (int j = 0; j < nt && ok; ++j) {
           const int slot = slot_of(page, j);
           page = entry(j + 1);
-          put(&maps.k, full_k, empty_k, S::K_OFF, S::KS, kc, slot);
-          if (j == 0) {
+          const int st = count % S::KS;
+          ok = ok && __all_sync(0xffffffffu,
+                                mbar_wait(empty + st, ((count / S::KS) & 1) ^ 1, abort));
+          if (!ok) break;
+          if (lane == 0) mbar_arrive_expect_tx(full + st, S::KV_TILE);
+          __syncwarp();
+          if (lane < boxes)
+            tma_load_2d(map, full + st, tiles + st * S::KV_TILE + half * S::PART + my * box * 128,
+                        w.kh * D + 64 * half, slot);
+          __syncwarp();
+          ++count;
+          if (j > 0 || vals) continue;
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              if (n[s] == 0 || !ok) continue;
-              ok = __all_sync(0xffffffffu, mbar_wait(&empty_q[s], (qc[s] & 1) ^ 1, abort));
-              if (!ok) continue;
-              if (lane == 0) mbar_arrive_expect_tx(&full_q[s], w.nh * tt * 128 * S::HALVES);
-              __syncwarp();
-              if (lane < w.nh * S::HALVES)  // at most 16 heads
-                tma_load_2d(&maps.q, &full_q[s], smem + s * S::Q_TILE + half * S::PART + my * tt * 128,
-                            (w.kh * a.group + w.g0 + my) * D + 64 * half, w.q0 + w.i0 + s * tt);
-              __syncwarp();
-              ++qc[s];
-            }
+          for (int s = 0; s < 2; ++s) {
+            if (n[s] == 0 || !ok) continue;
+            ok = __all_sync(0xffffffffu, mbar_wait(&empty_q[s], (qc[s] & 1) ^ 1, abort));
+            if (!ok) continue;
+            if (lane == 0) mbar_arrive_expect_tx(&full_q[s], a.hpt * tt * 128 * S::HALVES);
+            __syncwarp();
+            if (lane < S::HALVES)
+              tma_load_3d(&maps.q, &full_q[s], smem + s * S::Q_TILE + lane * S::PART, 64 * lane,
+                          w.q0 + w.i0 + s * tt, w.kh * a.group + w.g0);
+            __syncwarp();
+            ++qc[s];
           }
-          put(&maps.v, full_v, empty_v, S::V_OFF, S::VS, vc, slot);
         }
         if (!ok) break;
       }
@@ -470,10 +479,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         int drain = 0;
         for (int s = 0; s < 2; ++s)
           if (qc[s] > 0) (void)mbar_wait(&full_q[s], (qc[s] - 1) & 1, &drain);
-        for (int i = max(0, kc - S::KS); i < kc; ++i)
-          (void)mbar_wait(&full_k[i % S::KS], (i / S::KS) & 1, &drain);
-        for (int i = max(0, vc - S::VS); i < vc; ++i)
-          (void)mbar_wait(&full_v[i % S::VS], (i / S::VS) & 1, &drain);
+        for (int i = max(0, count - S::KS); i < count; ++i)
+          (void)mbar_wait(full + i % S::KS, (i / S::KS) & 1, &drain);
       }
     } else if (warp == 8) {
       // ---------------- issuer of the products ----------------
@@ -691,16 +698,23 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lanes = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
     const uint32_t sc_col = lanes + s * kKeys, o_col = lanes + 2 * kKeys + s * D;
     uint32_t sph = 0, dph = 0;
-    bool ok;
-    Work w;
-    for (int item = 0; take(item, w, ok); ++item) {
+    // of an item: its first key, the row tile's key tiles, and the keys that the row
+    // sees and that all rows of the row tile see (the rest stays in shared memory, which
+    // the item keeps until these warps have finished it)
+    int k0, n, lim, whole;
+    bool more;
+    auto begin = [&](int item) {
+      Work w;
+      bool ok;
+      more = take(item, w, ok);
       const AttnRequest rq = {w.q0, w.n, w.kv};
-      const int i = w.i0 + ti;
-      const bool in = g < w.nh && i < w.n;
-      const int lim = in ? attn_limit(rq, i) : 0;
-      // keys that all rows of the row tile see
-      const int whole = attn_limit(rq, min(w.i0 + s * tt, w.n - 1));
-      const int n = s ? w.n1 : w.n0;
+      k0 = w.k0;
+      n = s ? w.n1 : w.n0;
+      lim = g < w.nh && w.i0 + ti < w.n ? attn_limit(rq, w.i0 + ti) : 0;
+      whole = attn_limit(rq, min(w.i0 + s * tt, w.n - 1));
+    };
+    begin(0);
+    for (int item = 0; more; ++item) {
       float mx = -INFINITY;
       float2 sum[4];
 #pragma unroll
@@ -717,15 +731,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int c = 0; c < 4; ++c)
 #pragma unroll
           for (int x = 0; x < 32; ++x) asm volatile("" : "+r"(v[c][x]));  // (not before the wait)
-        const int key0 = w.k0 + kKeys * j;
+        const int key0 = k0 + kKeys * j;
         if (key0 + kKeys > whole) {
           const int left = lim - key0;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             if (key0 + 32 * c + 32 <= whole) continue;
+            const int m = min(max(left - 32 * c, 0), 32);
+            const uint32_t keep = m == 32 ? 0xFFFFFFFFu : (1u << m) - 1u;
 #pragma unroll
             for (int x = 0; x < 32; ++x)
-              if (32 * c + x >= left) v[c][x] = 0xFF800000u;
+              if (!(keep & (1u << x))) v[c][x] = 0xFF800000u;
           }
         }
         float t[4];
@@ -745,7 +761,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int x = 0; x < 4; ++x) sum[x] = make_float2(sum[x].x * f, sum[x].y * f);
           if (j > 0) {
-#pragma unroll
+#pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
               uint32_t o[16];
               tmem_ld_async<16>(o_col + 16 * c, o);
@@ -779,26 +795,36 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&full_p[s]);
       }
-      // the row's output
-      if (n > 0) {
-        wait(&done[s], dph);
-        dph ^= 1;
-        tc_fence_after();
-      }
+      // the row's output: all that can be is got ready while the last product runs, the
+      // next item among it
+      const Work& w = works[item & 1];
+      const int i = w.i0 + ti, keys = n;
+      const bool in = g < w.nh && i < w.n;
       const float2 s01 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
       const float total = s01.x + s01.y;
       const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
       const int64_t at = static_cast<int64_t>(w.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
       const int64_t zat = static_cast<int64_t>(w.z) * a.tokens * a.heads + at;
+      const uint32_t rows_in = __ballot_sync(0xffffffffu, in);
+      const bool alone = w.alone;
+      char* base = alone ? static_cast<char*>(a.out) + at * (D * 2)
+                         : reinterpret_cast<char*>(a.part) + zat * (D * 4);
+      const int out_x = w.kh * a.group + w.g0 + g, out_y = w.q0 + i;
+      // the notes' keys are counted from there
+      const int seen_keys = lim - w.k0 - max(w.lim0 - w.k0, 0) / kKeys * kKeys;
+      begin(item + 1);
+      if (keys > 0) {
+        wait(&done[s], dph);
+        dph ^= 1;
+        tc_fence_after();
+      }
       // 128 bytes of each of the warp's rows at a time, through shared memory (rows in
-      // swizzled atoms of eight).  Eight rows are eight tokens of a head: a TMA store
-      // takes them while the warp goes on; those at a request's end, and partial
-      // results, are stored by the warp, four rows at a time.
+      // swizzled atoms of eight).  The 32 rows are a box of tokens x heads, or up to four
+      // (each is issued by itself, 130 cycles): a TMA store takes it while the warp goes
+      // on; those at a request's end, and partial results, are stored by the warp, four
+      // rows at a time.
       unsigned char* stage = smem + S::OUT_OFF + warp * 4096;
       const uint32_t mine = smem_u32(stage) + lane * 128;
-      const uint32_t rows_in = __ballot_sync(0xffffffffu, in);
-      char* base = w.alone ? static_cast<char*>(a.out) + at * (D * 2)
-                           : reinterpret_cast<char*>(a.part) + zat * (D * 4);
       auto put = [&](const uint32_t (&o)[32], int off, int c, bool boxes) {
         asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (of this stage)
         __syncwarp();
@@ -811,13 +837,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         uint32_t left = rows_in;
         if (boxes) {
-          // lane 8 k: rows 8 k .. 8 k + 7, if all are tokens of the request
-          const bool whole = (rows_in >> (lane & 24) & 255u) == 255u;
-          if ((lane & 7) == 0 && whole)
+          const uint32_t all = a.box_rows == 32 ? ~0u : (1u << a.box_rows) - 1;
+          const int b0 = lane & ~(a.box_rows - 1);
+          const bool whole = (rows_in >> b0 & all) == all;  // all are tokens of the request
+          if (lane == b0 && whole)
             asm volatile(
-                "cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(
+                "cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(
                     reinterpret_cast<uint64_t>(&maps.out)),
-                "r"((w.kh * a.group + w.g0 + g) * D + 64 * c), "r"(w.q0 + i), "r"(mine)
+                "r"(64 * c), "r"(out_y), "r"(out_x), "r"(mine)
                 : "memory");
           asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           const uint32_t some = __ballot_sync(0xffffffffu, !whole);
@@ -838,10 +865,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (left >> row & 1) *reinterpret_cast<uint4*>(dst + off + (lane & 7) * 16) = u;
         }
       };
-      const uint32_t keep = n > 0 ? 0xFFFFFFFFu : 0u;  // (else nothing was added up there)
+      const uint32_t keep = keys > 0 ? 0xFFFFFFFFu : 0u;  // (else nothing was added up there)
       // (Compact code, each path in a loop of its own: it runs once an item, out of
       // the instruction caches.)
-      if (w.alone) {
+      if (alone) {
 #pragma unroll 1
         for (int c = 0; c < D / 64; ++c) {
           uint32_t o[2][32];
@@ -857,7 +884,7 @@ __global__ void __launch_bounds__(kThreads, 1)
               const float2 y = mul2(__uint_as_float(o[h][2 * x]), __uint_as_float(o[h][2 * x + 1]), r);
               p[16 * h + x] = Pair<T>::pack(y.x, y.y) & keep;
             }
-          if (n > 0 && c == D / 64 - 1) {
+          if (keys > 0 && c == D / 64 - 1) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&free_o[s]);
@@ -876,7 +903,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             o[2 * x] = __float_as_uint(y.x) & keep;
             o[2 * x + 1] = __float_as_uint(y.y) & keep;
           }
-          if (n > 0 && c == D / 32 - 1) {
+          if (keys > 0 && c == D / 32 - 1) {
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(&free_o[s]);
@@ -887,7 +914,6 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       if (odd[item & 1]) {  // infinite and NaN values that the row sees
         const uint32_t* notes = first + (item & 1) * D;
-        const int seen_keys = lim - w.k0 - max(w.lim0 - w.k0, 0) / kKeys * kKeys;
         asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");  // (the rows are stored)
         asm volatile("fence.proxy.async;" ::: "memory");
         __syncwarp();
@@ -899,7 +925,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (static_cast<int>((f >> 10) & 1023u) < seen_keys) y -= INFINITY;
           if (static_cast<int>(f >> 20) < seen_keys) y = NAN;
           if (y == 0.f) continue;
-          if (w.alone) {
+          if (alone) {
             uint16_t* at16 = reinterpret_cast<uint16_t*>(base) + d;
             *at16 = static_cast<uint16_t>(Pair<T>::pack(y + Pair<T>::value(*at16), 0.f));
           } else {
@@ -935,8 +961,24 @@ CUresult encode(EncodeTiledFn enc, CUtensorMap* map, CUtensorMapDataType type, c
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+// boxes of 64 columns x tokens x heads
+CUresult encode_heads(EncodeTiledFn enc, CUtensorMap* map, CUtensorMapDataType type,
+                      const void* base, int heads, int dim, int64_t tokens, int64_t stride,
+                      int box_tokens, int box_heads) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(tokens),
+                              static_cast<cuuint64_t>(heads)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(stride) * 2,
+                                 static_cast<cuuint64_t>(dim) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_tokens),
+                             static_cast<cuuint32_t>(box_heads)};
+  const cuuint32_t estr[3] = {1, 1, 1};
+  return enc(map, type, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 template <typename T, int D>
-cudaError_t run_prompt(const AttnArgs& a, cudaStream_t stream) {
+cudaError_t run_prompt(AttnArgs a, cudaStream_t stream) {
   EncodeTiledFn enc = tensor_map_encoder();
   if (enc == nullptr) return cudaErrorNotSupported;
   const CUtensorMapDataType type = std::is_same<T, __half>::value
@@ -944,14 +986,18 @@ cudaError_t run_prompt(const AttnArgs& a, cudaStream_t stream) {
                                        : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
   const int box = a.table ? std::min(kKeys, 1 << a.page_shift) : kKeys;
   AttnMaps maps;
-  if (encode(enc, &maps.q, type, a.q, static_cast<int64_t>(a.heads) * D, a.tokens, a.q_stride,
-             a.tpt / 2) != CUDA_SUCCESS ||
+  const int tt = a.tpt / 2;
+  // the output's boxes: tokens (a power of two that divides a row tile's) x heads
+  const int bt = std::min(tt & -tt, 32), bh = bt == tt ? 32 / bt : 1;
+  a.box_rows = bt * bh;
+  if (encode_heads(enc, &maps.q, type, a.q, a.heads, D, a.tokens, a.q_stride, tt, a.hpt) !=
+          CUDA_SUCCESS ||
       encode(enc, &maps.k, type, a.k, static_cast<int64_t>(a.kv_heads) * D, a.slots, a.kv_stride,
              box) != CUDA_SUCCESS ||
       encode(enc, &maps.v, type, a.v, static_cast<int64_t>(a.kv_heads) * D, a.slots, a.kv_stride,
              box) != CUDA_SUCCESS ||
-      encode(enc, &maps.out, type, a.out, static_cast<int64_t>(a.heads) * D, a.tokens,
-             static_cast<int64_t>(a.heads) * D, 8) != CUDA_SUCCESS)
+      encode_heads(enc, &maps.out, type, a.out, a.heads, D, a.tokens,
+                   static_cast<int64_t>(a.heads) * D, bt, bh) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
   auto kern = attn_prompt_kernel<T, D>;
   cudaError_t e = ensure_smem(kern, PromptSmem<D>::TOTAL);

@@ -10,13 +10,13 @@ from test_kernel_order import kernel_text
 
 
 def roles(items, stages, keys_seen=True):
-    """Generators of scheduler, producer, issuer, tensor core, four warps that look
-    through values, and 2 x 2 softmax warps (of 2 x 4) over items (n0, n1) of key
+    """Generators of scheduler, producers (of queries and keys, and of values), issuer,
+    tensor core, four warps that look through values, and 2 x 2 softmax warps (of 2 x 4) over items (n0, n1) of key
     tiles.  keys_seen: a stage of keys is given back by the issuer and by the warp
     that sees every key tile, not by the issuer alone."""
     pair = lambda n: [Bar(n), Bar(n)]  # noqa: E731
     full_q, empty_q, full_s, full_p, done, free_o = pair(1), pair(1), pair(1), pair(2), pair(1), pair(2)
-    full_w, empty_w = pair(1), pair(10)
+    full_w, empty_w = pair(1), pair(11)
     ring = lambda n: [Bar(n) for _ in range(stages)]  # noqa: E731
     full_k, empty_k, full_v, seen, empty_v = ring(1), ring(2 if keys_seen else 1), ring(1), ring(4), ring(1)
     queue, works = [], [None, None]
@@ -49,7 +49,9 @@ def roles(items, stages, keys_seen=True):
 
     rng = random.Random(1)
 
-    def producer():
+    ended = []
+
+    def producer(values):
         c, q = 0, [0, 0]
         i = 0
         while True:
@@ -58,20 +60,20 @@ def roles(items, stages, keys_seen=True):
             empty_w[i & 1].arrive()
             if n is None:
                 yield lambda: not flying
-                flying.append(None)
+                ended.append(values)
+                if len(ended) == 2:
+                    flying.append(None)
                 return
             for j in range(max(n)):
                 st, ph = at(c)
-                yield lambda: empty_k[st].passed(ph ^ 1)
-                copy(full_k[st])
-                if j == 0:
+                yield lambda: (empty_v if values else empty_k)[st].passed(ph ^ 1)
+                copy((full_v if values else full_k)[st])
+                if j == 0 and not values:
                     for s in range(2):
                         if n[s]:
                             yield lambda: empty_q[s].passed(q[s] & 1 ^ 1)
                             copy(full_q[s])
                             q[s] += 1
-                yield lambda: empty_v[st].passed(ph ^ 1)
-                copy(full_v[st])
                 c += 1
             i += 1
 
@@ -163,15 +165,18 @@ def roles(items, stages, keys_seen=True):
     def softmax(s):
         sp = dp = 0
         i = 0
+        yield from take(0)
+        after = works[0]
         while True:
-            yield from take(i)
-            n = works[i & 1]
+            n = after
             if n is None:
                 return
             for j in range(n[s]):
                 yield lambda: full_s[s].passed(sp)
                 sp ^= 1
                 full_p[s].arrive()
+            yield from take(i + 1)
+            after = works[i + 1 & 1]
             if n[s]:
                 yield lambda: done[s].passed(dp)
                 dp ^= 1
@@ -179,7 +184,7 @@ def roles(items, stages, keys_seen=True):
             empty_w[i & 1].arrive()
             i += 1
 
-    return ([scheduler(), producer(), issuer(), tensor_core(), memory()] + [looker(i) for i in range(4)]
+    return ([scheduler(), producer(False), producer(True), issuer(), tensor_core(), memory()] + [looker(i) for i in range(4)]
             + [softmax(s) for s in (0, 0, 1, 1)])
 
 
@@ -194,7 +199,7 @@ def all_finish(items, stages, keys_seen):
     for i in range(150):
         pick = rng.choice
         if i % 2:
-            order = list(range(13))
+            order = list(range(14))
             rng.shuffle(order)
             pick = lambda ready: min(ready, key=order.index)  # noqa: E731
         if not finishes(roles(items, stages, keys_seen), pick):
@@ -216,4 +221,4 @@ def test_the_kernel_gives_back_as_the_model_does():
     body = kernel_text("attn_prompt.cu", "attn_prompt_kernel")
     assert "mbar_init(&empty_k[s], 2);" in body
     assert body.count("mbar_arrive(&empty_k[") == 2 and body.count("umma_commit(&empty_k[") == 3
-    assert body.count("mbar_wait(&full_k[") == 3 and body.count(" wait(&full_k[") == 1
+    assert body.count("mbar_wait(&full_k[") == 2 and body.count(" wait(&full_k[") == 1
