@@ -59,17 +59,18 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
     return p;
   }
   // Few rows: a cluster of as many CTAs as run at a time (two an SM, and whole
-  // clusters in a cluster of SMs: 8 of 16 CTAs, 32 of 8), of 128 keys each at least.  A
-  // second wave costs more than it evens out (32 requests of 512 keys: 14.2 us whole,
-  // 19.3 in pairs; 8 of 125 to 1000: 8.4 us in fours, 16.2 in eights), but where keys
-  // are many (20 requests of 400 to 3000: 31 us whole, 23.4 in pairs; 16 of 130 to 16384:
-  // 89 us in pairs, 59 in fours; 64 of 12000 to 16384: 534 us whole, 516 in fours).
+  // clusters in a cluster of SMs: 8 of 16 CTAs, 32 of 8), while half as many would have
+  // more than 128 keys each (one request of 500 keys: 5.8 us in pairs, 4.8 in fours; of
+  // 900: 5.8 in fours, 4.9 in eights).  A second wave costs more than it evens out (24
+  // requests of 150 to 1200 keys: 15.7 us whole, 17.5 in pairs; 32 of 256 to 2000: 24.6 in
+  // pairs, 31.2 in fours), but where keys are many (20 requests of 400 to 3000: 30.6 us
+  // whole, 23.0 in pairs; 16 of 130 to 16384: 89 us in pairs, 59 in fours; 64 of 12000 to
+  // 16384: 548 us whole, 530 in fours).
   constexpr int64_t kLeast = 128;
   const int64_t fit = items <= 8 ? 16 : items <= 32 ? 8 : items <= 2 * sms / 4 ? 4 : items <= sms ? 2 : 1;
   int64_t cluster = std::max<int64_t>(fit, max_kv >= 4096 ? 4 : max_kv >= 2048 ? 2 : 1);
-  while (cluster > 1 && cluster * kLeast > max_kv) cluster /= 2;
+  while (cluster > 1 && (cluster - 1) * kLeast >= max_kv) cluster /= 2;
   p.nsplit = cluster;
-  p.chunk = kLeast;
   return p;
 }
 

@@ -11,14 +11,16 @@
 // running maximum m, sum and fp32 output of its own; they meet once, at the end.
 // 16 keys never leave a page, so a step's rows have one base address; 32 steps'
 // table entries are read ahead, one per lane.  Where tiles are few, the keys of one are
-// split over the CTAs of a cluster, which join their outputs through distributed shared
-// memory: no second kernel, no workspace, and a fixed order.
+// split over the CTAs of a cluster, 64 at a time in turn, which join their outputs through
+// distributed shared memory: no second kernel, no workspace, and a fixed order.  The
+// stores into a peer are counted by a barrier there (a cluster-wide barrier after plain
+// ones took 0.2 to 0.4 us longer).
 //
 // Measured (32 heads of 128 over 8, bf16): 64 requests of 12000 to 16384 keys 530 us, 7.0
 // TB/s, above the copy rate; 16 ragged ones of 130 to 16384 (64 heads) 59.6 us, 84 % of
-// it, the longest request's cluster being last; one request of 2047 keys 6.5 us, the
-// launch, the table's and the first keys' latency and the join.  A ring of two or four
-// steps, and three CTAs an SM, were slower on the whole; so was dividing all
+// it, the longest request's cluster being last; one request of 2047 keys 5.8 us, the
+// launch, the lengths' and the first keys' latency and the join.  A ring of two or four
+// steps (at 16 rows), and three CTAs an SM, were slower on the whole; so was dividing all
 // requests' keys evenly over the SMs with a second kernel to join (64 against 59, 558
 // against 516 us).
 // m is raised only where a score passes it by 8 (then 2^8 at most enters the
@@ -27,6 +29,7 @@
 #include <algorithm>
 
 #include "attn.cuh"
+#include "tc.cuh"
 
 namespace sss {
 namespace {
@@ -34,14 +37,18 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStep = 16;   // keys of a warp's step
-constexpr int kStages = 3;  // steps in a warp's ring
 constexpr float kRaise = 8.0f;
 
 template <int D, int R, bool CL>
 struct RowsSmem {
+  // Steps in a warp's ring: as many as leave room for two CTAs an SM (32 rows of 128: 16
+  // requests of 500 to 4000 keys and 32 heads to a key/value head: 38.4 us with three and
+  // one CTA, 23.2 with two and two).
+  static constexpr int kStages = R * D == 32 * 128 ? 2 : 3;
   static constexpr int TILE = kStep * D * 2;             // 16 keys (or values)
   static constexpr int RING = kStages * 2 * TILE;        // of a warp
-  static constexpr int RINGS = kWarps * RING;
+  static constexpr int LD = D + 4;  // of the warps' outputs, which follow: distinct banks
+  static constexpr int RINGS = std::max(kWarps * RING, kWarps * R * LD * 4);
   // the splits' pieces of the values that this one joins (their number rounded up)
   static constexpr int TOTAL = RINGS + (CL ? (R * D / 4 + 16) * 16 : 0);
 };
@@ -83,39 +90,52 @@ __device__ __forceinline__ void mma16816(float (&c)[4], const uint32_t (&a)[4], 
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// Stores into the shared memory of another CTA of the cluster, at the address that
-// addr is in this one's.
+// Shared memory of another CTA of the cluster, at the address that addr is in this
+// one's; stores into it, whose bytes a barrier there counts.
 __device__ __forceinline__ uint32_t of_peer(uint32_t addr, int rank) {
   uint32_t r;
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
   return r;
 }
-__device__ __forceinline__ void peer_store(uint32_t addr, float v) {
-  asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
-}
-__device__ __forceinline__ void peer_store(uint32_t addr, float4 v) {
-  asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y),
-               "f"(v.z), "f"(v.w)
+__device__ __forceinline__ void peer_store(uint32_t addr, float v, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(
+                   addr),
+               "f"(v), "r"(bar)
                : "memory");
 }
+__device__ __forceinline__ void peer_store(uint32_t addr, float4 v, uint32_t bar) {
+  asm volatile(
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, "
+      "[%5];" ::"r"(addr),
+      "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(bar)
+      : "memory");
+}
 
-// MT tiles of 16 rows.  CL: the splits of a tile's keys are the CTAs of a cluster, of
-// equal length whatever the request's, and join through its shared memory: each adds up
-// a share of the values (16 bytes at a time), and the others store their partial results
-// there.
+// MT tiles of 16 rows.  CL: the splits of a tile's keys are the CTAs of a cluster, whose
+// keys differ in number by 64 at most, and join through its shared memory: each adds up a
+// share of the values (16 bytes at a time), and all store their partial results there.
 template <typename T, int D, int MT, bool CL>
 __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int R = 16 * MT;
   using S = RowsSmem<D, R, CL>;
+  constexpr int kStages = S::kStages;
   constexpr int CH = D / 8;       // 16-byte pieces of a row
   constexpr int KD = D / 16;      // mma steps along d
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float wmax[kWarps][R], wsum[kWarps][R];
   __shared__ float split_lse[CL ? 16 : 1][R];  // of every split
+  __shared__ uint64_t arrived;  // what the splits store here
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   // another CTA's shared memory exists only once that CTA has started: waited for
   // before the first store into a peer
-  if constexpr (CL) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  if constexpr (CL) {
+    if (threadIdx.x == 0) {
+      mbar_init(&arrived, 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
@@ -130,6 +150,18 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
   const auto leave = [&]() {
     if constexpr (CL) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   };
+  // The keys go to the splits and their warps 16 at a time in turn: whatever the
+  // request's length, step s of the warp starts at key_of(s).  So the table's entries of
+  // its first 32 steps (one per lane) are asked for with the request's lengths, not after.
+  const auto key_of = [&](int s) { return kStep * (warp + kWarps * (CL ? z + a.nsplit * s : s)); };
+  const int64_t width = static_cast<int64_t>(a.table_width) << a.page_shift;
+  const auto entry = [&](const int32_t* table, int s) {
+    const int64_t key = kStep * (warp + kWarps * (CL ? z + static_cast<int64_t>(a.nsplit) * s : s));
+    return key < width && key < a.max_kv ? __ldg(table + (key >> a.page_shift)) : 0;
+  };
+  int page = 0;
+  if (a.table && a.one_tile && blockIdx.z < a.batch)
+    page = entry(a.table + static_cast<int64_t>(blockIdx.z) * a.table_width, lane);
   int b, i0;
   uint32_t flags = 0;
   AttnRequest rq;
@@ -140,36 +172,29 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     return leave();
   }
   const int lim1 = attn_limit(rq, i0 + nt - 1);
-  int k0 = 0, k1 = lim1, chunk = 0;
-  bool alone = true;  // the tile has no other split
-  if constexpr (CL) {
-    constexpr int kAll = kWarps * kStep;
-    chunk = max(a.chunk,
-                ((lim1 + a.nsplit - 1 >> (31 - __clz(a.nsplit))) + kAll - 1) / kAll * kAll);
-    k0 = min(z * chunk, lim1);
-    k1 = min(lim1, k0 + chunk);
-    alone = lim1 <= chunk;
-    if (k0 >= k1 && z > 0 && alone) return leave();
-  }
   const int lim0 = attn_limit(rq, i0);
-  const int steps = (max(k1 - k0, 0) + kStep - 1) / kStep;
-
-  // The warp's steps: warp, warp + 4, ... of the split's.  Lane l keeps the table
-  // entry of the warp's step 32 n + l.
-  const int mine = warp < steps ? (steps - warp + kWarps - 1) / kWarps : 0;
+  const int steps = (lim1 + kStep - 1) / kStep;
+  // splits with keys
+  const int n = CL ? max(1, min(a.nsplit, (steps + kWarps - 1) / kWarps)) : 1;
+  const bool alone = n == 1;  // the tile has no other split
+  if (CL && alone && z > 0) return leave();
+  const int first = warp + kWarps * z;
+  const int turn = CL ? 31 - __clz(kWarps * a.nsplit) : 2;  // (a cluster is a power of two)
+  static_assert(kWarps == 4, "turn");
+  const int mine = first < steps ? (steps - first - 1 >> turn) + 1 : 0;  // steps of the warp
   const int32_t* table = a.table ? a.table + static_cast<int64_t>(b) * a.table_width : nullptr;
-  int page = 0;
   unsigned char* ring = smem + warp * S::RING;
   const uint32_t ring_addr = smem_addr(ring);
   const int64_t row_bytes = a.kv_stride * 2;
+  // each split adds up `per` of the tile's 16-byte pieces: piece x belongs to split x / per
+  constexpr int PIECES = D / 4;  // of a row
+  const int rows = nt * a.hpt;  // (with those of heads that a last group of heads lacks)
+  const int per = CL ? (rows * PIECES + n - 1) / n : 1;
+  const int per_inverse = CL ? (1 << 20) / per + 1 : 1;  // (exact: x < 1024, per <= 512)
   auto issue = [&](int s) {
     if (s < mine) {
-      if (table && (s & 31) == 0) {
-        const int ahead = s + lane;
-        const int key = k0 + kStep * (warp + kWarps * ahead);
-        page = ahead < mine ? __ldg(table + (key >> a.page_shift)) : 0;
-      }
-      const int key = k0 + kStep * (warp + kWarps * s);
+      if (table && (s & 31) == 0 && (s > 0 || !a.one_tile)) page = entry(table, s + lane);
+      const int key = key_of(s);
       int64_t slot = rq.q0 + key;
       if (table) slot = attn_slot(a, __shfl_sync(0xffffffffu, page, s & 31), key);
       if (slot < 0) flags |= SSS_FLAG_INDEX;
@@ -180,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
 #pragma unroll
       for (int i = 0; i < kStep * CH / 32; ++i) {
         const int row = (lane + 32 * i) / CH, c = (lane + 32 * i) % CH;
-        const bool in = slot >= 0 && key + row < k1;
+        const bool in = slot >= 0 && key + row < lim1;
         const int64_t off = in ? row * row_bytes + c * 16 : 0;
         const uint32_t to = dst + row * (D * 2) + ((c ^ (row & 7)) * 16);
         copy16(to, ksrc + off, in);
@@ -233,7 +258,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
     __syncwarp();
     const uint32_t kt = ring_addr + (s % kStages) * 2 * S::TILE, vt = kt + S::TILE;
-    const int key0 = k0 + kStep * (warp + kWarps * s);
+    const int key0 = key_of(s);
 
     // scores: two tiles of 8 keys, each in two sums (shorter chains of products)
     float sc[MT][2][4], odd_sc[MT][2][4];
@@ -378,10 +403,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
   if (flags && a.status) atomicOr(a.status, flags);
 
   // join the warps
-  constexpr int LD = D + 4;  // (rows' lanes in distinct banks)
-  static_assert(kWarps * R * LD * 4 <= S::RINGS, "the partial outputs reuse the rings");
+  constexpr int LD = S::LD;
   float* part = reinterpret_cast<float*>(smem);
-  const int rows = nt * a.hpt;  // (with those of heads that a last group of heads lacks)
   __syncthreads();
 #pragma unroll
   for (int m = 0; m < MT; ++m)
@@ -399,11 +422,17 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
         *reinterpret_cast<float2*>(dst + 8 * n) = make_float2(o[m][n][2 * e], o[m][n][2 * e + 1]);
     }
   __syncthreads();
-  const int n = CL ? (lim1 + chunk - 1) / chunk : 1;  // splits with keys
   // pieces of 16 bytes; with CL those of a split follow one another in `gather`
-  constexpr int PIECES = D / 4;
   const uint32_t gather = smem_addr(smem + S::RINGS), lse0 = smem_addr(&split_lse[0][0]);
-  if (CL && !alone) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  if (CL && !alone) {
+    if (threadIdx.x == 0) {  // from each split this one's pieces and their rows' sums
+      const int end = min(z * per + per, rows * PIECES);
+      const int bytes = (end - z * per) * 16 + ((end - 1) / PIECES - z * per / PIECES + 1) * 4;
+      if (z < n) mbar_arrive_expect_tx(&arrived, z * per < end ? n * bytes : 0);
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
   for (int x = threadIdx.x; x < rows * PIECES; x += kThreads) {
     const int row = x / PIECES, d = 4 * (x % PIECES);
     const int i = token_of(row), g = row - i * a.hpt;
@@ -433,19 +462,22 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
       if (g < nh) *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
     } else if constexpr (CL) {
       if (z < n) {
-        const int per = (rows * PIECES + n - 1) / n, to = x / per;
-        peer_store(of_peer(gather + (z * per + x - to * per) * 16, to), acc);
+        const int to = x * per_inverse >> 20;
+        const uint32_t bar = of_peer(smem_addr(&arrived), to);
+        peer_store(of_peer(gather + (z * per + x - to * per) * 16, to), acc, bar);
         // (the row's pieces belong to a few of the splits: each gets its sum)
-        if (d == 0 || x == to * per) peer_store(of_peer(lse0 + (z * R + row) * 4, to), lse);
+        if (d == 0 || x == to * per) peer_store(of_peer(lse0 + (z * R + row) * 4, to), lse, bar);
       }
     }
   }
   if constexpr (CL) {
     if (alone) return leave();
-    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    const int per = (rows * PIECES + n - 1) / n;
     if (z >= n) return;
+    int abort = 0;
+    if (!mbar_wait(&arrived, 0, &abort)) {
+      if (a.status && lane == 0) atomicOr(a.status, SSS_FLAG_TIMEOUT);
+      return;
+    }
     // a lane per split and piece (a cluster is a power of two)
     const int cl = a.nsplit, w = threadIdx.x & (cl - 1);
     for (int y0 = 0; y0 < per; y0 += kThreads / cl) {

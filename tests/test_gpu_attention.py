@@ -371,3 +371,15 @@ def test_a_cache_keeps_its_tensors():
         cache.k = torch.zeros_like(k)
     with pytest.raises(AttributeError):
         cache.page_size = 32
+
+
+@pytest.mark.parametrize("fresh,kv,hq,hkv,dim", [
+    ([1] * 5, [3000, 1, 65, 0, 700], 64, 2, 128), ([3, 1, 2], [2100, 64, 129], 20, 2, 128),
+    ([1] * 3, [1025, 4100, 127], 32, 1, 64), ([2, 2], [2047, 1500], 32, 2, 128),
+])
+@pytest.mark.parametrize("page", [16, 256])
+def test_32_rows_over_many_splits(fresh, kv, hq, hkv, dim, page):
+    c = make(fresh, kv, hq, hkv, dim, BF, page, seed=25)
+    first = call(c)
+    check(c, first)
+    assert torch.equal(call(c), first)
