@@ -9,8 +9,9 @@
 // `hchunks` tiles).
 //
 // Keys.  A tile's keys may be cut into splits.  With few rows they are the CTAs of a
-// cluster of nsplit, which join there; with many rows each split of `chunk` keys leaves its normalised fp32 rows and the log2 of
-// their sums in the workspace, and attn_join_kernel adds them.
+// cluster of nsplit, which join there; with many rows each split of `chunk` keys leaves
+// its normalised fp32 rows and the log2 of their sums in the workspace, and
+// attn_join_kernel adds them.
 #pragma once
 
 #include "sss_internal.cuh"

@@ -41,17 +41,20 @@
 // warps 12-15 replace it by zero and note the first key of each kind for its
 // column, and the rows that see that key add it at the end.
 //
-// Measured: 8192 tokens of 32 heads of 128 over 8 key/value heads, bf16: 331 us, 1.66
-// PFLOP/s of what the causal rows need, 87 % of the measured bf16 rate (tensor pipe busy
-// 75 % of the SMs' cycles, at 1.90 GHz).  A step of both row tiles takes about 2900
-// cycles where its products take 2048: a row tile's softmax is a chain of about 1400
-// (read the scores, the maximum, 128 exponentials, write p), longer than the other
-// tile's products that cover it.  10 ragged prompts: 86 us, 2.1 times their
-// products' time: an item's end and start cost about 4500 cycles there, against 3 to 16
-// steps.  512 tokens: 12.3 us, mostly its start and four steps in a row.
+// Measured: 8192 tokens of 32 heads of 128 over 8 key/value heads, bf16: 325 us, 1.69
+// PFLOP/s of what the causal rows need, 89 % of the measured bf16 rate (at 1.91 GHz).  A
+// step of both row tiles takes about 2600 cycles where its products take 2048: a row
+// tile's softmax is a chain of about 1300 (read the scores, the maximum, 128
+// exponentials, write p), longer than the other tile's products that cover it.  10
+// ragged prompts: 86 us, 2.1 times their products' time: an item's end and start cost
+// 4100 to 6000 cycles, against 1 to 16 steps, and a tile of which rows see a part 1000
+// more; this code runs once an item, a quarter of it waiting for instructions.  512
+// tokens: 11.6 us, 4.6 of them up to the first scores, then four steps in a row.
 // Other divisions of the work that were slower at 8192 tokens: an issuing warp per row
 // tile (426 us free-running, 342 in turns), two threads to a row (357), p handed over
-// in halves (437), outputs written by warps of their own (339; ragged 106).
+// in halves (437), outputs written by warps of their own (339; ragged 106) or straight from
+// registers in 32-byte pieces (333; ragged 91), partly seen tiles 32 keys at a time in a
+// loop (353; ragged 97).
 //
 // Tensor memory: scores (then p) of A and B, 128 columns each; outputs of A and B,
 // D columns each.  Every wait is bounded (about one second); on expiry the CTA
