@@ -200,12 +200,13 @@ template <typename IN, typename OUT, int D>
 cudaError_t run(RopeArgs& a, cudaStream_t stream) {
   constexpr int GH = 256 / D;
   const int groups = (a.hq + 2 * a.hkv + GH - 1) / GH;
-  // a run of 8 groups shares its cosines and sines; fewer while the warps of
-  // the call would not fill the SMs
-  a.run = 8;
-  while (a.run > 1 &&
-         static_cast<int64_t>(a.tokens) * ((groups + a.run - 1) / a.run) < 32 * device_sm_count())
-    a.run /= 2;
+  // A run's groups share their cosines and sines; the shortest runs, up to 8, whose warps
+  // are on the SMs all at once (200 tokens of 80 heads: 6.8 us in a wave and a half, 4.4 in
+  // one; 512 of 48 heads: 5.8 and 4.8; 48: 2.5 at any length).
+  a.run = 1;
+  while (a.run < 8 && static_cast<int64_t>(a.tokens) * ((groups + a.run - 1) / a.run) >
+                          kCtas * (kThreads / 32) * device_sm_count())
+    ++a.run;
   a.runs = (groups + a.run - 1) / a.run;
   const int64_t warps = static_cast<int64_t>(a.tokens) * a.runs;
   cudaLaunchConfig_t cfg = {};
