@@ -540,7 +540,7 @@ sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, in
  *                     outside what they may (a request past `tokens` is left
  *                     out, lengths are cut to max_q, max_kv, the table's width or
  *                     the request's own rows, a page that is none reads as zeros).
- *                     SSS_FLAG_TIMEOUT: a bounded wait ran out (many rows only).
+ *                     SSS_FLAG_TIMEOUT: a bounded wait ran out.
  * The result does not depend on timing, and a request's not on the others in the
  * batch but through max_q, max_kv and their number, by which the work is split.
  * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim; a driver without tensor maps),
