@@ -34,7 +34,10 @@
 // The maximum is raised only where a score passes it by 8 powers of two: until then
 // p stays within 2^8 and nothing has to be rescaled.  (O of the tile lies in
 // tensor memory, and a row's thread rescales it there between the scores' arrival,
-// which says that the previous product has completed, and the next one's start.)
+// which says that the previous product has completed, and the next one's start.)  A
+// warp's rows are raised together, by a vote in which only rows of the request have a
+// say: the others hold the next request's queries, or what shared memory happened to
+// hold, and a request's result must not depend on either.
 //
 // A value that is infinite or NaN must not reach rows that do not see its key (0 x
 // NaN would).  In tiles that every row of the CTA sees it cannot do harm; in the others
@@ -703,8 +706,10 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint32_t sph = 0, dph = 0;
     // of an item: its first key, the row tile's key tiles, and the keys that the row
     // sees and that all rows of the row tile see (the rest stays in shared memory, which
-    // the item keeps until these warps have finished it)
+    // the item keeps until these warps have finished it); by how much a score must pass
+    // the row's maximum to raise it
     int k0, n, lim, whole;
+    float pass;
     bool more;
     auto begin = [&](int item) {
       Work w;
@@ -713,7 +718,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const AttnRequest rq = {w.q0, w.n, w.kv};
       k0 = w.k0;
       n = s ? w.n1 : w.n0;
-      lim = g < w.nh && w.i0 + ti < w.n ? attn_limit(rq, w.i0 + ti) : 0;
+      const bool in = g < w.nh && w.i0 + ti < w.n;
+      lim = in ? attn_limit(rq, w.i0 + ti) : 0;
+      pass = in ? kRaise : INFINITY;  // (a row of no token has no say)
       whole = attn_limit(rq, min(w.i0 + s * tt, w.n - 1));
     };
     begin(0);
@@ -757,7 +764,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           t[c] = fmaxf(t[c], __uint_as_float(v[c][31]));
         }
         const float top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
-        if (__any_sync(0xffffffffu, (top - mx) * a.scale_log2 > kRaise)) {
+        if (__any_sync(0xffffffffu, (top - mx) * a.scale_log2 > pass)) {
           const float to = fmaxf(mx, top);
           const float f = to == -INFINITY ? 1.f : ex2((mx - to) * a.scale_log2);
           mx = to;
