@@ -8,7 +8,9 @@
 // heads, at a fraction of its rate), and everything else serves the loads: each of
 // the CTA's four warps streams its own steps of 16 keys and 16 values through a
 // private ring of cp.async copies, without a barrier in the loop, and keeps a
-// running maximum m, sum and fp32 output of its own; they meet once, at the end.
+// running maximum m, sum and fp32 output of its own; they meet once, at the end.  No
+// part is left out of a join because its weight is zero: an infinite or NaN value in it
+// has to reach the row all the same.
 // 16 keys never leave a page, so a step's rows have one base address; 32 steps'
 // table entries are read ahead, one per lane.  Where tiles are few, the keys of one are
 // split over the CTAs of a cluster, 64 at a time in turn, which join their outputs through
@@ -444,8 +446,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float f = ex2(wmax[w][row] - ref);
-      if (f == 0.f && wsum[w][row] == 0.f) continue;  // (a warp without keys)
+      const float f = ex2(wmax[w][row] - ref);  // (0 of a warp without keys)
       const float4 v = *reinterpret_cast<const float4*>(part + (w * R + row) * LD + d);
       total += f * wsum[w][row];
       acc.x += f * v.x;
@@ -489,7 +490,7 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
       for (int m = cl / 2; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
       float total = l == -INFINITY ? 0.f : ex2(l - top);
       float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (total != 0.f) {
+      if (in && w < n) {
         v = *reinterpret_cast<const float4*>(smem + S::RINGS + (w * per + y) * 16);
         v = make_float4(v.x * total, v.y * total, v.z * total, v.w * total);
       }
@@ -551,7 +552,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const __grid
     const float4 v = lane < LANES ? reinterpret_cast<const float4*>(a.part + (z * rows + row) * D)[lane]
                                   : make_float4(0.f, 0.f, 0.f, 0.f);
     const float f = ex2(lse - ref);
-    if (lse == -INFINITY) continue;
     total += f;
     acc.x += f * v.x;
     acc.y += f * v.y;
