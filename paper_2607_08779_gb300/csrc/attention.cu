@@ -28,7 +28,7 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
   p.hchunks = (group + p.hpt - 1) / p.hpt;
   p.one_tile = max_q <= p.tpt;
   p.tiles = p.one_tile ? batch : std::min(tokens / p.tpt + batch,
-                                          static_cast<int64_t>(batch) * ((max_q + p.tpt - 1) / p.tpt));
+                                          static_cast<int64_t>(batch) * ((max_q + int64_t{p.tpt} - 1) / p.tpt));
   const int64_t per_tile = static_cast<int64_t>(c.heads) * p.hchunks;
   const int64_t items = std::max<int64_t>(1, p.tiles * per_tile);
   if (p.prompt) {

@@ -1013,7 +1013,7 @@ cudaError_t run_prompt(AttnArgs a, cudaStream_t stream) {
   cudaError_t e = ensure_smem(kern, PromptSmem<D>::TOTAL);
   if (e != cudaSuccess) return e;
   const int64_t blocks = static_cast<int64_t>(a.tiles) * a.kv_heads * a.hchunks * a.nsplit;
-  if (blocks > INT32_MAX) return cudaErrorNotSupported;
+  if (blocks < 1 || blocks > INT32_MAX) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(blocks));
   cfg.blockDim = dim3(kThreads);

@@ -554,12 +554,17 @@ sss_status_t check_attention(int64_t tokens, int32_t heads, const sss_kv_cache_t
   if (max_q < 0 || max_kv < 0 || max_kv > INT32_MAX / 2) return SSS_E_ARG;
   return SSS_OK;
 }
+// a request has no more tokens than the call, whatever bound the caller knows
+int32_t bound_q(int32_t max_q, int64_t tokens) {
+  return max_q < tokens ? max_q : static_cast<int32_t>(tokens);
+}
 }  // namespace
 
 size_t sss_attention_workspace_bytes(int64_t tokens, int32_t heads, const sss_kv_cache_t* cache,
                                      int32_t batch, int32_t max_q, int64_t max_kv) {
   if (check_attention(tokens, heads, cache, batch, max_q, max_kv) != SSS_OK) return 0;
   if (tokens == 0 || batch == 0 || max_q == 0) return 0;
+  max_q = bound_q(max_q, tokens);
   return plan_attention(tokens, heads, *cache, batch, max_q, max_kv).ws_bytes;
 }
 
@@ -582,6 +587,7 @@ sss_status_t sss_attention(const void* q, int64_t q_stride, int32_t heads,
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(cu_q, 4) || !aligned(kv_len, 4) ||
       !aligned(block_table, 4) || !aligned(dev_status, 4) || !aligned(workspace, 16))
     return SSS_E_ALIGN;
+  max_q = bound_q(max_q, tokens);
   const AttnPlan p = plan_attention(tokens, heads, *cache, batch, max_q, max_kv);
   if (p.ws_bytes > 0 && (workspace == nullptr || ws_bytes < p.ws_bytes)) return SSS_E_WORKSPACE;
   return finish("sss_attention",

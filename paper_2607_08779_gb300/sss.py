@@ -862,6 +862,7 @@ def sss_qk_norm_rope(q, k, v, rope: Rope, positions, cache: KVCache, slots=None,
 def sss_attention_workspace_bytes(tokens: int, heads: int, cache: KVCache, batch: int, max_q: int,
                                   max_kv: int) -> int:
     """Workspace bytes of sss_attention with these sizes."""
+    max_q = min(max_q, tokens)  # (any bound will do: no request has more)
     return int(load().sss_attention_workspace_bytes(tokens, heads, cache._ref, batch, max_q,
                                                     max_kv))
 
@@ -891,6 +892,7 @@ def sss_attention(q, cache: KVCache, cu_q, kv_len, max_q: int, max_kv: int, bloc
     batch = cu_q.numel() - 1
     if q.dtype is not cache.k.dtype:
         raise SssError(fn, 1, f"q must be {cache.k.dtype}, as the cache")
+    max_q = min(max_q, tokens)  # (any bound will do: no request has more)
     qs = _rows(fn, "q", q, tokens, heads * dim)
     if out is None:
         out = _empty_on(stream, (tokens, heads, dim), q.dtype, q.device)
