@@ -78,8 +78,8 @@ typedef enum {
                                    inf or NaN                                         */
 #define SSS_FLAG_TIMEOUT 0x4u   /* a bounded pipeline wait of sss_gemm (or
                                    sss_gemm_noalloc), sss_quantize,
-                                   sss_quantize_rotated or sss_attention (of many
-                                   rows) expired; the output is incomplete                                         */
+                                   sss_quantize_rotated or sss_attention expired; the
+                                   output is incomplete                               */
 #define SSS_FLAG_INDEX 0x8u     /* sss_page_plan, sss_qk_norm_rope, sss_attention: a length,
                                    position, slot or page lies outside what the call's
                                    arguments allow; what the calls do then is said there */
@@ -602,8 +602,8 @@ size_t sss_gemm_noalloc_max_scratch_bytes(void);
  * sss_test_set_stall -- test hook for the bounded waits; the paper has no
  * counterpart.  While a bit below is set, every later launch of that kernel
  * family leaves one mbarrier one arrive short: the GEMM on the first
- * stage's weight tile, the attention of many rows on its first value tile.  The
- * decode GEMV kernels (batch 1 and batched) have no data-dependent waits (their
+ * stage's weight tile, the attention of many rows on its first value tile (of few
+ * rows whose keys are split: on what a CTA's peers store into it).  The decode GEMV kernels (batch 1 and batched) have no data-dependent waits (their
  * warps meet only at CTA-wide barriers), so their bits have no effect.  The wait
  * on that barrier then runs out after its bound (about one second), the kernel
  * raises SSS_FLAG_TIMEOUT in dev_status, lets its own copies and MMAs in flight
@@ -617,6 +617,8 @@ size_t sss_gemm_noalloc_max_scratch_bytes(void);
 #define SSS_TEST_STALL_GEMM 0x4u       /* gemm_kernel (sss_gemm, sss_gemm_noalloc)             */
 #define SSS_TEST_STALL_ATTENTION 0x8u  /* attn_prompt_kernel (sss_attention of many rows): the
                                           first value tile is never handed on              */
+#define SSS_TEST_STALL_ATTENTION_ROWS 0x10u /* attn_rows_kernel (of few rows), where keys are
+                                          split: each CTA expects 16 bytes too many        */
 void sss_test_set_stall(uint32_t mask);
 
 #ifdef __cplusplus

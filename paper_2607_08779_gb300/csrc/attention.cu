@@ -112,7 +112,8 @@ cudaError_t launch_attention(const AttnPlan& p, const void* q, int64_t q_stride,
   a.nsplit = static_cast<int>(p.nsplit);
   a.rows = p.rows;
   a.scale_log2 = scale * 1.4426950408889634f;
-  a.stall = (test_stall_mask() & SSS_TEST_STALL_ATTENTION) ? 1 : 0;
+  const uint32_t stall = p.prompt ? SSS_TEST_STALL_ATTENTION : SSS_TEST_STALL_ATTENTION_ROWS;
+  a.stall = (test_stall_mask() & stall) ? 1 : 0;
   cudaError_t e = p.prompt ? launch_attn_prompt(a, c.dtype, c.dim, stream)
                            : launch_attn_rows(a, c.dtype, c.dim, stream);
   if (e == cudaSuccess && p.join) e = launch_attn_join(a, c.dtype, c.dim, stream);

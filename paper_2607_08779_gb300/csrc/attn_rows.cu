@@ -16,7 +16,11 @@
 // split over the CTAs of a cluster, 64 at a time in turn, which join their outputs through
 // distributed shared memory: no second kernel, no workspace, and a fixed order.  The
 // stores into a peer are counted by a barrier there (a cluster-wide barrier after plain
-// ones took 0.2 to 0.4 us longer).
+// ones took 0.2 to 0.4 us longer).  That wait is bounded (about one second): on expiry the
+// CTA raises SSS_FLAG_TIMEOUT.  No CTA leaves its shared memory before all of the cluster
+// have issued their stores (a second cluster barrier, arrived at behind the stores and
+// waited for at the very end, when as a rule all have), and one whose wait ran out first lets
+// those that are under way land.
 //
 // Measured (32 heads of 128 over 8, bf16): 64 requests of 12000 to 16384 keys 530 us, 7.0
 // TB/s, above the copy rate; 16 ragged ones of 130 to 16384 (64 heads) 59.6 us, 84 % of
@@ -430,7 +434,8 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     if (threadIdx.x == 0) {  // from each split this one's pieces and their rows' sums
       const int end = min(z * per + per, rows * PIECES);
       const int bytes = (end - z * per) * 16 + ((end - 1) / PIECES - z * per / PIECES + 1) * 4;
-      if (z < n) mbar_arrive_expect_tx(&arrived, z * per < end ? n * bytes : 0);
+      // (the test hook: 16 bytes that nobody stores)
+      if (z < n) mbar_arrive_expect_tx(&arrived, (z * per < end ? n * bytes : 0) + (a.stall ? 16 : 0));
     }
     __syncwarp();
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -473,15 +478,17 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
   }
   if constexpr (CL) {
     if (alone) return leave();
-    if (z >= n) return;
-    int abort = 0;
-    if (!mbar_wait(&arrived, 0, &abort)) {
-      if (a.status && lane == 0) atomicOr(a.status, SSS_FLAG_TIMEOUT);
-      return;
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    bool ok = z < n;  // this CTA has pieces to join
+    if (ok) {
+      int abort = 0;
+      ok = __all_sync(0xffffffffu, mbar_wait(&arrived, 0, &abort));
+      if (!ok && a.status && lane == 0) atomicOr(a.status, SSS_FLAG_TIMEOUT);
     }
     // a lane per split and piece (a cluster is a power of two)
     const int cl = a.nsplit, w = threadIdx.x & (cl - 1);
-    for (int y0 = 0; y0 < per; y0 += kThreads / cl) {
+    for (int y0 = 0; ok && y0 < per; y0 += kThreads / cl) {
       const int y = y0 + threadIdx.x / cl, x = z * per + y, row = x / PIECES, d = 4 * (x % PIECES);
       const int i = token_of(row), g = row - i * a.hpt;
       const bool in = y < per && row < rows;
@@ -506,6 +513,12 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
       const int64_t at = static_cast<int64_t>(rq.q0 + i0 + i) * a.heads + kh * a.group + g0 + g;
       const uint2 u = make_uint2(Pair<T>::pack(v.x * r, v.y * r), Pair<T>::pack(v.z * r, v.w * r));
       *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (z < n && !ok) {
+      int drain = 0;
+      (void)mbar_wait(&arrived, 0, &drain);
     }
   }
 }

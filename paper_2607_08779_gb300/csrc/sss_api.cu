@@ -155,7 +155,7 @@ const char* sss_last_error(void) { return g_last_error; }
 
 void sss_test_set_stall(uint32_t mask) {
   g_test_stall.store(mask & (SSS_TEST_STALL_GEMV | SSS_TEST_STALL_GEMV_BATCH | SSS_TEST_STALL_GEMM |
-                             SSS_TEST_STALL_ATTENTION),
+                             SSS_TEST_STALL_ATTENTION | SSS_TEST_STALL_ATTENTION_ROWS),
                      std::memory_order_relaxed);
 }
 

@@ -59,6 +59,7 @@ TEST_STALL_GEMV = 0x1
 TEST_STALL_GEMV_BATCH = 0x2
 TEST_STALL_GEMM = 0x4
 TEST_STALL_ATTENTION = 0x8
+TEST_STALL_ATTENTION_ROWS = 0x10
 
 
 class SssError(RuntimeError):
