@@ -531,7 +531,7 @@ sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, in
  *   max_q, max_kv [in] bounds of a request's new tokens and keys; what is near
  *                     them is faster.  max_q may be any (above `tokens` it counts as
  *                     that), max_kv at most 2^30 - 1.
- *   scale       [in]  > 0, finite.
+ *   scale       [in]  > 0, at most 2.3e38.
  *   out         [out] device [tokens][heads][dim] of the cache's dtype, dense,
  *                     16-byte aligned (bf16: the x_bf16 of the o_proj).
  *   workspace   [in]  device scratch of ws_bytes >=

@@ -575,7 +575,8 @@ sss_status_t sss_attention(const void* q, int64_t q_stride, int32_t heads,
                            void* workspace, size_t ws_bytes, uint32_t* dev_status, void* stream) {
   sss_status_t st = check_attention(tokens, heads, cache, batch, max_q, max_kv);
   if (st != SSS_OK) return st;
-  if (!(scale > 0.0f) || !(scale <= 3.0e38f)) return SSS_E_ARG;
+  // (the kernels take powers of two: scale * log2(e) has to be finite as well)
+  if (!(scale > 0.0f) || !(scale <= 2.3e38f)) return SSS_E_ARG;
   if (q_stride < static_cast<int64_t>(heads) * cache->dim || q_stride > kMaxDim ||
       q_stride % 8 != 0)
     return SSS_E_ARG;

@@ -5,7 +5,7 @@ import ctypes
 import pytest
 
 from paper_2607_08779_gb300 import sss
-from test_attention_abi import cache
+from test_attention_abi import attention, cache
 
 NONE = 2 ** 31 - 1  # "no bound"
 
@@ -31,3 +31,8 @@ def test_bounds_past_int32_from_python():
     assert size(64) > 0
     for n in (2 ** 31, 2 ** 32 + 1, 2 ** 40):
         assert size(n) == size(64)
+
+
+@pytest.mark.parametrize("scale,want", [(1e-38, 0), (1e30, 0), (2.2e38, 0), (2.4e38, 1), (2.9e38, 1), (3.4e38, 1)])
+def test_scales_whose_product_with_log2_e_is_not_finite(scale, want):
+    assert attention(scale=scale) == want
