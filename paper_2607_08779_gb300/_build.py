@@ -1,5 +1,6 @@
 """Build the CUDA library libsss.so in-tree with nvcc (sm_103a only), and with g++
-_binding.so, the compiled part of the Python binding.
+_binding.so, the compiled part of the Python binding.  The library needs nvcc alone;
+the binding is built apart from it, for the torch and Python that will load it.
 
 Each translation unit under csrc/ is compiled in parallel to an object file
 under _build/, then linked into paper_2607_08779_gb300/libsss.so.  The CUDA
@@ -21,6 +22,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libsss.so")
 BINDING_SRC = os.path.join(CSRC, "binding.cpp")
 BINDING = os.path.join(PKG, "_binding.so")
+STAMP = os.path.join(BUILD, "binding.stamp")  # what _binding.so was built for
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
@@ -40,25 +42,51 @@ def sources():
 
 def _deps():
     files = sources() + [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")]
-    files.append(BINDING_SRC)
-    files.append(os.path.join(INCLUDE, "sss.h"))
-    files.append(os.path.abspath(__file__))
-    return files
+    return files + _common_deps()
+
+
+def _common_deps():
+    return [os.path.join(INCLUDE, "sss.h"), os.path.abspath(__file__)]
+
+
+def _newer(target, files) -> bool:
+    if not os.path.exists(target):
+        return False
+    t = os.path.getmtime(target)
+    return all(os.path.getmtime(f) <= t for f in files)
 
 
 def up_to_date() -> bool:
-    if not (os.path.exists(LIB) and os.path.exists(BINDING)):
+    return _newer(LIB, _deps())
+
+
+def _stamp() -> str:
+    import platform
+    import sys
+
+    import torch
+
+    return "\n".join((torch.__version__, torch.__file__, sys.version, platform.machine()))
+
+
+def binding_up_to_date() -> bool:
+    """Whether _binding.so is there, newer than its sources, and built for this
+    interpreter and the torch that it imports."""
+    if not _newer(BINDING, [BINDING_SRC] + _common_deps()) or not os.path.exists(STAMP):
         return False
-    t = min(os.path.getmtime(LIB), os.path.getmtime(BINDING))
-    return all(os.path.getmtime(f) <= t for f in _deps())
+    with open(STAMP) as f:
+        return f.read() == _stamp()
 
 
-def build_binding() -> None:
+def build_binding(force: bool = False) -> str:
     """_binding.so, against the torch that this interpreter imports."""
     import sysconfig
 
     import torch
 
+    if not force and binding_up_to_date():
+        return BINDING
+    os.makedirs(BUILD, exist_ok=True)
     home = os.path.dirname(torch.__file__)
     cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc()))), "include")
     include = [INCLUDE, os.path.join(home, "include"),
@@ -74,6 +102,11 @@ def build_binding() -> None:
     if r.returncode != 0:
         raise RuntimeError(f"g++ failed for {BINDING_SRC}:\n{r.stderr}")
     os.replace(tmp, BINDING)
+    tmp = STAMP + f".tmp{os.getpid()}"
+    with open(tmp, "w") as f:
+        f.write(_stamp())
+    os.replace(tmp, STAMP)
+    return BINDING
 
 
 def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
@@ -93,10 +126,8 @@ def build(force: bool = False, verbose: bool = False, extra_flags=()) -> str:
         return obj
 
     srcs = sources()
-    with cf.ThreadPoolExecutor(max_workers=min(len(srcs) + 1, os.cpu_count() or 4)) as ex:
-        binding = ex.submit(build_binding)
+    with cf.ThreadPoolExecutor(max_workers=min(len(srcs), os.cpu_count() or 4)) as ex:
         objs = list(ex.map(compile_one, srcs))
-        binding.result()
     tmp = LIB + f".tmp{os.getpid()}"
     cmd = [cc, *ARCH, "-shared", "-Xcompiler", "-fPIC", "-o", tmp, *objs,
            "-cudart", "static"]

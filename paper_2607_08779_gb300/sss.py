@@ -8,7 +8,9 @@ The calls go through ctypes.  Those that a decoding step makes for every layer
 (sss_page_plan, sss_qk_norm_rope, sss_attention) check and pass their usual
 arguments in compiled code (_binding.so, csrc/binding.cpp), which leaves to the
 Python below whatever it does not take, refusals among it: 3 us a call, 9 to 11
-without.
+without.  Where that part cannot be built (it needs g++ and Python's headers, the
+library nvcc alone) these calls go through ctypes too, to the same kernels, and a
+warning says so once.
 """
 from __future__ import annotations
 
@@ -196,25 +198,48 @@ def load(build_if_needed: bool = True):
 _fast = None
 
 
+class _NoBinding:
+    """In place of the compiled part: takes no call, so that each goes through ctypes."""
+
+    @staticmethod
+    def page_plan(*_):
+        return -1
+
+    qk_norm_rope = attention = page_plan
+
+
+def _load_binding():
+    import importlib.machinery
+    import importlib.util
+
+    import torch  # noqa: F401  (its libraries come first)
+
+    loader = importlib.machinery.ExtensionFileLoader("_binding", _build.build_binding())
+    spec = importlib.util.spec_from_loader("_binding", loader)
+    m = importlib.util.module_from_spec(spec)
+    loader.exec_module(m)
+    return m
+
+
 def _binding():
     """The compiled part of the binding: it checks and makes the attention step's
     calls that are in order."""
     global _fast
     if _fast is None:
-        import importlib.machinery
-        import importlib.util
-
-        import torch  # noqa: F401  (its libraries come first)
-
         L = load()
         with _lock:
             if _fast is None:
-                loader = importlib.machinery.ExtensionFileLoader("_binding", _build.BINDING)
-                spec = importlib.util.spec_from_loader("_binding", loader)
-                m = importlib.util.module_from_spec(spec)
-                loader.exec_module(m)
-                m.init(*[ctypes.cast(f, ctypes.c_void_p).value
-                         for f in (L.sss_page_plan, L.sss_qk_norm_rope, L.sss_attention)])
+                try:
+                    m = _load_binding()
+                except (RuntimeError, ImportError, OSError) as e:
+                    import warnings
+
+                    warnings.warn("the attention step's calls go through ctypes, 6 to 8 us slower each: "
+                                  f"{_build.BINDING} cannot be built or loaded: {e}", RuntimeWarning)
+                    m = _NoBinding
+                else:
+                    m.init(*[ctypes.cast(f, ctypes.c_void_p).value
+                             for f in (L.sss_page_plan, L.sss_qk_norm_rope, L.sss_attention)])
                 _fast = m
     return _fast
 
