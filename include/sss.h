@@ -432,12 +432,13 @@ typedef struct {
  *                      others left alone.
  *   cu_q         [out] device int32 [batch + 1]: the first token of each request
  *                      among the step's, and their number.
- *   kv_len       [out] device int32 [batch]: past + fresh.
+ *   kv_len       [out] device int32 [batch]: past + fresh (of the tokens that cu_q has).
  *   positions    [out] device int32 [tokens]: each new token's position.
  *   slots        [out] device int32 [tokens]: its slot.  Rows past the step's
  *                      tokens get position 0 and slot -1 (a buffer may be larger
  *                      than the step, as in a captured graph).
- *   used         [out] device int32: how many of free_pages were taken.
+ *   used         [out] device int32: how many of free_pages were taken (also for tokens
+ *                      that are past `tokens` or past the table's columns).
  *   dev_status   [out] nullable.  SSS_FLAG_PAGES: free pages or table columns do
  *                      not suffice; the tokens without a page get slot -1 (and
  *                      the table -1).  SSS_FLAG_INDEX: a length is negative

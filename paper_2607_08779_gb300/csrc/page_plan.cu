@@ -89,9 +89,11 @@ __global__ void __launch_bounds__(kThreads) page_plan_kernel(const PlanArgs a) {
     past_of[tid] = static_cast<int>(past);
     if (tid == 0) first_token[kThreads] = tokens0;
     if (writer && b < a.batch) {
-      // (never past the buffers of a token's row, whatever the lengths say)
-      a.cu_q[b] = static_cast<int32_t>(min(t0 + ts - fresh, a.tokens));
-      a.kv_len[b] = static_cast<int32_t>(past + fresh);
+      // (never past the buffers of a token's row, whatever the lengths say: a request that
+      // they cut has the keys of the tokens that are left)
+      const int64_t from = min(t0 + ts - fresh, a.tokens), to = min(t0 + ts, a.tokens);
+      a.cu_q[b] = static_cast<int32_t>(from);
+      a.kv_len[b] = static_cast<int32_t>(past + to - from);
     }
     __syncthreads();
     const int64_t begin = first_token[0], end = min(tokens0, a.tokens);
