@@ -544,7 +544,8 @@ sss_status_t sss_qk_norm_rope(const void* q, int64_t q_stride, const void* k, in
  *                     the request's own rows, a page that is none reads as zeros).
  *                     SSS_FLAG_TIMEOUT: a bounded wait ran out.
  * The result does not depend on timing, and a request's not on the others in the
- * batch but through max_q, max_kv and their number, by which the work is split.
+ * batch but through `tokens`, max_q, max_kv and their number, by which the work is
+ * split (a split changes the order of the sums, so the last bits).
  * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim; a driver without tensor maps),
  * SSS_E_ALIGN, SSS_E_WORKSPACE, SSS_E_CUDA.
  */

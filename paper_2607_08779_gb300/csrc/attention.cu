@@ -59,9 +59,9 @@ AttnPlan plan_attention(int64_t tokens, int heads, const sss_kv_cache_t& c, int 
     return p;
   }
   // Few rows: a cluster of as many CTAs as run at a time (two an SM, and whole
-  // clusters in a cluster of SMs: 8 of 16 CTAs, 32 of 8), while half as many would have
-  // more than 128 keys each (one request of 500 keys: 5.8 us in pairs, 4.8 in fours; of
-  // 900: 5.8 in fours, 4.9 in eights).  A second wave costs more than it evens out (24
+  // clusters in a cluster of SMs: 8 of 16 CTAs, 32 of 8), halved until all of them but one
+  // have 128 keys: 2 above 128 keys, 4 above 384, 8 above 896, 16 above 1920 (one request of
+  // 500 keys: 5.8 us in pairs, 4.8 in fours; of 900: 5.8 in fours, 4.9 in eights).  A second wave costs more than it evens out (24
   // requests of 150 to 1200 keys: 15.7 us whole, 17.5 in pairs; 32 of 256 to 2000: 24.6 in
   // pairs, 31.2 in fours), but where keys are many (20 requests of 400 to 3000: 30.6 us
   // whole, 23.0 in pairs; 16 of 130 to 16384: 89 us in pairs, 59 in fours; 64 of 12000 to

@@ -39,20 +39,28 @@
 // say: the others hold the next request's queries, or what shared memory happened to
 // hold, and a request's result must not depend on either.
 //
+// p is rounded to the cache's type, the tensor core's operand (both operands of a product
+// are of one type, and values are read as the cache holds them); the row's sum is that of
+// p in fp32, taken as the exponentials come, where a sum of the rounded ones would unpack
+// them again in the step's longest chain.  Error against 64 bits, of the output's norm:
+// 1.9e-3 to 2.3e-3 in bf16, 2.5e-4 to 2.9e-4 in fp16 (rounded once at the end: 1.6e-3,
+// 2.1e-4).
+//
 // A value that is infinite or NaN must not reach rows that do not see its key (0 x
 // NaN would).  In tiles that every row of the CTA sees it cannot do harm; in the others
 // warps 12-15 replace it by zero and note the first key of each kind for its
 // column, and the rows that see that key add it at the end.
 //
-// Measured: 8192 tokens of 32 heads of 128 over 8 key/value heads, bf16: 325 us, 1.69
-// PFLOP/s of what the causal rows need, 89 % of the measured bf16 rate (at 1.91 GHz).  A
+// Measured: 8192 tokens of 32 heads of 128 over 8 key/value heads, bf16: 353 us in a
+// stream, 1.56 PFLOP/s of what the causal rows need, 82 % of the measured bf16 rate; a few
+// calls alone, before the power cap lowers the clock (at 1.91 GHz), 324 us, 1.70 PFLOP/s.  A
 // step of both row tiles takes about 2600 cycles where its products take 2048: a row
 // tile's softmax is a chain of about 1300 (read the scores, the maximum, 128
 // exponentials, write p), longer than the other tile's products that cover it.  10
-// ragged prompts: 86 us, 2.1 times their products' time: an item's end and start cost
+// ragged prompts: 84 us, 2.1 times their products' time: an item's end and start cost
 // 4100 to 6000 cycles, against 1 to 16 steps, and a tile of which rows see a part 1000
 // more; this code runs once an item, a quarter of it waiting for instructions.  512
-// tokens: 11.6 us, 4.6 of them up to the first scores, then four steps in a row.
+// tokens: 11.7 us, 4.6 of them up to the first scores, then four steps in a row.
 // Other divisions of the work that were slower at 8192 tokens: an issuing warp per row
 // tile (426 us free-running, 342 in turns), two threads to a row (357), p handed over
 // in halves (437), outputs written by warps of their own (339; ragged 106) or straight from

@@ -22,9 +22,9 @@
 // waited for at the very end, when as a rule all have), and one whose wait ran out first lets
 // those that are under way land.
 //
-// Measured (32 heads of 128 over 8, bf16): 64 requests of 12000 to 16384 keys 530 us, 7.0
-// TB/s, above the copy rate; 16 ragged ones of 130 to 16384 (64 heads) 59.6 us, 84 % of
-// it, the longest request's cluster being last; one request of 2047 keys 5.8 us, the
+// Measured (32 heads of 128 over 8, bf16): 64 requests of 12000 to 16384 keys 517 to 530
+// us, 7.0 TB/s, above the copy rate; 16 ragged ones of 130 to 16384 (64 heads) 59.3 us, 85 %
+// of it, the longest request's cluster being last; one request of 2047 keys 5.9 us, the
 // launch, the lengths' and the first keys' latency and the join.  A ring of two or four
 // steps (at 16 rows), and three CTAs an SM, were slower on the whole; so was dividing all
 // requests' keys evenly over the SMs with a second kernel to join (64 against 59, 558
@@ -117,7 +117,9 @@ __device__ __forceinline__ void peer_store(uint32_t addr, float4 v, uint32_t bar
       : "memory");
 }
 
-// MT tiles of 16 rows.  CL: the splits of a tile's keys are the CTAs of a cluster, whose
+// (Two CTAs an SM are 255 registers a thread at most.  16 rows need 160 to 247; 32 rows of
+// 64 values 226 or 230; 32 rows of 128 spill 148 or 172 bytes, which costs less than one
+// CTA an SM: see RowsSmem.)  MT tiles of 16 rows.  CL: the splits of a tile's keys are the CTAs of a cluster, whose
 // keys differ in number by 64 at most, and join through its shared memory: each adds up a
 // share of the values (16 bytes at a time), and all store their partial results there.
 template <typename T, int D, int MT, bool CL>

@@ -12,9 +12,10 @@
 // another.  So the rotation needs no exchange between lanes, and the norm a sum over
 // the head's lanes only.  A warp takes a run of a token's heads, two groups of them at
 // a time with the next two's loads in flight, and keeps the token's cosines and sines
-// in registers.  8191 tokens of 64 + 16 heads of 128: 88.5 us, 5.7 TB/s, 86 % of the
-// copy rate (four lanes' worth of exchange per value and no loads ahead: 110 us; more
-// heads at a time or fewer registers: 91 to 104 us).
+// in registers.  8191 tokens of 64 + 16 heads of 128: 90 us, 5.6
+// TB/s, 84 % of the copy rate (four lanes' worth of exchange per value and no loads ahead:
+// 110 us; more heads at a time: 91 to 104 us).  Of 16-bit inputs 116 us, 2.9 TB/s: a lane
+// then loads 8 bytes at a time, and the loads ahead are half as many bytes.
 #include <algorithm>
 
 #include "sss_internal.cuh"
@@ -23,7 +24,8 @@ namespace sss {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kCtas = 7;    // per SM: 72 registers a thread hold the loads ahead
+constexpr int kCtas = 7;    // per SM: 72 registers a thread hold the loads ahead (8 bytes
+                            // spill; more CTAs with fewer registers: 91 to 131 us)
 constexpr int kUnroll = 2;
 
 struct RopeArgs {
