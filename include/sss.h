@@ -565,6 +565,168 @@ size_t sss_attention_workspace_bytes(int64_t tokens, int32_t heads,
                                      const sss_kv_cache_t* cache, int32_t batch,
                                      int32_t max_q, int64_t max_kv);
 
+/*
+ * The same cache in 4 bits: keys and values on the signed symmetric grid of the
+ * weights (eq:signed_sym_quant, eq:sign_rule), in groups of 32 consecutive values of a
+ * head: M = max |x|, s = -M/8 where the dominant value is positive, else M/8 (so it lands
+ * on the code -8), c = clip(RNE(x / s), -8, 7) of the exact quotient.  The value that is
+ * held is fp16(s) c.  9/16 of a byte a value against 2: a decode step reads its keys and
+ * values 3.6 times as fast.
+ *
+ * Pages are as above.  A page holds, per key/value head, page_size / 16 blocks of 16
+ * slots; a block is 18 * dim bytes that lie together (one bulk copy brings a block):
+ * the 16 keys' codes (8 * dim bytes, dim / 2 to a slot), their scales (fp16, dim / 32 to a
+ * slot), then the values' codes and scales.  With W = dim / 8 words of 32 bits to a slot's
+ * codes, word w holds as its nibble n = a + 4 h (the lowest is 0) the stored code c + 8
+ * of dimension 2 W a + W h + w.  The values' words of slots whose number has bit 1 set
+ * have their halves swapped where dim is 128 (word w lies at w ^ 8).
+ */
+typedef struct {
+  void* blocks;        /* [pages][heads][page_size / 16][18 * dim] bytes, 16-byte aligned  */
+  int64_t pages;       /* 0 .. 2^31 / page_size - 1                                        */
+  int64_t page_stride; /* bytes from a page to the next: at least heads * page_size / 16 *
+                          18 * dim, a multiple of 16                                       */
+  int32_t page_size;   /* 16, 32, 64, 128 or 256                                           */
+  int32_t heads;       /* key/value heads, 1 ..                                            */
+  int32_t dim;         /* 64 or 128                                                        */
+  int32_t reserved;    /* must be 0                                                        */
+} sss_kv_cache_q4_t;
+
+/*
+ * sss_kv_store_q4 -- keys and values into the cache, in 4 bits (of sss_qk_norm_rope, say,
+ * whose packed output the prompt attends to at full precision).
+ *   k, v       [in]  device [tokens][heads * dim] of in_dtype (sss_dtype_t), rows k_stride
+ *                    and v_stride elements apart (multiples of 8; fp32: of 4); 16-byte
+ *                    aligned.
+ *   slots      [in]  device int32 [tokens], no two alike; negative: the token is not kept.
+ *                    NULL: token t's slot is t.
+ *   dev_status [out] nullable.  SSS_FLAG_NONFINITE: a group holds an infinity or NaN; it is
+ *                    stored as zeros.  SSS_FLAG_RANGE: a scale is 65520 or more and
+ *                    stored as 65504.  SSS_FLAG_INDEX: a slot past the cache (not written).
+ * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim), SSS_E_ALIGN, SSS_E_CUDA.
+ */
+sss_status_t sss_kv_store_q4(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                             int32_t in_dtype, int64_t tokens, const sss_kv_cache_q4_t* cache,
+                             const int32_t* slots, uint32_t* dev_status, void* stream);
+
+/*
+ * sss_kv_fetch_q4 -- what the cache holds in the given slots, any number of times each:
+ * fp16(s) c, exact in fp32, rounded once to a 16-bit out_dtype.
+ *   slots      [in]  device int32 [count]; negative: the row is zeros.  NULL: row t is
+ *                    slot t.
+ *   k, v       [out] nullable device [count][heads][dim] of out_dtype, 16-byte aligned.
+ *   dev_status [out] nullable.  SSS_FLAG_INDEX: a slot past the cache (zeros).
+ * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim), SSS_E_ALIGN, SSS_E_CUDA.
+ */
+sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slots, int64_t count,
+                             void* k, void* v, int32_t out_dtype, uint32_t* dev_status,
+                             void* stream);
+
+/*
+ * sss_attention_q4 -- sss_attention over the cache in 4 bits: the same requests, rows,
+ * bounds and flags, always with a block table (so with kv_len).  The new tokens' own keys
+ * and values are in the cache, as the others are.
+ *   dtype [in]  of q and out: SSS_OUT_F16 or SSS_OUT_BF16.
+ * A request's tokens times the heads of a group at most 32 (or single tokens): scores are
+ * sums of q times the codes, scaled in fp32; p_ij times the value's scale is rounded to
+ * fp16 (at most 2^-25 off where it is below fp16's normal range; a row's largest p_ij is
+ * 1).  More: the keys and values are first written to the workspace as 16-bit
+ * values of `dtype`, fp16(s) c rounded once (fp16 cannot hold those of 65520 and more, which
+ * only bf16 or fp32 inputs can have left in the cache).
+ * Errors: as sss_attention; SSS_E_UNSUPPORTED also where that copy of the cache would have
+ * 2^31 slots or more.
+ */
+sss_status_t sss_attention_q4(const void* q, int64_t q_stride, int32_t heads, int32_t dtype,
+                              const sss_kv_cache_q4_t* cache, const int32_t* cu_q,
+                              const int32_t* kv_len, const int32_t* block_table,
+                              int32_t table_width, int32_t batch, int64_t tokens, int32_t max_q,
+                              int64_t max_kv, float scale, void* out, void* workspace,
+                              size_t ws_bytes, uint32_t* dev_status, void* stream);
+
+/* Workspace bytes of that call (0 for invalid arguments, or if none are needed). */
+size_t sss_attention_q4_workspace_bytes(int64_t tokens, int32_t heads,
+                                        const sss_kv_cache_q4_t* cache, int32_t table_width,
+                                        int32_t batch, int32_t max_q, int64_t max_kv);
+
+/*
+ * What else a serving loop does with pages, of either cache: the block table says all that
+ * there is to know of them, and several of its rows may hold the same page.
+ *
+ * sss_page_fork -- the rows of a new block table from those of the old one: beams or
+ * samples that go on from their parents.  Row r takes over the pages of past[p] tokens of
+ * p = parents[r].  Full pages are shared.  A last page that is only partly filled is
+ * written to by the tokens that follow: the first row with that parent keeps it, each
+ * other one gets a free page in its place (from the front of free_pages, rows in order)
+ * and the entry (src[r], dst[r]) for sss_page_copy.  Pages of rows that nobody takes over are
+ * found by sss_page_reclaim on the new table.
+ *   parents      [in]  device int32 [rows]; negative: the row is empty.
+ *   past         [in]  device int32 [batch].
+ *   block_table  [in]  device int32 [batch][table_width].
+ *   new_table    [out] device int32 [rows][table_width], not block_table itself: all of
+ *                      it is written, -1 behind a row's pages.
+ *   new_past     [out] device int32 [rows], not past itself.
+ *   src, dst     [out] device int32 [rows]: -1 where nothing is to be copied.
+ *   used         [out] device int32: how many of free_pages were taken.
+ *   dev_status   [out] nullable.  SSS_FLAG_PAGES: free pages do not suffice (an entry of -1
+ *                      is none): the row ends with its last full page, new_past says so.
+ *                      SSS_FLAG_INDEX: a parent past the batch (the row is empty), a
+ *                      negative length (taken as 0), one that the table's columns do not
+ *                      hold (cut to them), or a last page to copy that is none (the row ends
+ *                      before it).
+ * Errors: SSS_E_ARG, SSS_E_ALIGN, SSS_E_CUDA.
+ */
+sss_status_t sss_page_fork(const int32_t* parents, int32_t rows, const int32_t* past,
+                           int32_t batch, int32_t page_size, const int32_t* free_pages,
+                           int32_t free_count, const int32_t* block_table, int32_t table_width,
+                           int32_t* new_table, int32_t* new_past, int32_t* src, int32_t* dst,
+                           int32_t* used, uint32_t* dev_status, void* stream);
+
+/*
+ * sss_page_reclaim -- the free pages, from the block table: those of 0 .. pages - 1 that no
+ * row holds among its first ceil(past / page_size) entries, in ascending order (so pages of
+ * requests that ended, or whose length was cut, are free again, and shared ones once the
+ * last row has let go of them).
+ * With `moves` it compacts as well: the i-th lowest free page takes the i-th highest held
+ * one, while that is the higher and i < most_moves.  src and dst get the moves for
+ * sss_page_copy, new_table the held entries after them, free_pages what is then free.
+ *   past         [in]  device int32 [batch].
+ *   block_table  [in]  device int32 [batch][table_width].
+ *   pages        [in]  of the cache, 0 .. 2^20.
+ *   free_pages   [out] device int32 [pages]: -1 behind the free ones (as sss_page_plan
+ *                      and sss_page_fork take it whole).
+ *   free_count   [out] device int32.
+ *   new_table    [out] device int32 [batch][table_width] (with moves): only held entries
+ *                      are written; may be block_table itself.
+ *   src, dst     [out] device int32 [most_moves] (with moves): -1 behind them.
+ *   moves        [out] nullable device int32: their number.
+ *   dev_status   [out] nullable.  SSS_FLAG_INDEX: a length is negative (taken as 0) or past
+ *                      the table's columns (cut to them), or a held entry is no page (left
+ *                      as it is).
+ * Errors: SSS_E_ARG, SSS_E_ALIGN, SSS_E_CUDA.
+ */
+sss_status_t sss_page_reclaim(const int32_t* block_table, int32_t table_width,
+                              const int32_t* past, int32_t batch, int32_t page_size,
+                              int32_t pages, int32_t* free_pages, int32_t* free_count,
+                              int32_t* new_table, int32_t* src, int32_t* dst, int32_t most_moves,
+                              int32_t* moves, uint32_t* dev_status, void* stream);
+
+/*
+ * sss_page_copy, sss_page_copy_q4 -- page src[i] to page dst[i] in each of the caches (the
+ * layers of a model), keys and values, as they are.
+ *   caches     [in]  host array of `count` descriptors, 0 .. 128; not retained.  All have the
+ *                    same page_size, heads, dim and number of pages (slots / page_size).
+ *   src, dst   [in]  device int32 [n].  Both negative: no copy.  No page is the destination
+ *                    of two copies, nor the source of one and the destination of another.
+ *   dev_status [out] nullable.  SSS_FLAG_INDEX: only one of the two is negative, or one is
+ *                    past the cache (not copied).
+ * Errors: SSS_E_ARG, SSS_E_UNSUPPORTED (dim), SSS_E_ALIGN, SSS_E_CUDA.
+ */
+sss_status_t sss_page_copy(const sss_kv_cache_t* const* caches, int32_t count, const int32_t* src,
+                           const int32_t* dst, int32_t n, uint32_t* dev_status, void* stream);
+sss_status_t sss_page_copy_q4(const sss_kv_cache_q4_t* const* caches, int32_t count,
+                              const int32_t* src, const int32_t* dst, int32_t n,
+                              uint32_t* dev_status, void* stream);
+
 #define SSS_OP_GEMV 0
 #define SSS_OP_GEMM 1
 /* Workspace bytes sss_gemv (op SSS_OP_GEMV, m_or_batch = batch) or sss_gemm

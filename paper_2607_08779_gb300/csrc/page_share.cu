@@ -1,0 +1,486 @@
+// page_share.cu -- pages that several rows of a block table hold: forking rows, finding
+// the free pages again (and moving held ones down), and copying pages.
+//
+// Nothing keeps counts of a page's holders: the table says who holds what.  Forking reads
+// rows and writes rows; the free pages are those that no row names.  So a request ends, a
+// beam is dropped or a length cut by changing the table's rows and lengths alone.
+#include <algorithm>
+
+#include "kv_q4.cuh"
+
+namespace sss {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Fork.  Row r takes the pages of past[p] tokens of its parent p: all shared, but a last
+// one that is partly filled, which only the first row of each parent keeps.  The free
+// pages that the others take are numbered by an exclusive sum over the rows.
+//
+// Bound by latency where rows are few, by the tables' bytes where they are long (each
+// row's entries read once and written once).  As in page_plan.cu one launch without a
+// grid-wide wait: every CTA looks through all rows by itself, kForkThreads at a time, and
+// writes its share of the table.  Whether a parent was met in earlier chunks is a bit in
+// shared memory; within the chunk a row looks at those before it.
+// ---------------------------------------------------------------------------
+
+constexpr int kForkThreads = 256;
+constexpr int kMaxParents = 65536;  // bits in shared memory
+
+struct ForkArgs {
+  const int32_t *parents, *past, *free_pages, *table;
+  int32_t *new_table, *new_past, *src, *dst, *used;
+  uint32_t* status;
+  int rows, batch, nfree, width, shift;
+};
+
+__device__ __forceinline__ int warp_sum_to(int v, int lane) {
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int o = __shfl_up_sync(0xffffffffu, v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+
+__global__ void __launch_bounds__(kForkThreads) page_fork_kernel(const __grid_constant__ ForkArgs a) {
+  constexpr int kWarps = kForkThreads / 32;
+  __shared__ uint32_t met[kMaxParents / 32];
+  __shared__ int parent_of[kForkThreads];
+  __shared__ int held_of[kForkThreads];   // entries of the row
+  __shared__ int last_of[kForkThreads];   // its last one where that is a page of its own, or -1
+  __shared__ int warp_takes[kWarps];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int P = 1 << a.shift;
+  const bool writer = blockIdx.x == 0;
+  uint32_t flags = 0;
+  int taken = 0;
+  for (int i = tid; i < (a.batch + 31) / 32; i += kForkThreads) met[i] = 0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  for (int r0 = 0; r0 < a.rows; r0 += kForkThreads) {
+    const int r = r0 + tid;
+    int parent = -1;
+    int64_t past = 0;
+    if (r < a.rows) {
+      parent = a.parents[r];
+      if (parent >= a.batch) {
+        flags |= SSS_FLAG_INDEX;
+        parent = -1;
+      }
+      if (parent >= 0) {
+        past = a.past[parent];
+        const int64_t most = static_cast<int64_t>(a.width) << a.shift;
+        if (past < 0 || past > most) {
+          flags |= SSS_FLAG_INDEX;
+          past = past < 0 ? 0 : most;
+        }
+      }
+    }
+    __syncthreads();  // (the chunk before is read)
+    parent_of[tid] = parent;
+    __syncthreads();
+    // is this the parent's first row?
+    bool first = true;
+    if (parent >= 0) {
+      first = (met[parent >> 5] >> (parent & 31) & 1u) == 0;
+      for (int i = 0; i < tid; ++i) first = first && parent_of[i] != parent;
+    }
+    const bool open = (past & (P - 1)) != 0;  // the last page is partly filled
+    bool take = parent >= 0 && open && !first;
+    int from = -1;
+    if (take) {
+      from = a.table[static_cast<int64_t>(parent) * a.width + (past >> a.shift)];
+      if (from < 0) {  // nothing to copy
+        flags |= SSS_FLAG_INDEX;
+        take = false;
+        past &= ~static_cast<int64_t>(P - 1);
+      }
+    }
+    const int upto = warp_sum_to(take ? 1 : 0, lane);
+    if (lane == 31) warp_takes[warp] = upto;
+    __syncthreads();
+    if (parent >= 0) atomicOr(&met[parent >> 5], 1u << (parent & 31));
+    int at = taken + upto - 1;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      at += w < warp ? warp_takes[w] : 0;
+      taken += warp_takes[w];
+    }
+    int to = -1;
+    if (take) {
+      to = at < a.nfree ? a.free_pages[at] : -1;
+      if (to < 0) {
+        flags |= SSS_FLAG_PAGES;
+        from = -1;
+        past &= ~static_cast<int64_t>(P - 1);
+      }
+    }
+    held_of[tid] = static_cast<int>((past + P - 1) >> a.shift);
+    last_of[tid] = to;
+    if (writer && r < a.rows) {
+      a.new_past[r] = static_cast<int32_t>(past);
+      a.src[r] = from;
+      a.dst[r] = to;
+    }
+    __syncthreads();
+    // the chunk's rows, a warp to a piece of 256 entries
+    const int rows = min(kForkThreads, a.rows - r0), pieces = (a.width + 255) / 256;
+    const int64_t items = static_cast<int64_t>(rows) * pieces;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + warp; i < items;
+         i += static_cast<int64_t>(gridDim.x) * kWarps) {
+      const int row = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(row) * pieces) * 256;
+      const int p = parent_of[row], held = held_of[row], last = last_of[row];
+      const int32_t* in = a.table + static_cast<int64_t>(max(p, 0)) * a.width;
+      int32_t* out = a.new_table + static_cast<int64_t>(r0 + row) * a.width;
+      int32_t v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int c = c0 + 32 * k + lane;
+        v[k] = c < held ? __ldg(in + c) : -1;
+        if (c == held - 1 && last >= 0) v[k] = last;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const int c = c0 + 32 * k + lane;
+        if (c < a.width) out[c] = v[k];
+      }
+    }
+  }
+  if (writer && tid == 0) *a.used = min(taken, a.nfree);
+  if (flags && a.status && writer) atomicOr(a.status, flags);
+}
+
+// ---------------------------------------------------------------------------
+// Reclaim.  One cluster: each CTA sets the bits of the pages that its share of the table
+// names in a map of its own, the CTAs join their maps (each a slice of it from all, then
+// every slice from its CTA), and every CTA counts the map's words.  With rk(x) held pages
+// below x, m in all and k moves, the free page x is the (x - rk(x))-th and the held one the
+// (m - 1 - rk(x))-th from above: both say by themselves which move they belong to
+// and where in the list what is free afterwards stands:
+//   a free page that stays free: its number less the k that are taken, and the held pages
+//     below it that moved away, max(0, rk(x) - (m - k));
+//   one that moved away: rk(x) - (m - k), and the x - rk(x) - k free ones below it.
+// Bound by latency: a few waits of the cluster, and the table's entries.
+// ---------------------------------------------------------------------------
+
+constexpr int kMapThreads = 1024;
+constexpr int kMapCtas = 8;
+constexpr int kSpan = 8;  // words of the map to one running count
+
+struct MapArgs {
+  const int32_t *table, *past;
+  int32_t *free_pages, *free_count, *new_table, *src, *dst, *moves;
+  uint32_t* status;
+  int batch, width, shift, pages, most;
+};
+
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_word(const uint32_t* p, int rank) {
+  uint32_t addr = static_cast<uint32_t>(__cvta_generic_to_shared(p)), v;
+  asm("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(addr) : "r"(rank));
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+// the entries of row b that hold pages
+__device__ __forceinline__ int held_entries(const MapArgs& a, int b, uint32_t& flags) {
+  int64_t past = a.past[b];
+  const int64_t most = static_cast<int64_t>(a.width) << a.shift;
+  if (past < 0 || past > most) {
+    flags |= SSS_FLAG_INDEX;
+    past = past < 0 ? 0 : most;
+  }
+  return static_cast<int>((past + (1 << a.shift) - 1) >> a.shift);
+}
+
+__global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_constant__ MapArgs a) {
+  extern __shared__ uint32_t map[];  // [words], then the counts [spans + 1]
+  __shared__ int warp_held[32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int ctas = gridDim.x, me = blockIdx.x;  // (one cluster)
+  const int spans = (a.pages + 32 * kSpan - 1) / (32 * kSpan), words = spans * kSpan;
+  int* count = reinterpret_cast<int*>(map + words);
+  uint32_t flags = 0;
+  for (int i = tid; i < words; i += kMapThreads) map[i] = 0;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  __syncthreads();
+  // the rows' entries, a warp to a piece of 256
+  constexpr int kWarps = kMapThreads / 32;
+  const int pieces = (a.width + 255) / 256;
+  const int64_t items = static_cast<int64_t>(a.batch) * pieces;
+  for (int64_t i = static_cast<int64_t>(me) * kWarps + warp; i < items; i += static_cast<int64_t>(ctas) * kWarps) {
+    const int b = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(b) * pieces) * 256;
+    const int held = held_entries(a, b, flags);
+    const int32_t* row = a.table + static_cast<int64_t>(b) * a.width;
+    int32_t v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int c = c0 + 32 * k + lane;
+      v[k] = c < held ? row[c] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (c0 + 32 * k + lane >= held) continue;
+      if (v[k] < 0 || v[k] >= a.pages) flags |= SSS_FLAG_INDEX;
+      else atomicOr(&map[v[k] >> 5], 1u << (v[k] & 31));
+    }
+  }
+  if (ctas > 1) {
+    cluster_meet();
+    const int slice = (words + ctas - 1) / ctas;
+    for (int i = me * slice + tid; i < min(words, (me + 1) * slice); i += kMapThreads) {
+      uint32_t v = 0;
+      for (int c = 0; c < ctas; ++c) v |= peer_word(map + i, c);
+      map[i] = v;
+    }
+    cluster_meet();
+    for (int i = tid; i < words; i += kMapThreads)
+      if (i / slice != me) map[i] = peer_word(map + i, i / slice);
+  }
+  __syncthreads();
+  // counts: of the spans, then their sums
+  int m = 0;
+  for (int s0 = 0; s0 < spans; s0 += kMapThreads) {
+    const int s = s0 + tid;
+    int n = 0;
+    if (s < spans)
+#pragma unroll
+      for (int w = 0; w < kSpan; ++w) n += __popc(map[s * kSpan + w]);
+    const int upto = warp_sum_to(n, lane);
+    if (lane == 31) warp_held[warp] = upto;
+    __syncthreads();
+    const int of = warp_held[lane];
+    const int sums = warp_sum_to(of, lane);
+    const int before = __shfl_sync(0xffffffffu, sums - of, warp);
+    if (s < spans) count[s] = m + before + upto - n;
+    m += __shfl_sync(0xffffffffu, sums, 31);
+    __syncthreads();
+  }
+  const auto rank_of = [&](int x) {  // held pages below x
+    const int w = x >> 5, s = w / kSpan;
+    int n = count[s] + __popc(map[w] & ((1u << (x & 31)) - 1));
+    for (int i = s * kSpan; i < w; ++i) n += __popc(map[i]);
+    return n;
+  };
+  // moves: as many as there are free pages below m
+  int k = 0;
+  if (a.moves && m < a.pages) k = min(a.most, m - rank_of(m));
+  // the lists, a warp to a word
+  for (int w = me * kWarps + warp; w < (a.pages + 31) / 32; w += ctas * kWarps) {
+    const int x = 32 * w + lane;
+    if (x >= a.pages) continue;
+    const bool is_held = map[w] >> lane & 1u;
+    const int rk = rank_of(x);
+    int pos = -1;
+    if (is_held) {
+      const int i = m - 1 - rk;
+      if (i < k) {
+        a.src[i] = x;
+        pos = rk - (m - k) + (x - rk) - k;
+      }
+    } else {
+      const int i = x - rk;
+      if (i < k) a.dst[i] = x;
+      else pos = i - k + max(0, rk - (m - k));
+    }
+    if (pos >= 0) a.free_pages[pos] = x;
+    if (x >= a.pages - m) a.free_pages[x] = -1;
+  }
+  if (me == 0 && tid == 0) {
+    *a.free_count = a.pages - m;
+    if (a.moves) *a.moves = k;
+  }
+  if (a.moves) {
+    for (int i = k + me * kMapThreads + tid; i < a.most; i += ctas * kMapThreads) a.src[i] = a.dst[i] = -1;
+    // the moves' destinations, of all CTAs
+    if (ctas > 1) cluster_meet();
+    else __syncthreads();
+    for (int64_t i = static_cast<int64_t>(me) * kWarps + warp; i < items; i += static_cast<int64_t>(ctas) * kWarps) {
+      const int b = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(b) * pieces) * 256;
+      uint32_t said = 0;
+      const int held = held_entries(a, b, said);
+      const int64_t at = static_cast<int64_t>(b) * a.width;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = c0 + 32 * e + lane;
+        if (c >= held) continue;
+        int32_t v = a.table[at + c];
+        if (v >= 0 && v < a.pages) {
+          const int j = m - 1 - rank_of(v);
+          if (j < k) v = *static_cast<volatile int32_t*>(a.dst + j);
+        }
+        a.new_table[at + c] = v;
+      }
+    }
+  }
+  if (flags && a.status) atomicOr(a.status, flags);
+  // nobody leaves while a peer may still read its map
+  if (ctas > 1) cluster_meet();
+}
+
+// ---------------------------------------------------------------------------
+// Copy.  Each CTA takes pieces of the pages that are to be copied, of one cache after the
+// other.  Bound by HBM, or by the launch where pages are few: all layers go in one.
+// ---------------------------------------------------------------------------
+
+constexpr int kCopyThreads = 256;
+constexpr int kCopyCtas = 4;      // an SM
+constexpr int kCopyUnroll = 4;    // 16-byte loads in flight a thread
+
+struct CopyArgs {
+  char* base[2 * kMaxCopyCaches];      // keys and values, or blocks
+  int64_t stride[2 * kMaxCopyCaches];  // bytes from a page to the next
+  const int32_t *src, *dst;
+  uint32_t* status;
+  int64_t pages;
+  int parts, n;
+  int rows, row16;  // evenly spaced rows of a page (a power of two), 16-byte units of a row
+  int row_shift;
+  int pieces;       // of a page
+};
+
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) page_copy_kernel(const __grid_constant__ CopyArgs a) {
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  constexpr int kPiece = kCopyThreads * kCopyUnroll;  // units
+  const int64_t items = static_cast<int64_t>(a.n) * a.parts * a.pieces;
+  const int units = a.rows * a.row16;
+  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+    const int64_t e = it / a.pieces;
+    const int piece = static_cast<int>(it - e * a.pieces);
+    const int part = static_cast<int>(e / a.n), i = static_cast<int>(e - static_cast<int64_t>(part) * a.n);
+    const int64_t from = a.src[i], to = a.dst[i];
+    if (from < 0 || to < 0 || from >= a.pages || to >= a.pages) {
+      if ((from >= 0 || to >= 0) && threadIdx.x == 0 && a.status) atomicOr(a.status, SSS_FLAG_INDEX);
+      continue;
+    }
+    const int64_t stride = a.stride[part], row_stride = stride >> a.row_shift;
+    const char* in = a.base[part] + from * stride;
+    char* out = a.base[part] + to * stride;
+    uint4 v[kCopyUnroll];
+    int64_t at[kCopyUnroll];
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+      const int x = piece * kPiece + u * kCopyThreads + threadIdx.x;
+      const int row = x / a.row16;
+      at[u] = row * row_stride + static_cast<int64_t>(x - row * a.row16) * 16;
+      if (x < units) v[u] = __ldcs(reinterpret_cast<const uint4*>(in + at[u]));
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u)
+      if (piece * kPiece + u * kCopyThreads + threadIdx.x < units) *reinterpret_cast<uint4*>(out + at[u]) = v[u];
+  }
+}
+
+template <typename K, typename A>
+cudaError_t launch(K kern, const A& a, int64_t ctas, int threads, int smem, int cluster, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = cluster;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cluster > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, a);
+}
+
+int shift_of(int page_size) {
+  int s = 0;
+  while ((1 << s) < page_size) ++s;
+  return s;
+}
+
+cudaError_t copy(CopyArgs& a, cudaStream_t stream) {
+  const int units = a.rows * a.row16;
+  a.row_shift = shift_of(a.rows);
+  a.pieces = (units + kCopyThreads * kCopyUnroll - 1) / (kCopyThreads * kCopyUnroll);
+  const int64_t items = static_cast<int64_t>(a.n) * a.parts * a.pieces;
+  return launch(page_copy_kernel, a, std::min<int64_t>(items, int64_t{kCopyCtas} * device_sm_count()),
+                kCopyThreads, 0, 1, stream);
+}
+
+}  // namespace
+
+cudaError_t launch_page_fork(const int32_t* parents, int rows, const int32_t* past, int batch,
+                             int page_size, const int32_t* free_pages, int nfree,
+                             const int32_t* table, int width, int32_t* new_table,
+                             int32_t* new_past, int32_t* src, int32_t* dst, int32_t* used,
+                             uint32_t* status, cudaStream_t stream) {
+  const ForkArgs a = {parents, past, free_pages, table, new_table, new_past, src, dst, used,
+                      status, rows, batch, nfree, width, shift_of(page_size)};
+  const int64_t items = static_cast<int64_t>(std::min(rows, kForkThreads)) * ((width + 255) / 256);
+  const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>((items + 7) / 8, 2 * device_sm_count()));
+  return launch(page_fork_kernel, a, ctas, kForkThreads, 0, 1, stream);
+}
+
+cudaError_t launch_page_reclaim(const int32_t* table, int width, const int32_t* past, int batch,
+                                int page_size, int pages, int32_t* free_pages, int32_t* free_count,
+                                int32_t* new_table, int32_t* src, int32_t* dst, int most,
+                                int32_t* moves, uint32_t* status, cudaStream_t stream) {
+  const MapArgs a = {table, past, free_pages, free_count, new_table, src, dst, moves,
+                     status, batch, width, shift_of(page_size), pages, most};
+  const int spans = (pages + 32 * kSpan - 1) / (32 * kSpan);
+  const int smem = (spans * kSpan + spans) * 4;
+  cudaError_t e = ensure_smem(page_map_kernel, (kMaxMapPages / 32 + kMaxMapPages / (32 * kSpan)) * 4);
+  if (e != cudaSuccess) return e;
+  // a CTA for each two rounds of its warps over the table or the map
+  const int64_t work = std::max<int64_t>(static_cast<int64_t>(batch) * ((width + 255) / 256), pages / 64);
+  int ctas = 1;
+  while (ctas < kMapCtas && work > ctas * 64) ctas *= 2;
+  return launch(page_map_kernel, a, ctas, kMapThreads, smem, ctas, stream);
+}
+
+cudaError_t launch_page_copy(const sss_kv_cache_t* const* caches, int count, const int32_t* src,
+                             const int32_t* dst, int n, uint32_t* status, cudaStream_t stream) {
+  CopyArgs a = {};
+  const sss_kv_cache_t& c = *caches[0];
+  const bool dense = std::all_of(caches, caches + count, [](const sss_kv_cache_t* x) {
+    return x->stride == static_cast<int64_t>(x->heads) * x->dim;
+  });
+  a.rows = dense ? 1 : c.page_size;
+  a.row16 = c.heads * c.dim / 8 * (dense ? c.page_size : 1);
+  for (int i = 0; i < count; ++i)
+    for (int v = 0; v < 2; ++v) {
+      a.base[2 * i + v] = static_cast<char*>(v ? caches[i]->v : caches[i]->k);
+      a.stride[2 * i + v] = caches[i]->stride * 2 * c.page_size;
+    }
+  a.src = src;
+  a.dst = dst;
+  a.status = status;
+  a.pages = c.slots / c.page_size;
+  a.parts = 2 * count;
+  a.n = n;
+  return copy(a, stream);
+}
+
+cudaError_t launch_page_copy_q4(const sss_kv_cache_q4_t* const* caches, int count,
+                                const int32_t* src, const int32_t* dst, int n, uint32_t* status,
+                                cudaStream_t stream) {
+  CopyArgs a = {};
+  const sss_kv_cache_q4_t& c = *caches[0];
+  a.rows = 1;
+  a.row16 = c.heads * (c.page_size / 16) * (18 * c.dim / 16);
+  for (int i = 0; i < count; ++i) {
+    a.base[i] = static_cast<char*>(caches[i]->blocks);
+    a.stride[i] = caches[i]->page_stride;
+  }
+  a.src = src;
+  a.dst = dst;
+  a.status = status;
+  a.pages = c.pages;
+  a.parts = count;
+  a.n = n;
+  return copy(a, stream);
+}
+
+}  // namespace sss

@@ -1,6 +1,7 @@
 // sss_api.cu -- the C ABI declared in include/sss.h: synchronous argument
 // validation, dispatch to the kernels' launchers, and error mapping.  No
 // entry point allocates device memory.
+#include <initializer_list>
 #include <atomic>
 #include <map>
 #include <mutex>
@@ -595,6 +596,197 @@ sss_status_t sss_attention(const void* q, int64_t q_stride, int32_t heads,
                 launch_attention(p, q, q_stride, heads, *cache, cu_q, kv_len, block_table,
                                  table_width, batch, tokens, max_q, max_kv, scale, out, workspace,
                                  dev_status, static_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+sss_status_t check_cache_q4(const sss_kv_cache_q4_t* c) {
+  if (c == nullptr || c->reserved != 0) return SSS_E_ARG;
+  if (c->dim != 64 && c->dim != 128) return c->dim < 1 ? SSS_E_ARG : SSS_E_UNSUPPORTED;
+  if (c->heads < 1 || c->heads > kMaxHeads || !page_size_ok(c->page_size)) return SSS_E_ARG;
+  if (c->pages < 0 || c->pages > INT32_MAX / c->page_size) return SSS_E_ARG;
+  if (c->page_stride < static_cast<int64_t>(c->heads) * (c->page_size / 16) * 18 * c->dim ||
+      c->page_stride > (int64_t{1} << 40) || c->page_stride % 16 != 0)
+    return SSS_E_ARG;
+  if (c->pages > 0 && c->blocks == nullptr) return SSS_E_ARG;
+  if (!aligned(c->blocks, 16)) return SSS_E_ALIGN;
+  return SSS_OK;
+}
+bool ints_aligned(std::initializer_list<const void*> ps) {
+  for (const void* p : ps)
+    if (!aligned(p, 4)) return false;
+  return true;
+}
+}  // namespace
+
+sss_status_t sss_kv_store_q4(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                             int32_t in_dtype, int64_t tokens, const sss_kv_cache_q4_t* cache,
+                             const int32_t* slots, uint32_t* dev_status, void* stream) {
+  sss_status_t st = check_cache_q4(cache);
+  if (st != SSS_OK) return st;
+  if (in_dtype < SSS_OUT_F32 || in_dtype > SSS_OUT_BF16) return SSS_E_ARG;
+  if (tokens < 0 || tokens > kMaxTokens) return SSS_E_ARG;
+  const int64_t width = static_cast<int64_t>(cache->heads) * cache->dim;
+  const int of = in_dtype == SSS_OUT_F32 ? 4 : 8;
+  if (k_stride < width || v_stride < width || k_stride > kMaxDim || v_stride > kMaxDim ||
+      k_stride % of != 0 || v_stride % of != 0)
+    return SSS_E_ARG;
+  if (tokens == 0) return SSS_OK;
+  if (k == nullptr || v == nullptr) return SSS_E_ARG;
+  if (!aligned(k, 16) || !aligned(v, 16) || !ints_aligned({slots, dev_status})) return SSS_E_ALIGN;
+  return finish("sss_kv_store_q4",
+                launch_kv_store_q4(k, k_stride, v, v_stride, in_dtype, tokens, *cache, slots,
+                                   dev_status, static_cast<cudaStream_t>(stream)));
+}
+
+sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slots, int64_t count,
+                             void* k, void* v, int32_t out_dtype, uint32_t* dev_status,
+                             void* stream) {
+  sss_status_t st = check_cache_q4(cache);
+  if (st != SSS_OK) return st;
+  if (out_dtype < SSS_OUT_F32 || out_dtype > SSS_OUT_BF16) return SSS_E_ARG;
+  if (count < 0 || count > kMaxTokens) return SSS_E_ARG;
+  if (count == 0 || (k == nullptr && v == nullptr)) return SSS_OK;
+  if (!aligned(k, 16) || !aligned(v, 16) || !ints_aligned({slots, dev_status})) return SSS_E_ALIGN;
+  return finish("sss_kv_fetch_q4", launch_kv_fetch_q4(*cache, slots, count, k, v, out_dtype, dev_status,
+                                                      static_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+sss_status_t check_attention_q4(int64_t tokens, int32_t heads, const sss_kv_cache_q4_t* cache,
+                                int32_t table_width, int32_t batch, int32_t max_q, int64_t max_kv) {
+  sss_status_t st = check_cache_q4(cache);
+  if (st != SSS_OK) return st;
+  if (heads < 1 || heads > kMaxHeads || heads % cache->heads != 0) return SSS_E_ARG;
+  if (batch < 0 || batch > kMaxBatch || tokens < 0 || tokens > kMaxTokens) return SSS_E_ARG;
+  if (max_q < 0 || max_kv < 0 || max_kv > INT32_MAX / 2 || table_width < 1) return SSS_E_ARG;
+  return SSS_OK;
+}
+}  // namespace
+
+size_t sss_attention_q4_workspace_bytes(int64_t tokens, int32_t heads,
+                                        const sss_kv_cache_q4_t* cache, int32_t table_width,
+                                        int32_t batch, int32_t max_q, int64_t max_kv) {
+  if (check_attention_q4(tokens, heads, cache, table_width, batch, max_q, max_kv) != SSS_OK) return 0;
+  if (tokens == 0 || batch == 0 || max_q == 0) return 0;
+  return plan_attention_q4(tokens, heads, *cache, table_width, batch, bound_q(max_q, tokens), max_kv).ws_bytes;
+}
+
+sss_status_t sss_attention_q4(const void* q, int64_t q_stride, int32_t heads, int32_t dtype,
+                              const sss_kv_cache_q4_t* cache, const int32_t* cu_q,
+                              const int32_t* kv_len, const int32_t* block_table,
+                              int32_t table_width, int32_t batch, int64_t tokens, int32_t max_q,
+                              int64_t max_kv, float scale, void* out, void* workspace,
+                              size_t ws_bytes, uint32_t* dev_status, void* stream) {
+  sss_status_t st = check_attention_q4(tokens, heads, cache, table_width, batch, max_q, max_kv);
+  if (st != SSS_OK) return st;
+  if (dtype != SSS_OUT_F16 && dtype != SSS_OUT_BF16) return SSS_E_ARG;
+  if (!(scale > 0.0f) || !(scale <= 2.3e38f)) return SSS_E_ARG;  // (times log2(e): finite)
+  if (q_stride < static_cast<int64_t>(heads) * cache->dim || q_stride > kMaxDim || q_stride % 8 != 0)
+    return SSS_E_ARG;
+  if (tokens == 0 || batch == 0 || max_q == 0) return SSS_OK;
+  if (q == nullptr || out == nullptr || cu_q == nullptr || kv_len == nullptr || block_table == nullptr)
+    return SSS_E_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) ||
+      !ints_aligned({cu_q, kv_len, block_table, dev_status}))
+    return SSS_E_ALIGN;
+  max_q = bound_q(max_q, tokens);
+  const AttnQ4Plan p = plan_attention_q4(tokens, heads, *cache, table_width, batch, max_q, max_kv);
+  if (p.of.prompt && static_cast<int64_t>(batch) * p.pages * cache->page_size > INT32_MAX)
+    return SSS_E_UNSUPPORTED;
+  if (p.ws_bytes > 0 && (workspace == nullptr || ws_bytes < p.ws_bytes)) return SSS_E_WORKSPACE;
+  return finish("sss_attention_q4",
+                launch_attention_q4(p, q, q_stride, heads, dtype, *cache, cu_q, kv_len, block_table,
+                                    table_width, batch, tokens, max_q, max_kv, scale, out, workspace,
+                                    dev_status, static_cast<cudaStream_t>(stream)));
+}
+
+sss_status_t sss_page_fork(const int32_t* parents, int32_t rows, const int32_t* past,
+                           int32_t batch, int32_t page_size, const int32_t* free_pages,
+                           int32_t free_count, const int32_t* block_table, int32_t table_width,
+                           int32_t* new_table, int32_t* new_past, int32_t* src, int32_t* dst,
+                           int32_t* used, uint32_t* dev_status, void* stream) {
+  if (rows < 0 || rows > kMaxBatch || batch < 0 || batch > kMaxBatch || free_count < 0 ||
+      table_width < 0 || !page_size_ok(page_size) || used == nullptr)
+    return SSS_E_ARG;
+  if (rows > 0 && (parents == nullptr || new_past == nullptr || src == nullptr || dst == nullptr))
+    return SSS_E_ARG;
+  if (batch > 0 && past == nullptr) return SSS_E_ARG;
+  if (table_width > 0 && ((batch > 0 && block_table == nullptr) || (rows > 0 && new_table == nullptr)))
+    return SSS_E_ARG;
+  if (free_count > 0 && free_pages == nullptr) return SSS_E_ARG;
+  if (rows > 0 && batch > 0 && ((table_width > 0 && new_table == block_table) || new_past == past))
+    return SSS_E_ARG;
+  if (!ints_aligned({parents, past, free_pages, block_table, new_table, new_past, src, dst, used, dev_status}))
+    return SSS_E_ALIGN;
+  return finish("sss_page_fork",
+                launch_page_fork(parents, rows, past, batch, page_size, free_pages, free_count,
+                                 block_table, table_width, new_table, new_past, src, dst, used,
+                                 dev_status, static_cast<cudaStream_t>(stream)));
+}
+
+sss_status_t sss_page_reclaim(const int32_t* block_table, int32_t table_width,
+                              const int32_t* past, int32_t batch, int32_t page_size,
+                              int32_t pages, int32_t* free_pages, int32_t* free_count,
+                              int32_t* new_table, int32_t* src, int32_t* dst, int32_t most_moves,
+                              int32_t* moves, uint32_t* dev_status, void* stream) {
+  if (batch < 0 || table_width < 0 || !page_size_ok(page_size) || pages < 0 ||
+      pages > kMaxMapPages || most_moves < 0 || free_count == nullptr)
+    return SSS_E_ARG;
+  if (batch > 0 && (past == nullptr || (table_width > 0 && block_table == nullptr))) return SSS_E_ARG;
+  if (pages > 0 && free_pages == nullptr) return SSS_E_ARG;
+  if (moves == nullptr && new_table != nullptr) return SSS_E_ARG;
+  if (moves != nullptr && ((batch > 0 && table_width > 0 && new_table == nullptr) ||
+                           (most_moves > 0 && (src == nullptr || dst == nullptr))))
+    return SSS_E_ARG;
+  if (!ints_aligned({block_table, past, free_pages, free_count, new_table, src, dst, moves, dev_status}))
+    return SSS_E_ALIGN;
+  return finish("sss_page_reclaim",
+                launch_page_reclaim(block_table, table_width, past, batch, page_size, pages,
+                                    free_pages, free_count, new_table, src, dst, most_moves, moves,
+                                    dev_status, static_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+sss_status_t check_copy(int32_t count, const void* caches, const int32_t* src, const int32_t* dst,
+                        int32_t n, const uint32_t* dev_status) {
+  if (count < 0 || count > kMaxCopyCaches || n < 0 || (count > 0 && caches == nullptr)) return SSS_E_ARG;
+  if (n > 0 && (src == nullptr || dst == nullptr)) return SSS_E_ARG;
+  return ints_aligned({src, dst, dev_status}) ? SSS_OK : SSS_E_ALIGN;
+}
+}  // namespace
+
+sss_status_t sss_page_copy(const sss_kv_cache_t* const* caches, int32_t count, const int32_t* src,
+                           const int32_t* dst, int32_t n, uint32_t* dev_status, void* stream) {
+  sss_status_t st = check_copy(count, caches, src, dst, n, dev_status);
+  for (int i = 0; st == SSS_OK && i < count; ++i) {
+    const sss_kv_cache_t *c = caches[i], *first = caches[0];
+    st = check_cache(c);
+    if (st == SSS_OK && !page_size_ok(c->page_size)) st = SSS_E_ARG;
+    if (st == SSS_OK && (c->page_size != first->page_size || c->heads != first->heads || c->dim != first->dim ||
+                         c->slots / c->page_size != first->slots / first->page_size))
+      st = SSS_E_ARG;
+  }
+  if (st != SSS_OK) return st;
+  if (count == 0 || n == 0) return SSS_OK;
+  return finish("sss_page_copy", launch_page_copy(caches, count, src, dst, n, dev_status,
+                                                  static_cast<cudaStream_t>(stream)));
+}
+
+sss_status_t sss_page_copy_q4(const sss_kv_cache_q4_t* const* caches, int32_t count,
+                              const int32_t* src, const int32_t* dst, int32_t n,
+                              uint32_t* dev_status, void* stream) {
+  sss_status_t st = check_copy(count, caches, src, dst, n, dev_status);
+  for (int i = 0; st == SSS_OK && i < count; ++i) {
+    const sss_kv_cache_q4_t *c = caches[i], *first = caches[0];
+    st = check_cache_q4(c);
+    if (st == SSS_OK && (c->page_size != first->page_size || c->heads != first->heads || c->dim != first->dim ||
+                         c->pages != first->pages))
+      st = SSS_E_ARG;
+  }
+  if (st != SSS_OK) return st;
+  if (count == 0 || n == 0) return SSS_OK;
+  return finish("sss_page_copy_q4", launch_page_copy_q4(caches, count, src, dst, n, dev_status,
+                                                        static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -104,6 +104,44 @@ cudaError_t launch_attention(const AttnPlan& plan, const void* q, int64_t q_stri
                              int64_t tokens, int max_q, int64_t max_kv, float scale, void* out,
                              void* workspace, uint32_t* status, cudaStream_t stream);
 
+cudaError_t launch_kv_store_q4(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                               int in_dtype, int64_t tokens, const sss_kv_cache_q4_t& cache,
+                               const int32_t* slots, uint32_t* status, cudaStream_t stream);
+cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* slots, int64_t count,
+                               void* k, void* v, int out_dtype, uint32_t* status,
+                               cudaStream_t stream);
+
+// How a call of sss_attention_q4 is laid out.
+struct AttnQ4Plan {
+  AttnPlan of;     // its rows' form, or that of the 16-bit copy in the workspace
+  int pages;       // of the copy, for each request
+  size_t table_at, k_at, v_at, ws_bytes;  // the copy: its table, keys, values
+};
+AttnQ4Plan plan_attention_q4(int64_t tokens, int heads, const sss_kv_cache_q4_t& cache, int width,
+                             int batch, int max_q, int64_t max_kv);
+cudaError_t launch_attention_q4(const AttnQ4Plan& plan, const void* q, int64_t q_stride, int heads,
+                                int dtype, const sss_kv_cache_q4_t& cache, const int32_t* cu_q,
+                                const int32_t* kv_len, const int32_t* table, int width, int batch,
+                                int64_t tokens, int max_q, int64_t max_kv, float scale, void* out,
+                                void* workspace, uint32_t* status, cudaStream_t stream);
+
+cudaError_t launch_page_fork(const int32_t* parents, int rows, const int32_t* past, int batch,
+                             int page_size, const int32_t* free_pages, int nfree,
+                             const int32_t* table, int width, int32_t* new_table,
+                             int32_t* new_past, int32_t* src, int32_t* dst, int32_t* used,
+                             uint32_t* status, cudaStream_t stream);
+constexpr int kMaxMapPages = 1 << 20;  // a bit each in shared memory
+cudaError_t launch_page_reclaim(const int32_t* table, int width, const int32_t* past, int batch,
+                                int page_size, int pages, int32_t* free_pages, int32_t* free_count,
+                                int32_t* new_table, int32_t* src, int32_t* dst, int most,
+                                int32_t* moves, uint32_t* status, cudaStream_t stream);
+constexpr int kMaxCopyCaches = 128;
+cudaError_t launch_page_copy(const sss_kv_cache_t* const* caches, int count, const int32_t* src,
+                             const int32_t* dst, int n, uint32_t* status, cudaStream_t stream);
+cudaError_t launch_page_copy_q4(const sss_kv_cache_q4_t* const* caches, int count,
+                                const int32_t* src, const int32_t* dst, int n, uint32_t* status,
+                                cudaStream_t stream);
+
 // The kernel families whose next launches skip one barrier arrive
 // (sss_test_set_stall; 0 in normal use).
 uint32_t test_stall_mask();

@@ -47,7 +47,10 @@ EXPORTS = ("sss_codes_bytes", "sss_status_string", "sss_last_error", "sss_quanti
            "sss_gemm_q8", "sss_quantize_act_q8", "sss_sign_diagnostics", "sss_hadamard",
            "sss_quantize_rotated", "sss_quantize_lsq",
            "sss_page_plan", "sss_qk_norm_rope", "sss_attention",
-           "sss_attention_workspace_bytes")
+           "sss_attention_workspace_bytes",
+           "sss_kv_store_q4", "sss_kv_fetch_q4", "sss_attention_q4",
+           "sss_attention_q4_workspace_bytes", "sss_page_fork", "sss_page_reclaim",
+           "sss_page_copy", "sss_page_copy_q4")
 
 GEMV_PDL = 0x1
 GEMV_WEIGHTS_READY = 0x2
@@ -97,6 +100,19 @@ class KVCacheDesc(ctypes.Structure):
         ("heads", ctypes.c_int32),
         ("dim", ctypes.c_int32),
         ("dtype", ctypes.c_int32),
+    ]
+
+
+class KVCacheQ4Desc(ctypes.Structure):
+    """Mirror of sss_kv_cache_q4_t."""
+    _fields_ = [
+        ("blocks", ctypes.c_void_p),
+        ("pages", ctypes.c_int64),
+        ("page_stride", ctypes.c_int64),
+        ("page_size", ctypes.c_int32),
+        ("heads", ctypes.c_int32),
+        ("dim", ctypes.c_int32),
+        ("reserved", ctypes.c_int32),
     ]
 
 
@@ -189,6 +205,25 @@ def load(build_if_needed: bool = True):
         L.sss_attention.restype = i32
         L.sss_attention_workspace_bytes.argtypes = [i64, i32, C, i32, i32, i64]
         L.sss_attention_workspace_bytes.restype = sz
+        Q = ctypes.POINTER(KVCacheQ4Desc)
+        L.sss_kv_store_q4.argtypes = [vp, i64, vp, i64, i32, i64, Q, vp, vp, vp]
+        L.sss_kv_store_q4.restype = i32
+        L.sss_kv_fetch_q4.argtypes = [Q, vp, i64, vp, vp, i32, vp, vp]
+        L.sss_kv_fetch_q4.restype = i32
+        L.sss_attention_q4.argtypes = [vp, i64, i32, i32, Q, vp, vp, vp, i32, i32, i64, i32, i64,
+                                       f32, vp, vp, sz, vp, vp]
+        L.sss_attention_q4.restype = i32
+        L.sss_attention_q4_workspace_bytes.argtypes = [i64, i32, Q, i32, i32, i32, i64]
+        L.sss_attention_q4_workspace_bytes.restype = sz
+        L.sss_page_fork.argtypes = [vp, i32, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp,
+                                    vp, vp]
+        L.sss_page_fork.restype = i32
+        L.sss_page_reclaim.argtypes = [vp, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, vp, vp,
+                                       vp]
+        L.sss_page_reclaim.restype = i32
+        for f in (L.sss_page_copy, L.sss_page_copy_q4):
+            f.argtypes = [vp, i32, vp, vp, i32, vp, vp]
+            f.restype = i32
         L.sss_test_set_stall.argtypes = [ctypes.c_uint32]
         L.sss_test_set_stall.restype = None
         _lib = L
@@ -947,3 +982,232 @@ def sss_attention(q, cache: KVCache, cu_q, kv_len, max_q: int, max_kv: int, bloc
                               _stream(stream))
     _check(fn, st)
     return out
+
+
+# ---------------------------------------------------------------------------
+# the cache in 4 bits
+# ---------------------------------------------------------------------------
+
+@dataclass(frozen=True, eq=False)
+class KVCacheQ4:
+    """Keys and values in 4 bits: uint8 blocks [pages, heads, page_size / 16, 18 * dim],
+    what include/sss.h says lies in a block.  A page's blocks are dense; pages may be
+    further apart (the layers' caches as parts of one buffer).  The tensor may be refilled,
+    not replaced."""
+    blocks: "object"
+
+    def __post_init__(self):
+        import torch
+
+        fn, t = "KVCacheQ4", self.blocks
+        if t.dim() != 4 or t.dtype is not torch.uint8:
+            raise SssError(fn, 1, "blocks must be uint8 [pages, heads, page_size / 16, 18 * dim]")
+        pages, heads, blocks, size = t.shape
+        if size % 18:
+            raise SssError(fn, 1, "a block must be 18 * dim bytes")
+        dense = blocks * size * heads
+        if t.numel() and (t.stride(3) != 1 or (blocks > 1 and t.stride(2) != size)
+                          or (heads > 1 and t.stride(1) != blocks * size)):
+            raise SssError(fn, 1, "the blocks of a page must be contiguous")
+        _on_device(fn, blocks=t)
+        _describe(self, KVCacheQ4Desc(_ptr(t), pages, t.stride(0) if pages > 1 else dense,
+                                      16 * blocks, heads, size // 18, 0))
+
+    @property
+    def page_size(self) -> int:
+        return self._desc.page_size
+
+
+def empty_kv_cache_q4(pages: int, page_size: int, heads: int, dim: int, device="cuda") -> KVCacheQ4:
+    import torch
+
+    if page_size % 16:
+        raise SssError("empty_kv_cache_q4", 1, "page_size must be a multiple of 16")
+    return KVCacheQ4(torch.empty((pages, heads, page_size // 16, 18 * dim), dtype=torch.uint8,
+                                 device=device))
+
+
+def _need_cache(fn, cache, kind):
+    if not isinstance(cache, kind):
+        raise SssError(fn, 1, f"cache must be a {kind.__name__}")
+
+
+def sss_kv_store_q4(k, v, cache: KVCacheQ4, slots=None, dev_status=None, stream=None) -> None:
+    """k and v [tokens, heads, dim] (or [tokens, heads * dim]; float32 or 16-bit, rows may
+    be strided) into the cache's slots, in 4 bits.  Without slots token t goes to slot t."""
+    fn = "sss_kv_store_q4"
+    _need_cache(fn, cache, KVCacheQ4)
+    d = cache._desc
+    code = _dtype_code(k.dtype)
+    if code is None or v.dtype != k.dtype:
+        raise SssError(fn, 1, "k and v must be of one dtype: float32, float16 or bfloat16")
+    tokens = k.shape[0]
+    ks, vs = (_rows(fn, n, t, tokens, d.heads * d.dim) for n, t in (("k", k), ("v", v)))
+    if slots is not None:
+        _need_int32(fn, slots=(slots, tokens))
+    _need_status(fn, dev_status)
+    _on_device(fn, k=k, v=v, dev_status=dev_status)
+    st = load().sss_kv_store_q4(k.data_ptr(), ks, v.data_ptr(), vs, code, tokens, cache._ref,
+                                _ptr(slots), _ptr(dev_status), _stream(stream))
+    _check(fn, st)
+
+
+def sss_kv_fetch_q4(cache: KVCacheQ4, slots, k=None, v=None, dtype=None, dev_status=None,
+                    stream=None):
+    """The keys and values [count, heads, dim] that the cache holds in int32 slots [count],
+    written to k and v; both are allocated (of dtype, by default float32) where neither is
+    given, and one alone is fetched where only it is.  Returns (k, v)."""
+    import torch
+
+    fn = "sss_kv_fetch_q4"
+    _need_cache(fn, cache, KVCacheQ4)
+    d = cache._desc
+    _need_int32(fn, slots=(slots, None))
+    shape = (slots.numel(), d.heads, d.dim)
+    if k is None and v is None:
+        k, v = (_empty_on(stream, shape, dtype or torch.float32, slots.device) for _ in range(2))
+    like = k if k is not None else v
+    code = _dtype_code(like.dtype)
+    if code is None or (dtype is not None and dtype != like.dtype):
+        raise SssError(fn, 1, "k and v must be float32, float16 or bfloat16, of dtype if that is given")
+    for name, t in (("k", k), ("v", v)):
+        _need(fn, name, t, like.dtype, shape[0] * shape[1] * shape[2], optional=True)
+    _need_status(fn, dev_status)
+    _on_device(fn, k=k, v=v, dev_status=dev_status)
+    st = load().sss_kv_fetch_q4(cache._ref, slots.data_ptr(), shape[0], _ptr(k), _ptr(v), code,
+                                _ptr(dev_status), _stream(stream))
+    _check(fn, st)
+    return k, v
+
+
+def sss_attention_q4_workspace_bytes(tokens: int, heads: int, cache: KVCacheQ4, batch: int,
+                                     max_q: int, max_kv: int, table_width: int = 2 ** 31 - 1) -> int:
+    """Workspace bytes of sss_attention_q4 with these sizes (and a block table of any
+    width, if none is given)."""
+    return int(load().sss_attention_q4_workspace_bytes(tokens, heads, cache._ref, table_width, batch,
+                                                       min(max_q, tokens), max_kv))
+
+
+def sss_attention_q4(q, cache: KVCacheQ4, cu_q, kv_len, max_q: int, max_kv: int, block_table,
+                     scale=None, out=None, workspace=None, dev_status=None, stream=None):
+    """sss_attention over a cache in 4 bits, whose pages the block table names; q is
+    float16 or bfloat16.  Returns out [tokens, heads, dim]."""
+    import torch
+
+    fn = "sss_attention_q4"
+    _need_cache(fn, cache, KVCacheQ4)
+    d = cache._desc
+    if scale is None:
+        scale = d.dim ** -0.5
+    if q.dim() != 3 or q.shape[2] != d.dim:
+        raise SssError(fn, 1, "q must be [tokens, heads, dim] of the cache's dim")
+    code = _dtype_code(q.dtype)
+    if code not in (OUT_F16, OUT_BF16):
+        raise SssError(fn, 1, "q must be float16 or bfloat16")
+    tokens, heads, dim = q.shape
+    batch = cu_q.numel() - 1
+    max_q = min(max_q, tokens)  # (any bound will do: no request has more)
+    qs = _rows(fn, "q", q, tokens, heads * dim)
+    if out is None:
+        out = _empty_on(stream, (tokens, heads, dim), q.dtype, q.device)
+    if batch < 0:
+        raise SssError(fn, 1, "cu_q must be [batch + 1]")
+    _need_int32(fn, cu_q=(cu_q, None), kv_len=(kv_len, batch), block_table=(block_table, None))
+    if block_table.dim() != 2 or block_table.shape[0] != batch:
+        raise SssError(fn, 1, "block_table must be [batch, width]")
+    _need(fn, "out", out, q.dtype, tokens * heads * dim)
+    _need(fn, "workspace", workspace, torch.uint8, optional=True)
+    _need_status(fn, dev_status)
+    _on_device(fn, q=q, out=out, workspace=workspace, dev_status=dev_status)
+    width = block_table.shape[1]
+    if workspace is None:
+        need = sss_attention_q4_workspace_bytes(tokens, heads, cache, batch, max_q, max_kv, width)
+        if need > 0:
+            workspace = _empty_on(stream, need, torch.uint8, q.device)
+    ws_bytes = 0 if workspace is None else workspace.numel()
+    st = load().sss_attention_q4(q.data_ptr(), qs, heads, code, cache._ref, cu_q.data_ptr(),
+                                 kv_len.data_ptr(), block_table.data_ptr(), width, batch, tokens,
+                                 max_q, max_kv, scale, out.data_ptr(), _ptr(workspace), ws_bytes,
+                                 _ptr(dev_status), _stream(stream))
+    _check(fn, st)
+    return out
+
+
+# ---------------------------------------------------------------------------
+# pages that several requests hold
+# ---------------------------------------------------------------------------
+
+def _need_table(fn, name, t, rows, width=None):
+    if t.dim() != 2 or t.shape[0] != rows or (width is not None and t.shape[1] != width):
+        raise SssError(fn, 1, f"{name} must be [{rows}, {'width' if width is None else width}]")
+    _need_int32(fn, **{name: (t, None)})
+
+
+def sss_page_fork(parents, past, page_size: int, free_pages, block_table, new_table, new_past, src,
+                  dst, used, dev_status=None, stream=None) -> None:
+    """Rows of a block table from their parents': int32 parents [rows], past [batch], the
+    block table [batch, width] and free_pages to new_table [rows, width], new_past, src
+    and dst [rows] (for sss_page_copy) and used [1]."""
+    fn = "sss_page_fork"
+    rows, batch = parents.numel(), past.numel()
+    _need_table(fn, "block_table", block_table, batch)
+    _need_table(fn, "new_table", new_table, rows, block_table.shape[1])
+    _need_int32(fn, parents=(parents, rows), past=(past, batch), free_pages=(free_pages, None),
+                new_past=(new_past, rows), src=(src, rows), dst=(dst, rows), used=(used, 1))
+    _need_status(fn, dev_status)
+    _on_device(fn, dev_status=dev_status)
+    st = load().sss_page_fork(parents.data_ptr(), rows, past.data_ptr(), batch, page_size,
+                              free_pages.data_ptr(), free_pages.numel(), block_table.data_ptr(),
+                              block_table.shape[1], new_table.data_ptr(), new_past.data_ptr(),
+                              src.data_ptr(), dst.data_ptr(), used.data_ptr(), _ptr(dev_status),
+                              _stream(stream))
+    _check(fn, st)
+
+
+def sss_page_reclaim(block_table, past, page_size: int, free_pages, free_count, new_table=None,
+                     src=None, dst=None, moves=None, dev_status=None, stream=None) -> None:
+    """The pages 0 .. free_pages.numel() - 1 that no row of the block table [batch, width]
+    holds among those of its past[b] tokens, to int32 free_pages (-1 behind them) and
+    free_count [1].  With new_table [batch, width], src and dst [most] and moves [1] held
+    pages move down: src and dst are for sss_page_copy, new_table is the table then."""
+    fn = "sss_page_reclaim"
+    batch = past.numel()
+    _need_table(fn, "block_table", block_table, batch)
+    _need_int32(fn, past=(past, batch), free_pages=(free_pages, None), free_count=(free_count, 1))
+    most = 0
+    if new_table is None:
+        if src is not None or dst is not None or moves is not None:
+            raise SssError(fn, 1, "src, dst and moves are given with new_table")
+    else:
+        _need_table(fn, "new_table", new_table, batch, block_table.shape[1])
+        _need_int32(fn, src=(src, None), dst=(dst, None), moves=(moves, 1))
+        most = src.numel()
+        if dst.numel() != most:
+            raise SssError(fn, 1, "src and dst must be of one size")
+    _need_status(fn, dev_status)
+    _on_device(fn, dev_status=dev_status)
+    st = load().sss_page_reclaim(block_table.data_ptr(), block_table.shape[1], past.data_ptr(), batch,
+                                 page_size, free_pages.numel(), free_pages.data_ptr(),
+                                 free_count.data_ptr(), _ptr(new_table), _ptr(src), _ptr(dst), most,
+                                 _ptr(moves), _ptr(dev_status), _stream(stream))
+    _check(fn, st)
+
+
+def sss_page_copy(caches, src, dst, dev_status=None, stream=None) -> None:
+    """Page src[i] to page dst[i] (int32 [n]; both negative: none) in each of the caches, a
+    KVCache or KVCacheQ4 or a list of them (all layers of a model in one call)."""
+    fn = "sss_page_copy"
+    if isinstance(caches, (KVCache, KVCacheQ4)):
+        caches = [caches]
+    q4 = len(caches) > 0 and isinstance(caches[0], KVCacheQ4)
+    for c in caches:
+        _need_cache(fn, c, KVCacheQ4 if q4 else KVCache)
+    _need_int32(fn, src=(src, None), dst=(dst, src.numel()))
+    _need_status(fn, dev_status)
+    _on_device(fn, dev_status=dev_status)
+    L = load()
+    array = (ctypes.c_void_p * len(caches))(*[c._address for c in caches])
+    st = (L.sss_page_copy_q4 if q4 else L.sss_page_copy)(array, len(caches), src.data_ptr(),
+                                                         dst.data_ptr(), src.numel(),
+                                                         _ptr(dev_status), _stream(stream))
+    _check(fn, st)
