@@ -28,6 +28,24 @@ sss_kv_cache_t staged(const AttnQ4Plan& p, const sss_kv_cache_q4_t& c, int batch
   s.dtype = dtype;
   return s;
 }
+
+// Row tiles of 8 or 16 tokens x heads, and the splits of their keys.
+void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int batch, int max_q, int64_t max_kv) {
+  const int64_t sms = device_sm_count();
+  p.rows = static_cast<int64_t>(group) * max_q <= 8 ? 8 : 16;
+  p.hpt = std::min(group, p.rows);
+  p.tpt = std::min(p.rows / p.hpt, max_q);
+  p.hchunks = (group + p.hpt - 1) / p.hpt;
+  p.one_tile = max_q <= p.tpt;
+  p.tiles = p.one_tile ? batch : std::min(tokens / p.tpt + batch,
+                                          static_cast<int64_t>(batch) * ((max_q + int64_t{p.tpt} - 1) / p.tpt));
+  const int64_t items = std::max<int64_t>(1, p.tiles * kv_heads * p.hchunks);
+  constexpr int64_t kLeast = 128;
+  const int64_t fit = items <= 8 ? 16 : items <= 32 ? 8 : items <= 2 * sms / 4 ? 4 : items <= sms ? 2 : 1;
+  int64_t cluster = std::max<int64_t>(fit, max_kv >= 4096 ? 4 : max_kv >= 2048 ? 2 : 1);
+  while (cluster > 1 && (cluster - 1) * kLeast >= max_kv) cluster /= 2;
+  p.nsplit = cluster;
+}
 }  // namespace
 
 AttnQ4Plan plan_attention_q4(int64_t tokens, int heads, const sss_kv_cache_q4_t& c, int width,
@@ -35,7 +53,9 @@ AttnQ4Plan plan_attention_q4(int64_t tokens, int heads, const sss_kv_cache_q4_t&
   AttnQ4Plan p = {};
   p.pages = static_cast<int>(std::min<int64_t>(width, (max_kv + c.page_size - 1) / c.page_size));
   p.of = plan_attention(tokens, heads, staged(p, c, batch, SSS_OUT_BF16, nullptr), batch, max_q, max_kv);
-  if (p.of.prompt) {
+  if (!p.of.prompt) {
+    plan_rows(p.of, tokens, heads / c.heads, c.heads, batch, max_q, max_kv);
+  } else {
     const size_t bytes = static_cast<size_t>(batch) * p.pages * c.page_size * c.heads * c.dim * 2;
     p.table_at = rounded(p.of.ws_bytes);
     p.k_at = p.table_at + rounded(static_cast<size_t>(batch) * p.pages * 4);
@@ -77,7 +97,16 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
   a.group = heads / c.heads;
   a.table_width = width;
   while ((1 << a.page_shift) < c.page_size) ++a.page_shift;
+  a.hpt = p.of.hpt;
+  a.hchunks = p.of.hchunks;
+  a.hpt_inverse = 65536 / p.of.hpt + 1;
+  a.tpt = p.of.tpt;
+  a.tiles = static_cast<int>(p.of.tiles);
+  a.one_tile = p.of.one_tile ? 1 : 0;
+  a.nsplit = static_cast<int>(p.of.nsplit);
+  a.rows = p.of.rows;
   a.scale_log2 = scale * 1.4426950408889634f;
+  a.stall = (test_stall_mask() & SSS_TEST_STALL_ATTENTION_ROWS) ? 1 : 0;
   return launch_attn_rows_q4(a, q4_cache(c), dtype, c.dim, stream);
 }
 

@@ -1,130 +1,653 @@
-// attn_rows_q4.cu -- attention of few rows over the cache in 4 bits.
+// attn_rows_q4.cu -- attention of few rows (the single tokens, or a few drafted ones, of a
+// decode step) over the cache in 4 bits.
 //
 //   o_i = sum_j p_ij v_j / sum_j p_ij,   p_ij = 2^(c q_i.k_j - m_i),  c = scale log2(e)
 //
-// A warp to a token and head.  A key is D / 8 lanes, one code word each, so a warp takes
-// 256 / D keys at a time and keeps a running maximum, sum and output for each of them.
+// with k_jd = s_jg k'_jd, v_jd = t_jg v'_jd: codes k', v' in -8 .. 7, a scale for each group g of
+// 32 dimensions.  The products run on mma.sync over the codes alone, keys (and then
+// dimensions) as its 16 rows, tokens x heads as its 8 columns:
+//   scores   x_ij = sum_g s_jg (sum_{d in g} q_id k'_jd),  scaled in fp32 group by group;
+//   outputs  o_id = sum_j (p_ij t_jg) v'_jd, with p t rounded to fp16 for the product.
+// A nibble u = code + 8 becomes a 16-bit operand by one AND: in bits 0-3 of a half it is the
+// (subnormal) number u 2^-24, in bits 4-7 u 2^-20, exactly.  For the keys the 8 that are too
+// much are taken off by what the sums start from, -8 times q's sums; for the values by a
+// subtraction, exact as well.  q is made fp16 with a power of two of its row's own (|q'| <
+// 2^15: what is 2^-28 of the row's largest or less is rounded), whatever its type; the odd nibbles' q' is
+// a 16th.  So the type of q and out does not matter inside.
+//
+// Bound by HBM, with the issue slots not far behind: 16 keys and values of a head of 128 are
+// 2304 bytes, which an SM's share of the bandwidth brings in 96 cycles, and four
+// schedulers have 384 issue slots in that time, for about 230 instructions with 8 columns.
+// A block of the cache is one bulk copy into a ring that each warp has for itself, with a
+// barrier for each stage and no other wait in the loop.  The codes lie so that each lane's are
+// vector loads without bank conflicts (the keys' order in a tile, key_slot below, is chosen for
+// that), and that neighbours in an operand are the halves of a word (keys) or one byte
+// permutation apart (values).  The rest is as in attn_rows.cu: 32 steps' table entries
+// read ahead, splits of a tile's keys joined in a cluster in a fixed order.
 #include <algorithm>
 
 #include "attn.cuh"
 #include "kv_q4.cuh"
+#include "tc.cuh"
 
 namespace sss {
 namespace {
 
 constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kStep = kQ4Slots;  // keys of a warp's step
+constexpr int kStages = 8;       // steps in a warp's ring
 
-template <typename T, int D>
-__global__ void __launch_bounds__(32 * kWarps) attn_rows_q4_kernel(const __grid_constant__ AttnArgs a,
-                                                                  const __grid_constant__ Q4Cache c) {
+template <int D, int R, bool CL>
+struct RowsQ4Smem {
+  static constexpr int RING = kStages * Q4Block<D>::kBytes;  // of a warp
+  static constexpr int LD = D + 4;  // of the warps' outputs, which follow
+  static constexpr int RINGS = std::max(kWarps * RING, kWarps * R * LD * 4);
+  // the splits' pieces of the values that this one joins (their number rounded up)
+  static constexpr int TOTAL = RINGS + (CL ? (R * D / 4 + 16) * 16 : 0);
+};
+
+// The slot of a step that is row (or operand column) i of a tile: four slots in order for the
+// even ones, four in reverse for the odd.
+__device__ __forceinline__ int key_slot(int i) {
+  return (i & 8) + ((i & 1) ? 4 + ((i >> 1 & 3) ^ 3) : (i >> 1 & 3));
+}
+
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                        uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// an 8 x 8 matrix of 16-bit values, two of a row to a lane, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// nibble e (0 .. 3) of both halves as subnormal numbers: u 2^-24, or u 2^-20 where e is odd
+__device__ __forceinline__ uint32_t nibbles(uint32_t w, int e) {
+  return (e >= 2 ? w >> 8 : w) & (e & 1 ? 0x00F000F0u : 0x000F000Fu);
+}
+// the same less 8 of that unit
+__device__ __forceinline__ uint32_t codes(uint32_t w, int e) {
+  uint32_t r = nibbles(w, e);
+  asm("sub.rn.f16x2 %0, %0, %1;" : "+r"(r) : "r"(e & 1 ? 0x00800080u : 0x00080008u));
+  return r;
+}
+template <typename V>
+__device__ __forceinline__ void lds(V& v, uint32_t addr);
+template <>
+__device__ __forceinline__ void lds(uint32_t& v, uint32_t addr) {
+  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+}
+template <>
+__device__ __forceinline__ void lds(uint2& v, uint32_t addr) {
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+}
+template <>
+__device__ __forceinline__ void lds(uint4& v, uint32_t addr) {
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ float2 halves(uint32_t w) {
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+
+// Shared memory of another CTA of the cluster, at the address that addr is in this
+// one's; stores into it, whose bytes a barrier there counts.
+__device__ __forceinline__ uint32_t of_peer(uint32_t addr, int rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ void peer_store(uint32_t addr, float v, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.f32 [%0], %1, [%2];" ::"r"(
+                   addr),
+               "f"(v), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void peer_store(uint32_t addr, float4 v, uint32_t bar) {
+  asm volatile(
+      "st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, "
+      "[%5];" ::"r"(addr),
+      "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(bar)
+      : "memory");
+}
+
+// NT tiles of 8 rows (tokens x heads).  CL: the splits of a tile's keys are the CTAs of a
+// cluster.
+template <typename T, int D, int NT, bool CL>
+__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
+    attn_rows_q4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Q4Cache c4) {
+  constexpr int R = 8 * NT;
+  using S = RowsQ4Smem<D, R, CL>;
   using B = Q4Block<D>;
-  constexpr int W = D / 8, KEYS = 32 / W;
-  const int lane = threadIdx.x & 31, w = lane % W, sub = lane / W;
+  constexpr int W = D / 8;      // words of a slot
+  constexpr int KW = W / 4;     // that a lane has of a key's
+  constexpr int VW = W / 8;     // and of a value's
+  constexpr int G = D / 32;     // groups
+  constexpr int PER = 4 / G;    // nibble places to a group
+  extern __shared__ __align__(128) unsigned char smem[];
+  __shared__ float wmax[kWarps][R], wsum[kWarps][R];
+  __shared__ float split_lse[CL ? 16 : 1][R];  // of every split
+  __shared__ uint64_t arrived;                 // what the splits store here
+  __shared__ uint64_t full[kWarps][kStages];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r = lane >> 2, c = lane & 3;  // of the operands' layouts
+  if (lane < kStages) mbar_init(&full[warp][lane], 1);
+  if (CL && threadIdx.x == 0) mbar_init(&arrived, 1);
+  asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  __syncwarp();
+  // another CTA's shared memory exists only once that CTA has started: waited for
+  // before the first store into a peer
+  if constexpr (CL) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  if (row >= static_cast<int64_t>(a.tokens) * a.heads) return;
-  const int t = static_cast<int>(row / a.heads), head = static_cast<int>(row - static_cast<int64_t>(t) * a.heads);
-  const int kh = head / a.group;
-  int lo = 0, hi = a.batch;  // the token's request: the last whose first token is not behind it
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    if (a.cu_q[mid] <= t) lo = mid;
-    else hi = mid;
-  }
+
+  const int z = blockIdx.x, hx = blockIdx.y;
+  const int kh = a.hchunks == 1 ? hx : hx / a.hchunks;
+  const int g0 = (hx - kh * a.hchunks) * a.hpt;
+  const int nh = min(a.hpt, a.group - g0);  // heads of the tile
+  const auto token_of = [&](int row) { return row * a.hpt_inverse >> 16; };
+  const auto leave = [&]() {
+    if constexpr (CL) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  };
+  // the keys go to the splits and their warps 16 at a time in turn
+  const auto key_of = [&](int s) { return kStep * (warp + kWarps * (CL ? z + a.nsplit * s : s)); };
+  const int64_t width = static_cast<int64_t>(a.table_width) << a.page_shift;
+  const auto entry = [&](const int32_t* table, int s) {
+    const int64_t key = kStep * (warp + kWarps * (CL ? z + static_cast<int64_t>(a.nsplit) * s : s));
+    return key < width && key < a.max_kv ? __ldg(table + (key >> a.page_shift)) : 0;
+  };
+  int page = 0;
+  if (a.one_tile && blockIdx.z < a.batch)
+    page = entry(a.table + static_cast<int64_t>(blockIdx.z) * a.table_width, lane);
+  int b, i0;
   uint32_t flags = 0;
-  const AttnRequest rq = attn_request(a, lo, flags);
-  const int i = t - rq.q0;
-  const bool mine = i >= 0 && i < rq.n;
-  const int lim = mine ? attn_limit(rq, i) : 0;
-  const int32_t* table = a.table + static_cast<int64_t>(lo) * a.table_width;
-  float q[8], o[8];
-  float m = -INFINITY, sum = 0.f;
-#pragma unroll
-  for (int n = 0; n < 8; ++n) {
-    q[n] = static_cast<float>(static_cast<const T*>(a.q)[t * a.q_stride + head * D + 2 * W * (n & 3) + W * (n >> 2) + w]);
-    o[n] = 0.f;
+  AttnRequest rq;
+  const bool found = attn_tile(a, blockIdx.z, b, i0, rq, flags);
+  const int nt = found ? min(a.tpt, rq.n - i0) : 0;  // tokens of the tile
+  if (nt <= 0) {
+    if (flags && a.status && warp == 0) atomicOr(a.status, flags);
+    return leave();
   }
-  for (int k0 = 0; k0 < lim; k0 += KEYS) {
-    const int key = k0 + sub;
-    uint32_t kw = 0x88888888u, vw = kw;
-    float ks[8], vs[8];
+  const int lim1 = attn_limit(rq, i0 + nt - 1);
+  const int lim0 = attn_limit(rq, i0);
+  const int steps = (lim1 + kStep - 1) / kStep;
+  // splits with keys
+  const int n = CL ? max(1, min(a.nsplit, (steps + kWarps - 1) / kWarps)) : 1;
+  const bool alone = n == 1;  // the tile has no other split
+  if (CL && alone && z > 0) return leave();
+  const int first = warp + kWarps * z;
+  const int turn = CL ? 31 - __clz(kWarps * a.nsplit) : 2;  // (a cluster is a power of two)
+  static_assert(kWarps == 4, "turn");
+  const int mine = first < steps ? (steps - first - 1 >> turn) + 1 : 0;  // steps of the warp
+  const int32_t* table = a.table + static_cast<int64_t>(b) * a.table_width;
+  const uint32_t ring = smem_u32(smem + warp * S::RING);
+  // each split adds up `per` of the tile's 16-byte pieces: piece x belongs to split x / per
+  constexpr int PIECES = D / 4;  // of a row
+  const int rows = nt * a.hpt;   // (with those of heads that a last group of heads lacks)
+  const int per = CL ? (rows * PIECES + n - 1) / n : 1;
+  const int per_inverse = CL ? (1 << 20) / per + 1 : 1;  // (exact: x < 1024, per <= 512)
+
+  // A step's block into its stage; where the table has no page for it, bit `stage` of `none`
+  // and an empty phase.
+  uint32_t none = 0;
+  const auto issue = [&](int s, int stage) {
+    if (s >= mine) return;
+    if ((s & 31) == 0 && (s > 0 || !a.one_tile)) page = entry(table, s + lane);
+    const int key = key_of(s);
+    const int64_t slot = attn_slot(a, __shfl_sync(0xffffffffu, page, s & 31), key);
+    if (slot < 0) {
+      flags |= SSS_FLAG_INDEX;
+      none |= 1u << stage;
+      if (lane == 0) mbar_arrive(&full[warp][stage]);
+      return;
+    }
+    none &= ~(1u << stage);
+    if (lane == 0) {
+      const char* src = q4_block<D>(c4, slot, kh);
+      mbar_arrive_expect_tx(&full[warp][stage], B::kBytes);
+      asm volatile(
+          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+          "[%3];" ::"r"(ring + stage * B::kBytes),
+          "l"(src), "r"(B::kBytes), "r"(smem_u32(&full[warp][stage]))
+          : "memory");
+    }
+  };
+#pragma unroll 1
+  for (int s = 0; s < kStages; ++s) issue(s, s);
+
+  // q' as operands, what the scores' sums start from, and the rows' scales and limits: of
+  // the accumulators' rows 2 c and 2 c + 1 of each tile
+  uint32_t qf[NT][4][KW];
+  float start[NT][G][2], rscale[NT][2];
+  int lim[NT][2];
 #pragma unroll
-    for (int n = 0; n < 8; ++n) ks[n] = vs[n] = 0.f;
-    if (key < lim) {
-      const int page = table[key >> a.page_shift];
-      const int64_t slot = attn_slot(a, page, key);
-      if (slot < 0) {
-        flags |= SSS_FLAG_INDEX;
+  for (int m = 0; m < NT; ++m) {
+    const int row = 8 * m + r;
+    const int i = token_of(row), g = row - i * a.hpt;
+    const bool in = i < nt && g < nh;
+    const T* src = static_cast<const T*>(a.q) + (rq.q0 + i0 + (in ? i : 0)) * a.q_stride +
+                   (kh * a.group + g0 + (in ? g : 0)) * D;
+    // the lane's dimensions: 2 W e + W h + w for its words w = KW c .. KW c + KW - 1
+    float x[4][2][KW];
+    float top = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t v[KW / 2];
+        const T* at = src + 2 * W * e + W * h + KW * c;
+        if constexpr (KW == 4) {
+          const uint2 u = in ? __ldg(reinterpret_cast<const uint2*>(at)) : make_uint2(0u, 0u);
+          v[0] = u.x;
+          v[1] = u.y;
+        } else {
+          v[0] = in ? __ldg(reinterpret_cast<const uint32_t*>(at)) : 0u;
+        }
+#pragma unroll
+        for (int w = 0; w < KW; ++w) {
+          x[e][h][w] = Pair<T>::value(static_cast<uint16_t>(w & 1 ? v[w / 2] >> 16 : v[w / 2]));
+          top = fmaxf(top, fabsf(x[e][h][w]));
+        }
+      }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // 2^(14 - E) for a largest size of 2^E and more
+    const int E = max(static_cast<int>(__float_as_uint(top) >> 23 & 255u) - 127, -112);
+    const float up = __int_as_float((14 - min(E, 127) + 127) << 23);
+    float sums[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) sums[g] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float f = e & 1 ? up * 0.0625f : up;
+        const __half2 v = __floats2half2_rn(x[e][0][w] * f, x[e][1][w] * f);
+        qf[m][e][w] = *reinterpret_cast<const uint32_t*>(&v);
+        sums[e / PER] += (__low2float(v) + __high2float(v)) * (e & 1 ? 16.f : 1.f);
+      }
+    // 2^(E - 14) of the scale, and the 2^24 of the nibbles'
+    const float rs = fminf(a.scale_log2 * __int_as_float((min(E, 127) - 14 + 127) << 23) * 0x1p24f, 3e38f);
+    const int limit = in ? attn_limit(rq, i0 + i) : 0;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      sums[g] += __shfl_xor_sync(0xffffffffu, sums[g], 1);
+      sums[g] += __shfl_xor_sync(0xffffffffu, sums[g], 2);
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int from = 4 * (2 * c + k);
+#pragma unroll
+      for (int g = 0; g < G; ++g)
+        start[m][g][k] = -0x1p-21f * __shfl_sync(0xffffffffu, sums[g], from);
+      rscale[m][k] = __shfl_sync(0xffffffffu, rs, from);
+      lim[m][k] = __shfl_sync(0xffffffffu, limit, from);
+    }
+  }
+
+  float o[NT][4][VW][4];  // rows 2 c, 2 c + 1 of dimensions 2 W e + w and 2 W e + W + w
+  float mx[NT][2], sum[NT][2];
+#pragma unroll
+  for (int m = 0; m < NT; ++m) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      mx[m][k] = -INFINITY;
+      sum[m][k] = 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int w = 0; w < VW; ++w)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[m][e][w][i] = 0.f;
+  }
+  const int j0 = key_slot(r), j1 = key_slot(r + 8);  // the lane's keys of the scores
+  int stage = 0;
+  uint32_t parity = 0;
+  bool waited = true;
+#pragma unroll 1
+  for (int s = 0; s < mine; ++s) {
+    int abort = 0;
+    waited = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], parity, &abort));
+    if (!waited) break;
+    const uint32_t at = ring + stage * B::kBytes;
+    const int key0 = key_of(s);
+    const bool cut = key0 + kStep > lim0;
+    // codes and scales
+    uint32_t kw[2][KW];
+    uint32_t vw[4][VW];  // of the operand's slots 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+    float ks[2][G], vs[2][G];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int j = e ? j1 : j0;
+      if constexpr (KW == 4) {
+        uint4 v;
+        lds(v, at + B::kK + j * B::kRow + 16 * c);
+        kw[e][0] = v.x; kw[e][1] = v.y; kw[e][2] = v.z; kw[e][3] = v.w;
+        uint2 u;
+        lds(u, at + B::kKS + j * B::kScales);
+        float2 f = halves(u.x);
+        ks[e][0] = f.x; ks[e][1] = f.y;
+        f = halves(u.y);
+        ks[e][2] = f.x; ks[e][3] = f.y;
+        lds(u, at + B::kVS + j * B::kScales);
+        f = halves(u.x);
+        vs[e][0] = f.x; vs[e][1] = f.y;
+        f = halves(u.y);
+        vs[e][2] = f.x; vs[e][3] = f.y;
       } else {
-        const int j = key & 15;
-        const char* b = q4_block<D>(c, slot, kh);
-        kw = reinterpret_cast<const uint32_t*>(b + B::kK + j * B::kRow)[w];
-        vw = reinterpret_cast<const uint32_t*>(b + B::kV + j * B::kRow)[q4_value_word<D>(w, j)];
-        const __half* kss = reinterpret_cast<const __half*>(b + B::kKS + j * B::kScales);
-        const __half* vss = reinterpret_cast<const __half*>(b + B::kVS + j * B::kScales);
+        uint2 v;
+        lds(v, at + B::kK + j * B::kRow + 8 * c);
+        kw[e][0] = v.x; kw[e][1] = v.y;
+        uint32_t u;
+        lds(u, at + B::kKS + j * B::kScales);
+        float2 f = halves(u);
+        ks[e][0] = f.x; ks[e][1] = f.y;
+        lds(u, at + B::kVS + j * B::kScales);
+        f = halves(u);
+        vs[e][0] = f.x; vs[e][1] = f.y;
+      }
+    }
 #pragma unroll
-        for (int n = 0; n < 8; ++n) {
-          const int g = (2 * W * (n & 3) + W * (n >> 2) + w) / 32;
-          ks[n] = __half2float(kss[g]);
-          vs[n] = __half2float(vss[g]);
+    for (int e = 0; e < 4; ++e) {
+      const int j = key_slot(2 * c + (e & 1) + 4 * (e & 2));
+      if constexpr (VW == 2) {
+        uint2 v;
+        lds(v, at + B::kV + j * B::kRow + 8 * (r ^ ((j & 2) << 1)));
+        vw[e][0] = v.x; vw[e][1] = v.y;
+      } else {
+        lds(vw[e][0], at + B::kV + j * B::kRow + 4 * r);
+      }
+    }
+    const bool blank = none >> stage & 1u;
+    __syncwarp();  // the stage is read
+    issue(s + kStages, stage);
+    if (++stage == kStages) {
+      stage = 0;
+      parity ^= 1u;
+    }
+    if (blank) {  // no page: zeros
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int g = 0; g < G; ++g) ks[e][g] = vs[e][g] = 0.f;
+    }
+
+    // scores
+    float x[NT][4];
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[m][i] = 0.f;
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      float acc[NT][4];
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[m][i] = start[m][g][i & 1];
+#pragma unroll
+      for (int e = g * PER; e < g * PER + PER; ++e)
+#pragma unroll
+        for (int w = 0; w < KW; w += 2) {
+          const uint32_t a0 = nibbles(kw[0][w], e), a1 = nibbles(kw[1][w], e);
+          const uint32_t a2 = nibbles(kw[0][w + 1], e), a3 = nibbles(kw[1][w + 1], e);
+#pragma unroll
+          for (int m = 0; m < NT; ++m) mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1]);
+        }
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[m][i] += ks[i >> 1][g] * acc[m][i];
+    }
+    // scale, mask, and raise the maxima where a score passes them
+    bool raise = false;
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[m][i] *= rscale[m][i & 1];
+        if (cut && key0 + (i >> 1 ? j1 : j0) >= lim[m][i & 1]) x[m][i] = -INFINITY;
+        raise = raise || x[m][i] > mx[m][i & 1];
+      }
+    if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float t = fmaxf(fmaxf(x[m][k], x[m][2 + k]), mx[m][k]);
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
+          const float f = t == -INFINITY ? 1.f : ex2(mx[m][k] - t);
+          mx[m][k] = t;
+          sum[m][k] *= f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+#pragma unroll
+            for (int w = 0; w < VW; ++w) {
+              o[m][e][w][k] *= f;
+              o[m][e][w][2 + k] *= f;
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float ref = mx[m][i & 1];
+        x[m][i] = ex2(x[m][i] - (ref == -INFINITY ? 0.f : ref));
+        sum[m][i & 1] += x[m][i];
+      }
+    // outputs
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      uint32_t p[NT][2];
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float t[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            t[k] = x[m][2 * e + k] * vs[e][g];
+            // (what a row does not see may be of any scale)
+            if (cut && key0 + (e ? j1 : j0) >= lim[m][k]) t[k] = 0.f;
+          }
+          p[m][e] = transposed(Pair<__half>::pack(t[0], t[1]));
+        }
+#pragma unroll
+      for (int w = 0; w < VW; ++w) {
+        const uint32_t lo0 = __byte_perm(vw[0][w], vw[1][w], 0x5410), hi0 = __byte_perm(vw[0][w], vw[1][w], 0x7632);
+        const uint32_t lo1 = __byte_perm(vw[2][w], vw[3][w], 0x5410), hi1 = __byte_perm(vw[2][w], vw[3][w], 0x7632);
+#pragma unroll
+        for (int e = g * PER; e < g * PER + PER; ++e) {
+          const uint32_t a0 = codes(lo0, e), a1 = codes(hi0, e), a2 = codes(lo1, e), a3 = codes(hi1, e);
+#pragma unroll
+          for (int m = 0; m < NT; ++m) mma_f16(o[m][e][w], a0, a1, a2, a3, p[m][0], p[m][1]);
         }
       }
     }
-    float x = 0.f;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) x += q[n] * (ks[n] * static_cast<float>(static_cast<int>(kw >> (4 * n) & 15u) - 8));
-#pragma unroll
-    for (int d = W / 2; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
-    if (key >= lim) continue;
-    x *= a.scale_log2;
-    const float top = fmaxf(m, x);
-    const float f = top == -INFINITY ? 1.f : ex2(m - top), p = ex2(x - (top == -INFINITY ? 0.f : top));
-    m = top;
-    sum = sum * f + p;
-#pragma unroll
-    for (int n = 0; n < 8; ++n)
-      o[n] = o[n] * f + p * (vs[n] * static_cast<float>(static_cast<int>(vw >> (4 * n) & 15u) - 8));
   }
-  __syncwarp();
-#pragma unroll
-  for (int d = W; d < 32; d <<= 1) {
-    const float om = __shfl_xor_sync(0xffffffffu, m, d), top = fmaxf(m, om);
-    const float f = top == -INFINITY ? 1.f : ex2(m - top), g = top == -INFINITY ? 1.f : ex2(om - top);
-    sum = sum * f + __shfl_xor_sync(0xffffffffu, sum, d) * g;
-    m = top;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) o[n] = o[n] * f + __shfl_xor_sync(0xffffffffu, o[n], d) * g;
+  if (!waited) {  // what is under way has to land before the ring is used again
+    flags |= SSS_FLAG_TIMEOUT;
+    for (int i = 0; i < kStages; ++i) {
+      int drain = 0;
+      (void)mbar_wait(&full[warp][stage], parity, &drain);
+      if (++stage == kStages) {
+        stage = 0;
+        parity ^= 1u;
+      }
+    }
   }
   if (flags && a.status) atomicOr(a.status, flags);
-  if (!mine || sub != 0) return;
-  const float r = sum == 0.f ? 0.f : 1.f / sum;
+
+  // join the warps
+  constexpr int LD = S::LD;
+  float* part = reinterpret_cast<float*>(smem);
+  __syncthreads();
 #pragma unroll
-  for (int n = 0; n < 8; ++n) {
-    const uint32_t v = Pair<T>::pack(o[n] * r, 0.f);
-    reinterpret_cast<uint16_t*>(a.out)[row * D + 2 * W * (n & 3) + W * (n >> 2) + w] = static_cast<uint16_t>(v);
+  for (int m = 0; m < NT; ++m)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int row = 8 * m + 2 * c + k;
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) sum[m][k] += __shfl_xor_sync(0xffffffffu, sum[m][k], d);
+      if (r == 0) {
+        wmax[warp][row] = mx[m][k];
+        wsum[warp][row] = sum[m][k];
+      }
+      float* dst = part + (warp * R + row) * LD + VW * r;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int w = 0; w < VW; ++w)
+            dst[2 * W * e + W * h + w] = o[m][e][w][2 * h + k] * (e & 1 ? 0x1p20f : 0x1p24f);
+    }
+  __syncthreads();
+  // pieces of 16 bytes; with CL those of a split follow one another in `gather`
+  const uint32_t gather = smem_u32(smem + S::RINGS), lse0 = smem_u32(&split_lse[0][0]);
+  if (CL && !alone) {
+    if (threadIdx.x == 0) {  // from each split this one's pieces and their rows' sums
+      const int end = min(z * per + per, rows * PIECES);
+      const int bytes = (end - z * per) * 16 + ((end - 1) / PIECES - z * per / PIECES + 1) * 4;
+      // (the test hook: 16 bytes that nobody stores)
+      if (z < n) mbar_arrive_expect_tx(&arrived, (z * per < end ? n * bytes : 0) + (a.stall ? 16 : 0));
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  for (int x = threadIdx.x; x < rows * PIECES; x += kThreads) {
+    const int row = x / PIECES, d = 4 * (x % PIECES);
+    const int i = token_of(row), g = row - i * a.hpt;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, wmax[w][row]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float total = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+      const float f = ex2(wmax[w][row] - ref);  // (0 of a warp without keys)
+      const float4 v = *reinterpret_cast<const float4*>(part + (w * R + row) * LD + d);
+      total += f * wsum[w][row];
+      acc.x += f * v.x;
+      acc.y += f * v.y;
+      acc.z += f * v.z;
+      acc.w += f * v.w;
+    }
+    const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
+    acc = make_float4(acc.x * r, acc.y * r, acc.z * r, acc.w * r);
+    const float lse = total == 0.f ? -INFINITY : top + log2f(total);
+    const int64_t at = static_cast<int64_t>(rq.q0 + i0 + i) * a.heads + kh * a.group + g0 + g;
+    if (alone) {
+      const uint2 u = make_uint2(Pair<T>::pack(acc.x, acc.y), Pair<T>::pack(acc.z, acc.w));
+      if (g < nh) *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
+    } else if constexpr (CL) {
+      if (z < n) {
+        const int to = x * per_inverse >> 20;
+        const uint32_t bar = of_peer(smem_u32(&arrived), to);
+        peer_store(of_peer(gather + (z * per + x - to * per) * 16, to), acc, bar);
+        // (the row's pieces belong to a few of the splits: each gets its sum)
+        if (d == 0 || x == to * per) peer_store(of_peer(lse0 + (z * R + row) * 4, to), lse, bar);
+      }
+    }
+  }
+  if constexpr (CL) {
+    if (alone) return leave();
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    bool ok = z < n;  // this CTA has pieces to join
+    if (ok) {
+      int abort = 0;
+      ok = __all_sync(0xffffffffu, mbar_wait(&arrived, 0, &abort));
+      if (!ok && a.status && lane == 0) atomicOr(a.status, SSS_FLAG_TIMEOUT);
+    }
+    // a lane per split and piece (a cluster is a power of two)
+    const int cl = a.nsplit, w = threadIdx.x & (cl - 1);
+    for (int y0 = 0; ok && y0 < per; y0 += kThreads / cl) {
+      const int y = y0 + threadIdx.x / cl, x = z * per + y, row = x / PIECES, d = 4 * (x % PIECES);
+      const int i = token_of(row), g = row - i * a.hpt;
+      const bool in = y < per && row < rows;
+      const float l = in && w < n ? split_lse[w][row] : -INFINITY;
+      float top = l;
+      for (int m = cl / 2; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+      float total = l == -INFINITY ? 0.f : ex2(l - top);
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (in && w < n) {
+        v = *reinterpret_cast<const float4*>(smem + S::RINGS + (w * per + y) * 16);
+        v = make_float4(v.x * total, v.y * total, v.z * total, v.w * total);
+      }
+      for (int m = cl / 2; m > 0; m >>= 1) {
+        total += __shfl_xor_sync(0xffffffffu, total, m);
+        v.x += __shfl_xor_sync(0xffffffffu, v.x, m);
+        v.y += __shfl_xor_sync(0xffffffffu, v.y, m);
+        v.z += __shfl_xor_sync(0xffffffffu, v.z, m);
+        v.w += __shfl_xor_sync(0xffffffffu, v.w, m);
+      }
+      if (!in || w != 0 || g >= nh) continue;
+      const float r = total == 0.f ? 0.f : 1.f / total;
+      const int64_t at = static_cast<int64_t>(rq.q0 + i0 + i) * a.heads + kh * a.group + g0 + g;
+      const uint2 u = make_uint2(Pair<T>::pack(v.x * r, v.y * r), Pair<T>::pack(v.z * r, v.w * r));
+      *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
+    }
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (z < n && !ok) {
+      int drain = 0;
+      (void)mbar_wait(&arrived, 0, &drain);
+    }
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int NT, bool CL>
 cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
+  auto kern = attn_rows_q4_kernel<T, D, NT, CL>;
+  constexpr int smem = RowsQ4Smem<D, 8 * NT, CL>::TOTAL;
+  cudaError_t e = ensure_smem(kern, smem);
+  if (e != cudaSuccess) return e;
+  if (CL && a.nsplit > 8) {
+    e = ensure_large_cluster(kern);
+    if (e != cudaSuccess) return e;
+  }
+  const dim3 grid(a.nsplit, a.kv_heads * a.hchunks, a.tiles);
+  if (grid.y > 65535 || grid.z > 65535) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>(a.tokens) * a.heads + kWarps - 1) / kWarps));
-  cfg.blockDim = dim3(32 * kWarps);
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = a.nsplit;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attn_rows_q4_kernel<T, D>, a, c);
+  cfg.numAttrs = a.nsplit > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, a, c);
+}
+template <typename T, int D>
+cudaError_t tiles(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
+  if (a.nsplit > 1) return a.rows == 8 ? run<T, D, 1, true>(a, c, stream) : run<T, D, 2, true>(a, c, stream);
+  return a.rows == 8 ? run<T, D, 1, false>(a, c, stream) : run<T, D, 2, false>(a, c, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_attn_rows_q4(const AttnArgs& a, const Q4Cache& c, int dtype, int dim, cudaStream_t stream) {
-  if (dtype == SSS_OUT_F16) return dim == 64 ? run<__half, 64>(a, c, stream) : run<__half, 128>(a, c, stream);
-  return dim == 64 ? run<__nv_bfloat16, 64>(a, c, stream) : run<__nv_bfloat16, 128>(a, c, stream);
+  if (dtype == SSS_OUT_F16) return dim == 64 ? tiles<__half, 64>(a, c, stream) : tiles<__half, 128>(a, c, stream);
+  return dim == 64 ? tiles<__nv_bfloat16, 64>(a, c, stream) : tiles<__nv_bfloat16, 128>(a, c, stream);
 }
 
 }  // namespace sss
