@@ -36,7 +36,7 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
 constexpr int kStep = kQ4Slots;  // keys of a warp's step
-constexpr int kStages = 8;       // steps in a warp's ring
+constexpr int kStages = 6;       // steps in a warp's ring
 
 template <int D, int R, bool CL>
 struct RowsQ4Smem {
@@ -53,12 +53,21 @@ __device__ __forceinline__ int key_slot(int i) {
   return (i & 8) + ((i & 1) ? 4 + ((i >> 1 & 3) ^ 3) : (i >> 1 & 3));
 }
 
-__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+// d = A B + (c0, c1) in both of its halves, or d += A B
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                        uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%10,%11,%10,%11};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // an 8 x 8 matrix of 16-bit values, two of a row to a lane, transposed
@@ -195,29 +204,41 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   const int per = CL ? (rows * PIECES + n - 1) / n : 1;
   const int per_inverse = CL ? (1 << 20) / per + 1 : 1;  // (exact: x < 1024, per <= 512)
 
+  // 32 steps' blocks, one to a lane, which issues that step's copy; and the steps among
+  // them that the table has no page for.
+  const char* block = nullptr;
+  uint32_t pageless = 0;
+  const auto look_up = [&](int s) {
+    const int key = key_of(s + lane);
+    const int64_t slot = attn_slot(a, page, key);
+    block = q4_block<D>(c4, slot < 0 ? 0 : slot, kh);
+    pageless = __ballot_sync(0xffffffffu, slot < 0);
+  };
+  if (!a.one_tile) page = entry(table, lane);
+  look_up(0);
   // A step's block into its stage; where the table has no page for it, bit `stage` of `none`
   // and an empty phase.
   uint32_t none = 0;
   const auto issue = [&](int s, int stage) {
     if (s >= mine) return;
-    if ((s & 31) == 0 && (s > 0 || !a.one_tile)) page = entry(table, s + lane);
-    const int key = key_of(s);
-    const int64_t slot = attn_slot(a, __shfl_sync(0xffffffffu, page, s & 31), key);
-    if (slot < 0) {
-      flags |= SSS_FLAG_INDEX;
-      none |= 1u << stage;
-      if (lane == 0) mbar_arrive(&full[warp][stage]);
-      return;
+    if ((s & 31) == 0 && s > 0) {
+      page = entry(table, s + lane);
+      look_up(s);
     }
-    none &= ~(1u << stage);
-    if (lane == 0) {
-      const char* src = q4_block<D>(c4, slot, kh);
-      mbar_arrive_expect_tx(&full[warp][stage], B::kBytes);
-      asm volatile(
-          "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
-          "[%3];" ::"r"(ring + stage * B::kBytes),
-          "l"(src), "r"(B::kBytes), "r"(smem_u32(&full[warp][stage]))
-          : "memory");
+    const uint32_t bad = pageless >> (s & 31) & 1u;
+    none = (none & ~(1u << stage)) | bad << stage;
+    if (lane == (s & 31)) {
+      if (bad) {
+        flags |= SSS_FLAG_INDEX;
+        mbar_arrive(&full[warp][stage]);
+      } else {
+        mbar_arrive_expect_tx(&full[warp][stage], B::kBytes);
+        asm volatile(
+            "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
+            "[%3];" ::"r"(ring + stage * B::kBytes),
+            "l"(block), "r"(B::kBytes), "r"(smem_u32(&full[warp][stage]))
+            : "memory");
+      }
     }
   };
 #pragma unroll 1
@@ -294,13 +315,13 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   }
 
   float o[NT][4][VW][4];  // rows 2 c, 2 c + 1 of dimensions 2 W e + w and 2 W e + W + w
-  float mx[NT][2], sum[NT][2];
+  float mx[NT][2], ref[NT][2], sum[NT][2];  // (ref: mx, or 0 where that is -inf)
 #pragma unroll
   for (int m = 0; m < NT; ++m) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       mx[m][k] = -INFINITY;
-      sum[m][k] = 0.f;
+      ref[m][k] = sum[m][k] = 0.f;
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -384,16 +405,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     // scores
     float x[NT][4];
 #pragma unroll
-    for (int m = 0; m < NT; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[m][i] = 0.f;
-#pragma unroll
     for (int g = 0; g < G; ++g) {
       float acc[NT][4];
-#pragma unroll
-      for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[m][i] = start[m][g][i & 1];
 #pragma unroll
       for (int e = g * PER; e < g * PER + PER; ++e)
 #pragma unroll
@@ -401,23 +414,36 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
           const uint32_t a0 = nibbles(kw[0][w], e), a1 = nibbles(kw[1][w], e);
           const uint32_t a2 = nibbles(kw[0][w + 1], e), a3 = nibbles(kw[1][w + 1], e);
 #pragma unroll
-          for (int m = 0; m < NT; ++m) mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1]);
+          for (int m = 0; m < NT; ++m) {
+            if (e == g * PER && w == 0)
+              mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1], start[m][g][0], start[m][g][1]);
+            else
+              mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1]);
+          }
         }
 #pragma unroll
       for (int m = 0; m < NT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[m][i] += ks[i >> 1][g] * acc[m][i];
+        for (int i = 0; i < 4; ++i)
+          x[m][i] = g == 0 ? ks[i >> 1][g] * acc[m][i] : x[m][i] + ks[i >> 1][g] * acc[m][i];
     }
     // scale, mask, and raise the maxima where a score passes them
     bool raise = false;
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[m][i] *= rscale[m][i & 1];
-        if (cut && key0 + (i >> 1 ? j1 : j0) >= lim[m][i & 1]) x[m][i] = -INFINITY;
-        raise = raise || x[m][i] > mx[m][i & 1];
-      }
+      for (int i = 0; i < 4; ++i) x[m][i] *= rscale[m][i & 1];
+    if (cut) {
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (key0 + (i >> 1 ? j1 : j0) >= lim[m][i & 1]) x[m][i] = -INFINITY;
+    }
+#pragma unroll
+    for (int m = 0; m < NT; ++m)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) raise = raise || x[m][i] > mx[m][i & 1];
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int m = 0; m < NT; ++m)
@@ -428,6 +454,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
           for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
           const float f = t == -INFINITY ? 1.f : ex2(mx[m][k] - t);
           mx[m][k] = t;
+          ref[m][k] = t == -INFINITY ? 0.f : t;
           sum[m][k] *= f;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -442,27 +469,35 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     for (int m = 0; m < NT; ++m)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float ref = mx[m][i & 1];
-        x[m][i] = ex2(x[m][i] - (ref == -INFINITY ? 0.f : ref));
+        x[m][i] = ex2(x[m][i] - ref[m][i & 1]);
         sum[m][i & 1] += x[m][i];
       }
     // outputs
+    uint32_t p[G][NT][2];
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      uint32_t p[NT][2];
+    for (int g = 0; g < G; ++g)
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          p[g][m][e] = Pair<__half>::pack(x[m][2 * e] * vs[e][g], x[m][2 * e + 1] * vs[e][g]);
+    if (cut) {  // what a row does not see may be of any scale
 #pragma unroll
       for (int m = 0; m < NT; ++m)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float t[2];
+          const int key = key0 + (e ? j1 : j0);
+          const uint32_t seen = (key < lim[m][0] ? 0xFFFFu : 0u) | (key < lim[m][1] ? 0xFFFF0000u : 0u);
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            t[k] = x[m][2 * e + k] * vs[e][g];
-            // (what a row does not see may be of any scale)
-            if (cut && key0 + (e ? j1 : j0) >= lim[m][k]) t[k] = 0.f;
-          }
-          p[m][e] = transposed(Pair<__half>::pack(t[0], t[1]));
+          for (int g = 0; g < G; ++g) p[g][m][e] &= seen;
         }
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+#pragma unroll
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) p[g][m][e] = transposed(p[g][m][e]);
 #pragma unroll
       for (int w = 0; w < VW; ++w) {
         const uint32_t lo0 = __byte_perm(vw[0][w], vw[1][w], 0x5410), hi0 = __byte_perm(vw[0][w], vw[1][w], 0x7632);
@@ -471,7 +506,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
         for (int e = g * PER; e < g * PER + PER; ++e) {
           const uint32_t a0 = codes(lo0, e), a1 = codes(hi0, e), a2 = codes(lo1, e), a3 = codes(hi1, e);
 #pragma unroll
-          for (int m = 0; m < NT; ++m) mma_f16(o[m][e][w], a0, a1, a2, a3, p[m][0], p[m][1]);
+          for (int m = 0; m < NT; ++m) mma_f16(o[m][e][w], a0, a1, a2, a3, p[g][m][0], p[g][m][1]);
         }
       }
     }
