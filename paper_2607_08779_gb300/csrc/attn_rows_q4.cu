@@ -35,12 +35,15 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kStep = kQ4Slots;  // keys of a warp's step
-constexpr int kStages = 6;       // steps in a warp's ring
+constexpr int kBlocks = 2;                  // of the cache in a warp's step
+constexpr int kStep = kBlocks * kQ4Slots;   // its keys
+constexpr int kStages = 3;                  // steps in a warp's ring
+constexpr int kAhead = 32 / kBlocks;        // steps whose blocks the lanes hold
 
 template <int D, int R, bool CL>
 struct RowsQ4Smem {
-  static constexpr int RING = kStages * Q4Block<D>::kBytes;  // of a warp
+  static constexpr int STAGE = kBlocks * Q4Block<D>::kBytes;
+  static constexpr int RING = kStages * STAGE;  // of a warp
   static constexpr int LD = D + 4;  // of the warps' outputs, which follow
   static constexpr int RINGS = std::max(kWarps * RING, kWarps * R * LD * 4);
   // the splits' pieces of the values that this one joins (their number rounded up)
@@ -148,7 +151,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   __shared__ uint64_t full[kWarps][kStages];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r = lane >> 2, c = lane & 3;  // of the operands' layouts
-  if (lane < kStages) mbar_init(&full[warp][lane], 1);
+  if (lane < kStages) mbar_init(&full[warp][lane], kBlocks);
   if (CL && threadIdx.x == 0) mbar_init(&arrived, 1);
   asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   __syncwarp();
@@ -166,16 +169,21 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   const auto leave = [&]() {
     if constexpr (CL) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   };
-  // the keys go to the splits and their warps 16 at a time in turn
+  // the keys go to the splits and their warps 32 at a time in turn
   const auto key_of = [&](int s) { return kStep * (warp + kWarps * (CL ? z + a.nsplit * s : s)); };
   const int64_t width = static_cast<int64_t>(a.table_width) << a.page_shift;
+  // the lane's block among those of steps s .. s + kAhead - 1
+  const auto lane_key = [&](int s) {
+    const int64_t t = s + lane / kBlocks;
+    return kStep * (warp + kWarps * (CL ? z + a.nsplit * t : t)) + kQ4Slots * (lane % kBlocks);
+  };
   const auto entry = [&](const int32_t* table, int s) {
-    const int64_t key = kStep * (warp + kWarps * (CL ? z + static_cast<int64_t>(a.nsplit) * s : s));
+    const int64_t key = lane_key(s);
     return key < width && key < a.max_kv ? __ldg(table + (key >> a.page_shift)) : 0;
   };
   int page = 0;
   if (a.one_tile && blockIdx.z < a.batch)
-    page = entry(a.table + static_cast<int64_t>(blockIdx.z) * a.table_width, lane);
+    page = entry(a.table + static_cast<int64_t>(blockIdx.z) * a.table_width, 0);
   int b, i0;
   uint32_t flags = 0;
   AttnRequest rq;
@@ -204,39 +212,42 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   const int per = CL ? (rows * PIECES + n - 1) / n : 1;
   const int per_inverse = CL ? (1 << 20) / per + 1 : 1;  // (exact: x < 1024, per <= 512)
 
-  // 32 steps' blocks, one to a lane, which issues that step's copy; and the steps among
-  // them that the table has no page for.
+  // kAhead steps' blocks, one to a lane, which issues their copies; and which of them are
+  // not there: without keys that a row sees, or without a page in the table.
   const char* block = nullptr;
   uint32_t pageless = 0;
   const auto look_up = [&](int s) {
-    const int key = key_of(s + lane);
-    const int64_t slot = attn_slot(a, page, key);
+    const int64_t key = lane_key(s);
+    const int64_t slot = key < lim1 ? attn_slot(a, page, static_cast<int>(key)) : -1;
+    if (slot < 0 && key < lim1) flags |= SSS_FLAG_INDEX;
     block = q4_block<D>(c4, slot < 0 ? 0 : slot, kh);
     pageless = __ballot_sync(0xffffffffu, slot < 0);
   };
-  if (!a.one_tile) page = entry(table, lane);
+  if (!a.one_tile) page = entry(table, 0);
   look_up(0);
-  // A step's block into its stage; where the table has no page for it, bit `stage` of `none`
-  // and an empty phase.
+  // A step's blocks into its stage; of one that is not there a bit of `none` (kBlocks to a
+  // stage), and only an arrival.
   uint32_t none = 0;
   const auto issue = [&](int s, int stage) {
     if (s >= mine) return;
-    if ((s & 31) == 0 && s > 0) {
-      page = entry(table, s + lane);
+    const int at = s % kAhead;
+    if (at == 0 && s > 0) {
+      page = entry(table, s);
       look_up(s);
     }
-    const uint32_t bad = pageless >> (s & 31) & 1u;
-    none = (none & ~(1u << stage)) | bad << stage;
-    if (lane == (s & 31)) {
-      if (bad) {
-        flags |= SSS_FLAG_INDEX;
-        mbar_arrive(&full[warp][stage]);
+    constexpr uint32_t kAll = (1u << kBlocks) - 1;
+    const uint32_t bad = pageless >> (kBlocks * at) & kAll;
+    none = (none & ~(kAll << (kBlocks * stage))) | bad << (kBlocks * stage);
+    if (lane / kBlocks == at) {
+      uint64_t* bar = &full[warp][stage];
+      if (pageless >> lane & 1u) {
+        mbar_arrive(bar);
       } else {
-        mbar_arrive_expect_tx(&full[warp][stage], B::kBytes);
+        mbar_arrive_expect_tx(bar, B::kBytes);
         asm volatile(
             "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
-            "[%3];" ::"r"(ring + stage * B::kBytes),
-            "l"(block), "r"(B::kBytes), "r"(smem_u32(&full[warp][stage]))
+            "[%3];" ::"r"(ring + stage * S::STAGE + lane % kBlocks * B::kBytes),
+            "l"(block), "r"(B::kBytes), "r"(smem_u32(bar))
             : "memory");
       }
     }
@@ -330,7 +341,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[m][e][w][i] = 0.f;
   }
-  const int j0 = key_slot(r), j1 = key_slot(r + 8);  // the lane's keys of the scores
+  // the lane's keys of the scores are slots j0 and j0 + 8 of a block, of the values v0, v1
+  // and those + 8
+  const int j0 = key_slot(r), v0 = key_slot(2 * c), v1 = key_slot(2 * c + 1);
+  const uint32_t k_at = j0 * B::kRow + 4 * KW * c, s_at = j0 * B::kScales;
+  const uint32_t v0_at = B::kV + v0 * B::kRow + 4 * q4_value_word<D>(VW * r, v0);
+  const uint32_t v1_at = B::kV + v1 * B::kRow + 4 * q4_value_word<D>(VW * r, v1);
   int stage = 0;
   uint32_t parity = 0;
   bool waited = true;
@@ -339,117 +355,105 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     int abort = 0;
     waited = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], parity, &abort));
     if (!waited) break;
-    const uint32_t at = ring + stage * B::kBytes;
+    const uint32_t at = ring + stage * S::STAGE;
     const int key0 = key_of(s);
     const bool cut = key0 + kStep > lim0;
-    // codes and scales
-    uint32_t kw[2][KW];
-    uint32_t vw[4][VW];  // of the operand's slots 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-    float ks[2][G], vs[2][G];
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int j = e ? j1 : j0;
-      if constexpr (KW == 4) {
-        uint4 v;
-        lds(v, at + B::kK + j * B::kRow + 16 * c);
-        kw[e][0] = v.x; kw[e][1] = v.y; kw[e][2] = v.z; kw[e][3] = v.w;
-        uint2 u;
-        lds(u, at + B::kKS + j * B::kScales);
-        float2 f = halves(u.x);
-        ks[e][0] = f.x; ks[e][1] = f.y;
-        f = halves(u.y);
-        ks[e][2] = f.x; ks[e][3] = f.y;
-        lds(u, at + B::kVS + j * B::kScales);
-        f = halves(u.x);
-        vs[e][0] = f.x; vs[e][1] = f.y;
-        f = halves(u.y);
-        vs[e][2] = f.x; vs[e][3] = f.y;
-      } else {
-        uint2 v;
-        lds(v, at + B::kK + j * B::kRow + 8 * c);
-        kw[e][0] = v.x; kw[e][1] = v.y;
-        uint32_t u;
-        lds(u, at + B::kKS + j * B::kScales);
-        float2 f = halves(u);
-        ks[e][0] = f.x; ks[e][1] = f.y;
-        lds(u, at + B::kVS + j * B::kScales);
-        f = halves(u);
-        vs[e][0] = f.x; vs[e][1] = f.y;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int j = key_slot(2 * c + (e & 1) + 4 * (e & 2));
-      if constexpr (VW == 2) {
-        uint2 v;
-        lds(v, at + B::kV + j * B::kRow + 8 * (r ^ ((j & 2) << 1)));
-        vw[e][0] = v.x; vw[e][1] = v.y;
-      } else {
-        lds(vw[e][0], at + B::kV + j * B::kRow + 4 * r);
-      }
-    }
-    const bool blank = none >> stage & 1u;
-    __syncwarp();  // the stage is read
-    issue(s + kStages, stage);
-    if (++stage == kStages) {
-      stage = 0;
-      parity ^= 1u;
-    }
-    if (blank) {  // no page: zeros
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int g = 0; g < G; ++g) ks[e][g] = vs[e][g] = 0.f;
-    }
+    const uint32_t blank = none >> (kBlocks * stage) & ((1u << kBlocks) - 1);
 
     // scores
-    float x[NT][4];
+    float x[kBlocks][NT][4];
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
-      float acc[NT][4];
+    for (int u = 0; u < kBlocks; ++u) {
+      uint32_t kw[2][KW];
+      float ks[2][G];
 #pragma unroll
-      for (int e = g * PER; e < g * PER + PER; ++e)
-#pragma unroll
-        for (int w = 0; w < KW; w += 2) {
-          const uint32_t a0 = nibbles(kw[0][w], e), a1 = nibbles(kw[1][w], e);
-          const uint32_t a2 = nibbles(kw[0][w + 1], e), a3 = nibbles(kw[1][w + 1], e);
-#pragma unroll
-          for (int m = 0; m < NT; ++m) {
-            if (e == g * PER && w == 0)
-              mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1], start[m][g][0], start[m][g][1]);
-            else
-              mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1]);
-          }
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t k = at + u * B::kBytes + B::kK + k_at + e * 8 * B::kRow;
+        const uint32_t f = at + u * B::kBytes + B::kKS + s_at + e * 8 * B::kScales;
+        if constexpr (KW == 4) {
+          uint4 w;
+          lds(w, k);
+          kw[e][0] = w.x; kw[e][1] = w.y; kw[e][2] = w.z; kw[e][3] = w.w;
+          uint2 h;
+          lds(h, f);
+          const float2 lo = halves(h.x), hi = halves(h.y);
+          ks[e][0] = lo.x; ks[e][1] = lo.y; ks[e][2] = hi.x; ks[e][3] = hi.y;
+        } else {
+          uint2 w;
+          lds(w, k);
+          kw[e][0] = w.x; kw[e][1] = w.y;
+          uint32_t h;
+          lds(h, f);
+          const float2 lo = halves(h);
+          ks[e][0] = lo.x; ks[e][1] = lo.y;
         }
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+        float acc[NT][4];
+#pragma unroll
+        for (int e = g * PER; e < g * PER + PER; ++e)
+#pragma unroll
+          for (int w = 0; w < KW; w += 2) {
+            const uint32_t a0 = nibbles(kw[0][w], e), a1 = nibbles(kw[1][w], e);
+            const uint32_t a2 = nibbles(kw[0][w + 1], e), a3 = nibbles(kw[1][w + 1], e);
+#pragma unroll
+            for (int m = 0; m < NT; ++m) {
+              if (e == g * PER && w == 0)
+                mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1], start[m][g][0], start[m][g][1]);
+              else
+                mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1]);
+            }
+          }
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[u][m][i] = g == 0 ? ks[i >> 1][g] * acc[m][i] : x[u][m][i] + ks[i >> 1][g] * acc[m][i];
+      }
+    }
+    // scale, mask, and raise the maxima where a score passes them
+#pragma unroll
+    for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
       for (int m = 0; m < NT; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          x[m][i] = g == 0 ? ks[i >> 1][g] * acc[m][i] : x[m][i] + ks[i >> 1][g] * acc[m][i];
+        for (int i = 0; i < 4; ++i) x[u][m][i] *= rscale[m][i & 1];
+    if (blank) {  // no page: zeros (what the stage holds is of any kind)
+#pragma unroll
+      for (int u = 0; u < kBlocks; ++u)
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (blank >> u & 1u) x[u][m][i] = 0.f;
     }
-    // scale, mask, and raise the maxima where a score passes them
+    if (cut) {
+#pragma unroll
+      for (int u = 0; u < kBlocks; ++u)
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (key0 + kQ4Slots * u + j0 + 8 * (i >> 1) >= lim[m][i & 1]) x[u][m][i] = -INFINITY;
+    }
+    float top[NT][2];
     bool raise = false;
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[m][i] *= rscale[m][i & 1];
-    if (cut) {
+      for (int k = 0; k < 2; ++k) {
+        top[m][k] = fmaxf(x[0][m][k], x[0][m][2 + k]);
 #pragma unroll
-      for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (key0 + (i >> 1 ? j1 : j0) >= lim[m][i & 1]) x[m][i] = -INFINITY;
-    }
-#pragma unroll
-    for (int m = 0; m < NT; ++m)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) raise = raise || x[m][i] > mx[m][i & 1];
+        for (int u = 1; u < kBlocks; ++u) top[m][k] = fmaxf(top[m][k], fmaxf(x[u][m][k], x[u][m][2 + k]));
+        raise = raise || top[m][k] > mx[m][k];
+      }
     if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
       for (int m = 0; m < NT; ++m)
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          float t = fmaxf(fmaxf(x[m][k], x[m][2 + k]), mx[m][k]);
+          float t = fmaxf(top[m][k], mx[m][k]);
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
           const float f = t == -INFINITY ? 1.f : ex2(mx[m][k] - t);
@@ -466,54 +470,90 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
         }
     }
 #pragma unroll
-    for (int m = 0; m < NT; ++m)
+    for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[m][i] = ex2(x[m][i] - ref[m][i & 1]);
-        sum[m][i & 1] += x[m][i];
-      }
+      for (int m = 0; m < NT; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[u][m][i] = ex2(x[u][m][i] - ref[m][i & 1]);
+          sum[m][i & 1] += x[u][m][i];
+        }
     // outputs
-    uint32_t p[G][NT][2];
 #pragma unroll
-    for (int g = 0; g < G; ++g)
+    for (int u = 0; u < kBlocks; ++u) {
+      uint32_t p[G][NT][2];  // p t of the lane's two keys
 #pragma unroll
-      for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-          p[g][m][e] = Pair<__half>::pack(x[m][2 * e] * vs[e][g], x[m][2 * e + 1] * vs[e][g]);
-    if (cut) {  // what a row does not see may be of any scale
-#pragma unroll
-      for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const int key = key0 + (e ? j1 : j0);
-          const uint32_t seen = (key < lim[m][0] ? 0xFFFFu : 0u) | (key < lim[m][1] ? 0xFFFF0000u : 0u);
-#pragma unroll
-          for (int g = 0; g < G; ++g) p[g][m][e] &= seen;
+      for (int e = 0; e < 2; ++e) {
+        const uint32_t f = at + u * B::kBytes + B::kVS + s_at + e * 8 * B::kScales;
+        uint32_t h[G / 2];
+        if constexpr (G == 4) {
+          uint2 w;
+          lds(w, f);
+          h[0] = w.x; h[1] = w.y;
+        } else {
+          lds(h[0], f);
         }
-    }
 #pragma unroll
-    for (int g = 0; g < G; ++g) {
+        for (int g = 0; g < G; ++g) {
+          const float2 t2 = halves(h[g / 2]);
+          const float t = g & 1 ? t2.y : t2.x;
 #pragma unroll
-      for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int e = 0; e < 2; ++e) p[g][m][e] = transposed(p[g][m][e]);
-#pragma unroll
-      for (int w = 0; w < VW; ++w) {
-        const uint32_t lo0 = __byte_perm(vw[0][w], vw[1][w], 0x5410), hi0 = __byte_perm(vw[0][w], vw[1][w], 0x7632);
-        const uint32_t lo1 = __byte_perm(vw[2][w], vw[3][w], 0x5410), hi1 = __byte_perm(vw[2][w], vw[3][w], 0x7632);
-#pragma unroll
-        for (int e = g * PER; e < g * PER + PER; ++e) {
-          const uint32_t a0 = codes(lo0, e), a1 = codes(hi0, e), a2 = codes(lo1, e), a3 = codes(hi1, e);
-#pragma unroll
-          for (int m = 0; m < NT; ++m) mma_f16(o[m][e][w], a0, a1, a2, a3, p[g][m][0], p[g][m][1]);
+          for (int m = 0; m < NT; ++m) p[g][m][e] = Pair<__half>::pack(x[u][m][2 * e] * t, x[u][m][2 * e + 1] * t);
         }
       }
+      if (cut) {  // what a row does not see may be of any scale
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int key = key0 + kQ4Slots * u + j0 + 8 * e;
+            const uint32_t seen = (key < lim[m][0] ? 0xFFFFu : 0u) | (key < lim[m][1] ? 0xFFFF0000u : 0u);
+#pragma unroll
+            for (int g = 0; g < G; ++g) p[g][m][e] &= seen;
+          }
+      }
+      if (blank >> u & 1u) continue;  // (the values are zeros)
+      uint32_t vw[4][VW];  // of the operand's columns 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t v = at + u * B::kBytes + (e & 1 ? v1_at : v0_at) + (e >> 1) * 8 * B::kRow;
+        if constexpr (VW == 2) {
+          uint2 w;
+          lds(w, v);
+          vw[e][0] = w.x; vw[e][1] = w.y;
+        } else {
+          lds(vw[e][0], v);
+        }
+      }
+#pragma unroll
+      for (int g = 0; g < G; ++g) {
+#pragma unroll
+        for (int m = 0; m < NT; ++m)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) p[g][m][e] = transposed(p[g][m][e]);
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+          const uint32_t lo0 = __byte_perm(vw[0][w], vw[1][w], 0x5410), hi0 = __byte_perm(vw[0][w], vw[1][w], 0x7632);
+          const uint32_t lo1 = __byte_perm(vw[2][w], vw[3][w], 0x5410), hi1 = __byte_perm(vw[2][w], vw[3][w], 0x7632);
+#pragma unroll
+          for (int e = g * PER; e < g * PER + PER; ++e) {
+            const uint32_t a0 = codes(lo0, e), a1 = codes(hi0, e), a2 = codes(lo1, e), a3 = codes(hi1, e);
+#pragma unroll
+            for (int m = 0; m < NT; ++m) mma_f16(o[m][e][w], a0, a1, a2, a3, p[g][m][0], p[g][m][1]);
+          }
+        }
+      }
+    }
+    __syncwarp();  // the stage is read
+    issue(s + kStages, stage);
+    if (++stage == kStages) {
+      stage = 0;
+      parity ^= 1u;
     }
   }
   if (!waited) {  // what is under way has to land before the ring is used again
     flags |= SSS_FLAG_TIMEOUT;
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < kStages; ++i) {  // (a stage without copies under way: no harm)
       int drain = 0;
       (void)mbar_wait(&full[warp][stage], parity, &drain);
       if (++stage == kStages) {
