@@ -40,9 +40,17 @@ void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int batch, 
   p.tiles = p.one_tile ? batch : std::min(tokens / p.tpt + batch,
                                           static_cast<int64_t>(batch) * ((max_q + int64_t{p.tpt} - 1) / p.tpt));
   const int64_t items = std::max<int64_t>(1, p.tiles * kv_heads * p.hchunks);
+  // A cluster of as many CTAs as leave them all at work at a time (three an SM), halved until
+  // all but one of them have the 128 keys that its warps take in a step: 4 above 384, 8 above
+  // 896, 16 above 1920 (one request of 500 keys: 4.3 us in fours, 4.8 in eights; of 8192: 8.4 in
+  // sixteens, 10.6 in eights).  More waves of CTAs cost 2 to 5 us each (64 requests of 300 to
+  // 500 keys and 8 key/value heads: 12.7 us whole, 20.4 in pairs; 32 of 256 to 2000: 21.0 us
+  // whole, 17.9 in pairs; 16 of 4000 to 8192: 39.9 in fours, 43.3 in eights), which long and
+  // so as a rule unlike requests are worth (64 of 1000 to 8192: 91 us whole, 81 in pairs, 85
+  // in fours; 16 of 130 to 16384: 43.7 in fours, 38.2 in eights).
   constexpr int64_t kLeast = 128;
-  const int64_t fit = items <= 8 ? 16 : items <= 32 ? 8 : items <= 2 * sms / 4 ? 4 : items <= sms ? 2 : 1;
-  int64_t cluster = std::max<int64_t>(fit, max_kv >= 4096 ? 4 : max_kv >= 2048 ? 2 : 1);
+  int64_t cluster = items <= 8 ? 16 : items <= 32 ? 8 : items <= sms ? 4 : items <= 2 * sms ? 2 : 1;
+  if (max_kv >= 4096) cluster = std::max<int64_t>(cluster, items <= sms && max_kv >= 12288 ? 8 : 2);
   while (cluster > 1 && (cluster - 1) * kLeast >= max_kv) cluster /= 2;
   p.nsplit = cluster;
 }

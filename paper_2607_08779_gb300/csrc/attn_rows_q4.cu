@@ -7,17 +7,24 @@
 // 32 dimensions.  The products run on mma.sync over the codes alone, keys (and then
 // dimensions) as its 16 rows, tokens x heads as its 8 columns:
 //   scores   x_ij = sum_g s_jg (sum_{d in g} q_id k'_jd),  scaled in fp32 group by group;
-//   outputs  o_id = sum_j (p_ij t_jg) v'_jd, with p t rounded to fp16 for the product.
+//   outputs  o_id = sum_j (p_ij t_jg) v'_jd, with p t rounded to fp16 for the product (for
+//            bf16 outputs p is rounded first: the product of two halves is one instruction for
+//            two rows, and an error of 2^-10 at most is a quarter of the output's own).
 // A nibble u = code + 8 becomes a 16-bit operand by one AND: in bits 0-3 of a half it is the
 // (subnormal) number u 2^-24, in bits 4-7 u 2^-20, exactly.  For the keys the 8 that are too
 // much are taken off by what the sums start from, -8 times q's sums; for the values by a
-// subtraction, exact as well.  q is made fp16 with a power of two of its row's own (|q'| <
+// subtraction, exact as well (by a product with constants instead: 237 us against 229, and by
+// numbers 1024 + u: 250).  q is made fp16 with a power of two of its row's own (|q'| <
 // 2^15: what is 2^-28 of the row's largest or less is rounded), whatever its type; the odd nibbles' q' is
-// a 16th.  So the type of q and out does not matter inside.
+// a 16th.  So the type of q and out hardly matters inside.
 //
-// Bound by HBM, with the issue slots not far behind: 16 keys and values of a head of 128 are
-// 2304 bytes, which an SM's share of the bandwidth brings in 96 cycles, and four
-// schedulers have 384 issue slots in that time, for about 230 instructions with 8 columns.
+// Bound by the issue of its instructions, not far from HBM: 16 keys and values of a head of
+// 128 are 2304 bytes, which an SM's share of the bandwidth brings in 96 cycles.  Four
+// schedulers have 384 issue slots in that time; the step takes about 270 with 8 columns, 16 of
+// them products that keep a scheduler for 7 cycles each.  64 requests of 16384 keys (32 heads
+// of 128 over 8): 233 us, 5.2 TB/s, 77 % of the copy rate; the copies without the arithmetic
+// take 170, the arithmetic on pages in L2 229.  What did not help: the next step's scores
+// beside this one's outputs (236), four CTAs an SM with two stages (249), 16 keys a step (262).
 // A block of the cache is one bulk copy into a ring that each warp has for itself, with a
 // barrier for each stage and no other wait in the loop.  The codes lie so that each lane's are
 // vector loads without bank conflicts (the keys' order in a tile, key_slot below, is chosen for
@@ -59,7 +66,7 @@ __device__ __forceinline__ int key_slot(int i) {
 // d = A B + (c0, c1) in both of its halves, or d += A B
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%10,%11,%10,%11};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
@@ -67,7 +74,7 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1,
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
@@ -79,9 +86,11 @@ __device__ __forceinline__ uint32_t transposed(uint32_t v) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// nibble e (0 .. 3) of both halves as subnormal numbers: u 2^-24, or u 2^-20 where e is odd
+// The lower (e = 0, 1) or upper nibble of the lower byte of both halves as subnormal numbers:
+// u 2^-24, or u 2^-20 where e is odd.  (The upper bytes come down by a byte permutation, which
+// costs half of what a shift does.)
 __device__ __forceinline__ uint32_t nibbles(uint32_t w, int e) {
-  return (e >= 2 ? w >> 8 : w) & (e & 1 ? 0x00F000F0u : 0x000F000Fu);
+  return w & (e & 1 ? 0x00F000F0u : 0x000F000Fu);
 }
 // the same less 8 of that unit
 __device__ __forceinline__ uint32_t codes(uint32_t w, int e) {
@@ -90,21 +99,14 @@ __device__ __forceinline__ uint32_t codes(uint32_t w, int e) {
   return r;
 }
 template <typename V>
-__device__ __forceinline__ void lds(V& v, uint32_t addr);
-template <>
-__device__ __forceinline__ void lds(uint32_t& v, uint32_t addr) {
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ void lds(V& v, const unsigned char* at) {
+  v = *reinterpret_cast<const V*>(at);
 }
-template <>
-__device__ __forceinline__ void lds(uint2& v, uint32_t addr) {
-  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
-}
-template <>
-__device__ __forceinline__ void lds(uint4& v, uint32_t addr) {
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(addr)
-               : "memory");
+// both halves of p times the lower or upper half of w
+__device__ __forceinline__ uint32_t times_half(uint32_t p, uint32_t w, bool upper) {
+  const __half2 t = *reinterpret_cast<const __half2*>(&w);
+  const __half2 v = __hmul2(*reinterpret_cast<const __half2*>(&p), upper ? __high2half2(t) : __low2half2(t));
+  return *reinterpret_cast<const uint32_t*>(&v);
 }
 __device__ __forceinline__ float2 halves(uint32_t w) {
   return __half22float2(*reinterpret_cast<const __half2*>(&w));
@@ -205,7 +207,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   static_assert(kWarps == 4, "turn");
   const int mine = first < steps ? (steps - first - 1 >> turn) + 1 : 0;  // steps of the warp
   const int32_t* table = a.table + static_cast<int64_t>(b) * a.table_width;
-  const uint32_t ring = smem_u32(smem + warp * S::RING);
+  unsigned char* ring = smem + warp * S::RING;
   // each split adds up `per` of the tile's 16-byte pieces: piece x belongs to split x / per
   constexpr int PIECES = D / 4;  // of a row
   const int rows = nt * a.hpt;   // (with those of heads that a last group of heads lacks)
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
         mbar_arrive_expect_tx(bar, B::kBytes);
         asm volatile(
             "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, "
-            "[%3];" ::"r"(ring + stage * S::STAGE + lane % kBlocks * B::kBytes),
+            "[%3];" ::"r"(smem_u32(ring) + stage * S::STAGE + lane % kBlocks * B::kBytes),
             "l"(block), "r"(B::kBytes), "r"(smem_u32(bar))
             : "memory");
       }
@@ -355,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     int abort = 0;
     waited = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], parity, &abort));
     if (!waited) break;
-    const uint32_t at = ring + stage * S::STAGE;
+    const unsigned char* at = ring + stage * S::STAGE;
     const int key0 = key_of(s);
     const bool cut = key0 + kStep > lim0;
     const uint32_t blank = none >> (kBlocks * stage) & ((1u << kBlocks) - 1);
@@ -368,8 +370,8 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
       float ks[2][G];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t k = at + u * B::kBytes + B::kK + k_at + e * 8 * B::kRow;
-        const uint32_t f = at + u * B::kBytes + B::kKS + s_at + e * 8 * B::kScales;
+        const unsigned char* k = at + u * B::kBytes + B::kK + k_at + e * 8 * B::kRow;
+        const unsigned char* f = at + u * B::kBytes + B::kKS + s_at + e * 8 * B::kScales;
         if constexpr (KW == 4) {
           uint4 w;
           lds(w, k);
@@ -388,6 +390,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
           ks[e][0] = lo.x; ks[e][1] = lo.y;
         }
       }
+      // bytes 0 and 2 of the words, then 1 and 3
+      uint32_t ku[2][KW];
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int w = 0; w < KW; ++w) ku[e][w] = __byte_perm(kw[e][w], 0u, 0x3311);
 #pragma unroll
       for (int g = 0; g < G; ++g) {
         float acc[NT][4];
@@ -395,8 +403,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
         for (int e = g * PER; e < g * PER + PER; ++e)
 #pragma unroll
           for (int w = 0; w < KW; w += 2) {
-            const uint32_t a0 = nibbles(kw[0][w], e), a1 = nibbles(kw[1][w], e);
-            const uint32_t a2 = nibbles(kw[0][w + 1], e), a3 = nibbles(kw[1][w + 1], e);
+            const uint32_t(&from)[2][KW] = e < 2 ? kw : ku;
+            const uint32_t a0 = nibbles(from[0][w], e), a1 = nibbles(from[1][w], e);
+            const uint32_t a2 = nibbles(from[0][w + 1], e), a3 = nibbles(from[1][w + 1], e);
 #pragma unroll
             for (int m = 0; m < NT; ++m) {
               if (e == g * PER && w == 0)
@@ -484,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
       uint32_t p[G][NT][2];  // p t of the lane's two keys
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t f = at + u * B::kBytes + B::kVS + s_at + e * 8 * B::kScales;
+        const unsigned char* f = at + u * B::kBytes + B::kVS + s_at + e * 8 * B::kScales;
         uint32_t h[G / 2];
         if constexpr (G == 4) {
           uint2 w;
@@ -493,12 +502,21 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
         } else {
           lds(h[0], f);
         }
+        if constexpr (std::is_same<T, __half>::value) {
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-          const float2 t2 = halves(h[g / 2]);
-          const float t = g & 1 ? t2.y : t2.x;
+          for (int g = 0; g < G; ++g) {
+            const float2 t2 = halves(h[g / 2]);
+            const float t = g & 1 ? t2.y : t2.x;
 #pragma unroll
-          for (int m = 0; m < NT; ++m) p[g][m][e] = Pair<__half>::pack(x[u][m][2 * e] * t, x[u][m][2 * e + 1] * t);
+            for (int m = 0; m < NT; ++m) p[g][m][e] = Pair<__half>::pack(x[u][m][2 * e] * t, x[u][m][2 * e + 1] * t);
+          }
+        } else {
+#pragma unroll
+          for (int m = 0; m < NT; ++m) {
+            const uint32_t p2 = Pair<__half>::pack(x[u][m][2 * e], x[u][m][2 * e + 1]);
+#pragma unroll
+            for (int g = 0; g < G; ++g) p[g][m][e] = times_half(p2, h[g / 2], g & 1);
+          }
         }
       }
       if (cut) {  // what a row does not see may be of any scale
@@ -516,7 +534,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
       uint32_t vw[4][VW];  // of the operand's columns 2 c, 2 c + 1, 2 c + 8, 2 c + 9
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const uint32_t v = at + u * B::kBytes + (e & 1 ? v1_at : v0_at) + (e >> 1) * 8 * B::kRow;
+        const unsigned char* v = at + u * B::kBytes + (e & 1 ? v1_at : v0_at) + (e >> 1) * 8 * B::kRow;
         if constexpr (VW == 2) {
           uint2 w;
           lds(w, v);
@@ -533,11 +551,14 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
           for (int e = 0; e < 2; ++e) p[g][m][e] = transposed(p[g][m][e]);
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
-          const uint32_t lo0 = __byte_perm(vw[0][w], vw[1][w], 0x5410), hi0 = __byte_perm(vw[0][w], vw[1][w], 0x7632);
-          const uint32_t lo1 = __byte_perm(vw[2][w], vw[3][w], 0x5410), hi1 = __byte_perm(vw[2][w], vw[3][w], 0x7632);
 #pragma unroll
           for (int e = g * PER; e < g * PER + PER; ++e) {
-            const uint32_t a0 = codes(lo0, e), a1 = codes(hi0, e), a2 = codes(lo1, e), a3 = codes(hi1, e);
+            // neighbours' bytes side by side
+            const uint32_t lo = e < 2 ? 0x5410u : 0x5511u, hi = e < 2 ? 0x7632u : 0x7733u;
+            const uint32_t a0 = codes(__byte_perm(vw[0][w], vw[1][w], lo), e);
+            const uint32_t a1 = codes(__byte_perm(vw[0][w], vw[1][w], hi), e);
+            const uint32_t a2 = codes(__byte_perm(vw[2][w], vw[3][w], lo), e);
+            const uint32_t a3 = codes(__byte_perm(vw[2][w], vw[3][w], hi), e);
 #pragma unroll
             for (int m = 0; m < NT; ++m) mma_f16(o[m][e][w], a0, a1, a2, a3, p[g][m][0], p[g][m][1]);
           }

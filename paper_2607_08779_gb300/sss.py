@@ -4,8 +4,8 @@ Argument marshalling only: every step of the path runs in libsss.so's CUDA
 kernels.  torch supplies device memory and streams.  There is no fallback:
 if the library cannot be built or loaded, these functions raise.
 
-The calls go through ctypes.  Those that a decoding step makes for every layer
-(sss_page_plan, sss_qk_norm_rope, sss_attention) check and pass their usual
+The calls go through ctypes.  Those that a decoding step makes for every layer, and the
+others on its pages and caches (from sss_page_plan on, below) check and pass their usual
 arguments in compiled code (_binding.so, csrc/binding.cpp), which leaves to the
 Python below whatever it does not take, refusals among it: 3 us a call, 9 to 11
 without.  Where that part cannot be built (it needs g++ and Python's headers, the
@@ -241,6 +241,8 @@ class _NoBinding:
         return -1
 
     qk_norm_rope = attention = page_plan
+    kv_store_q4 = kv_fetch_q4 = attention_q4 = page_plan
+    page_fork = page_reclaim = page_copy = page_plan
 
 
 def _load_binding():
@@ -274,7 +276,10 @@ def _binding():
                     m = _NoBinding
                 else:
                     m.init(*[ctypes.cast(f, ctypes.c_void_p).value
-                             for f in (L.sss_page_plan, L.sss_qk_norm_rope, L.sss_attention)])
+                             for f in (L.sss_page_plan, L.sss_qk_norm_rope, L.sss_attention,
+                                       L.sss_kv_store_q4, L.sss_kv_fetch_q4, L.sss_attention_q4,
+                                       L.sss_page_fork, L.sss_page_reclaim, L.sss_page_copy,
+                                       L.sss_page_copy_q4)])
                 _fast = m
     return _fast
 
@@ -1037,6 +1042,10 @@ def sss_kv_store_q4(k, v, cache: KVCacheQ4, slots=None, dev_status=None, stream=
     be strided) into the cache's slots, in 4 bits.  Without slots token t goes to slot t."""
     fn = "sss_kv_store_q4"
     _need_cache(fn, cache, KVCacheQ4)
+    if stream is None:
+        st = (_fast or _binding()).kv_store_q4(k, v, cache._address, slots, dev_status)
+        if st >= 0:
+            return _check(fn, st)
     d = cache._desc
     code = _dtype_code(k.dtype)
     if code is None or v.dtype != k.dtype:
@@ -1057,10 +1066,15 @@ def sss_kv_fetch_q4(cache: KVCacheQ4, slots, k=None, v=None, dtype=None, dev_sta
     """The keys and values [count, heads, dim] that the cache holds in int32 slots [count],
     written to k and v; both are allocated (of dtype, by default float32) where neither is
     given, and one alone is fetched where only it is.  Returns (k, v)."""
-    import torch
-
     fn = "sss_kv_fetch_q4"
     _need_cache(fn, cache, KVCacheQ4)
+    if stream is None and dtype is None and k is not None and v is not None:
+        st = (_fast or _binding()).kv_fetch_q4(cache._address, slots, k, v, dev_status)
+        if st >= 0:
+            _check(fn, st)
+            return k, v
+    import torch
+
     d = cache._desc
     _need_int32(fn, slots=(slots, None))
     shape = (slots.numel(), d.heads, d.dim)
@@ -1092,13 +1106,20 @@ def sss_attention_q4(q, cache: KVCacheQ4, cu_q, kv_len, max_q: int, max_kv: int,
                      scale=None, out=None, workspace=None, dev_status=None, stream=None):
     """sss_attention over a cache in 4 bits, whose pages the block table names; q is
     float16 or bfloat16.  Returns out [tokens, heads, dim]."""
-    import torch
-
     fn = "sss_attention_q4"
     _need_cache(fn, cache, KVCacheQ4)
     d = cache._desc
     if scale is None:
         scale = d.dim ** -0.5
+    if stream is None and out is not None:
+        st = (_fast or _binding()).attention_q4(q, cache._address, cu_q, kv_len, max_q, max_kv,
+                                                block_table, scale, out, workspace, dev_status)
+        # (a workspace that was not given is allocated below)
+        if st >= 0 and not (st == 5 and workspace is None):
+            _check(fn, st)
+            return out
+    import torch
+
     if q.dim() != 3 or q.shape[2] != d.dim:
         raise SssError(fn, 1, "q must be [tokens, heads, dim] of the cache's dim")
     code = _dtype_code(q.dtype)
@@ -1149,6 +1170,11 @@ def sss_page_fork(parents, past, page_size: int, free_pages, block_table, new_ta
     block table [batch, width] and free_pages to new_table [rows, width], new_past, src
     and dst [rows] (for sss_page_copy) and used [1]."""
     fn = "sss_page_fork"
+    if stream is None:
+        st = (_fast or _binding()).page_fork(parents, past, page_size, free_pages, block_table,
+                                             new_table, new_past, src, dst, used, dev_status)
+        if st >= 0:
+            return _check(fn, st)
     rows, batch = parents.numel(), past.numel()
     _need_table(fn, "block_table", block_table, batch)
     _need_table(fn, "new_table", new_table, rows, block_table.shape[1])
@@ -1171,6 +1197,11 @@ def sss_page_reclaim(block_table, past, page_size: int, free_pages, free_count, 
     free_count [1].  With new_table [batch, width], src and dst [most] and moves [1] held
     pages move down: src and dst are for sss_page_copy, new_table is the table then."""
     fn = "sss_page_reclaim"
+    if stream is None:
+        st = (_fast or _binding()).page_reclaim(block_table, past, page_size, free_pages, free_count,
+                                                new_table, src, dst, moves, dev_status)
+        if st >= 0:
+            return _check(fn, st)
     batch = past.numel()
     _need_table(fn, "block_table", block_table, batch)
     _need_int32(fn, past=(past, batch), free_pages=(free_pages, None), free_count=(free_count, 1))
@@ -1200,6 +1231,10 @@ def sss_page_copy(caches, src, dst, dev_status=None, stream=None) -> None:
     if isinstance(caches, (KVCache, KVCacheQ4)):
         caches = [caches]
     q4 = len(caches) > 0 and isinstance(caches[0], KVCacheQ4)
+    if stream is None and caches and (q4 or isinstance(caches[0], KVCache)):
+        st = (_fast or _binding()).page_copy(caches, q4, src, dst, dev_status)
+        if st >= 0:
+            return _check(fn, st)
     for c in caches:
         _need_cache(fn, c, KVCacheQ4 if q4 else KVCache)
     _need_int32(fn, src=(src, None), dst=(dst, src.numel()))

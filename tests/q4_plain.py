@@ -91,10 +91,14 @@ def bound_rows(w, dtype, dim, max_kv):
     row's largest) with codes of at most 15, less 8 times q's sums, added in fp32 (dim + 16
     roundings of 2^-23 of the sizes, which truncation is within), scaled and raised to a power; p times
     the scale is rounded to fp16, by 2^-25 at most below its normal range (times a code, over
-    a sum of 1 at least, for every key: 2^-22 each); the output once."""
-    u, h = UNIT[dtype], 2.0 ** -11
+    a sum of 1 at least, for every key: 2^-22 each); the output once.  For bf16 p is rounded to
+    fp16 before as well: (1 + 2^-11)^2 <= 1 + 2^-10 + 2^-22, and below p's normal range 2^-25
+    times the value, of which 2^-25 times its sum is at most 2^-25 of the largest for every key."""
+    u = UNIT[dtype]
+    h = 2.0 ** -11 if dtype is torch.float16 else 2.0 ** -10 + 2.0 ** -22
+    least = 0.0 if dtype is torch.float16 else max_kv * 2.0 ** -25 * 8 * w["most"][..., None]
     e = 2 * (dim + 16) * 2.0 ** -23 * 24 * w["coded"][..., None] + max_kv * 2.0 ** -22 + 2.0 ** -18
-    return u * np.abs(w["out"]) + (h + e) * (1 + u) * w["size"] + max_kv * 2.0 ** -22 + 2.0 ** -24
+    return u * np.abs(w["out"]) + (h + e) * (1 + u) * w["size"] + max_kv * 2.0 ** -22 + least + 2.0 ** -24
 
 
 def bound_many(w, dtype, dim, max_kv):
