@@ -20,7 +20,7 @@ namespace {
 // row's entries read once and written once).  As in page_plan.cu one launch without a
 // grid-wide wait: every CTA looks through all rows by itself, kForkThreads at a time, and
 // writes its share of the table.  Whether a parent was met in earlier chunks is a bit in
-// shared memory; within the chunk a row looks at those before it.
+// shared memory; within the chunk the warps look in turn, so that a row finds those before it.
 // ---------------------------------------------------------------------------
 
 constexpr int kForkThreads = 256;
@@ -78,12 +78,14 @@ __global__ void __launch_bounds__(kForkThreads) page_fork_kernel(const __grid_co
     }
     __syncthreads();  // (the chunk before is read)
     parent_of[tid] = parent;
-    __syncthreads();
     // is this the parent's first row?
-    bool first = true;
-    if (parent >= 0) {
-      first = (met[parent >> 5] >> (parent & 31) & 1u) == 0;
-      for (int i = 0; i < tid; ++i) first = first && parent_of[i] != parent;
+    bool first = (__match_any_sync(0xffffffffu, parent) & ((1u << lane) - 1)) == 0;
+    for (int w = 0; w < kWarps && r0 + 32 * w < a.rows; ++w) {
+      if (w == warp && parent >= 0) {
+        first = first && (met[parent >> 5] >> (parent & 31) & 1u) == 0;
+        if (first) atomicOr(&met[parent >> 5], 1u << (parent & 31));
+      }
+      __syncthreads();
     }
     const bool open = (past & (P - 1)) != 0;  // the last page is partly filled
     bool take = parent >= 0 && open && !first;
@@ -99,7 +101,6 @@ __global__ void __launch_bounds__(kForkThreads) page_fork_kernel(const __grid_co
     const int upto = warp_sum_to(take ? 1 : 0, lane);
     if (lane == 31) warp_takes[warp] = upto;
     __syncthreads();
-    if (parent >= 0) atomicOr(&met[parent >> 5], 1u << (parent & 31));
     int at = taken + upto - 1;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(kForkThreads) page_fork_kernel(const __grid_co
 // ---------------------------------------------------------------------------
 
 constexpr int kMapThreads = 1024;
-constexpr int kMapCtas = 8;
+constexpr int kMapCtas = 16;
 constexpr int kSpan = 8;  // words of the map to one running count
 
 struct MapArgs {
@@ -196,33 +197,34 @@ __device__ __forceinline__ int held_entries(const MapArgs& a, int b, uint32_t& f
 }
 
 __global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_constant__ MapArgs a) {
-  extern __shared__ uint32_t map[];  // [words], then the counts [spans + 1]
+  extern __shared__ __align__(16) uint32_t map[];  // [words], then the counts [spans] and [words]
   __shared__ int warp_held[32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ctas = gridDim.x, me = blockIdx.x;  // (one cluster)
   const int spans = (a.pages + 32 * kSpan - 1) / (32 * kSpan), words = spans * kSpan;
   int* count = reinterpret_cast<int*>(map + words);
+  uint8_t* in_span = reinterpret_cast<uint8_t*>(count + spans);  // of each word, from its span's first
   uint32_t flags = 0;
   for (int i = tid; i < words; i += kMapThreads) map[i] = 0;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __syncthreads();
-  // the rows' entries, a warp to a piece of 256
-  constexpr int kWarps = kMapThreads / 32;
-  const int pieces = (a.width + 255) / 256;
+  // the rows' entries, a warp to a piece of them
+  constexpr int kWarps = kMapThreads / 32, kPiece = 128;
+  const int pieces = (a.width + kPiece - 1) / kPiece;
   const int64_t items = static_cast<int64_t>(a.batch) * pieces;
   for (int64_t i = static_cast<int64_t>(me) * kWarps + warp; i < items; i += static_cast<int64_t>(ctas) * kWarps) {
-    const int b = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(b) * pieces) * 256;
+    const int b = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(b) * pieces) * kPiece;
     const int held = held_entries(a, b, flags);
     const int32_t* row = a.table + static_cast<int64_t>(b) * a.width;
-    int32_t v[8];
+    int32_t v[kPiece / 32];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kPiece / 32; ++k) {
       const int c = c0 + 32 * k + lane;
       v[k] = c < held ? row[c] : 0;
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
+    for (int k = 0; k < kPiece / 32; ++k) {
       if (c0 + 32 * k + lane >= held) continue;
       if (v[k] < 0 || v[k] >= a.pages) flags |= SSS_FLAG_INDEX;
       else atomicOr(&map[v[k] >> 5], 1u << (v[k] & 31));
@@ -232,8 +234,11 @@ __global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_c
     cluster_meet();
     const int slice = (words + ctas - 1) / ctas;
     for (int i = me * slice + tid; i < min(words, (me + 1) * slice); i += kMapThreads) {
-      uint32_t v = 0;
-      for (int c = 0; c < ctas; ++c) v |= peer_word(map + i, c);
+      uint32_t v = 0, of[kMapCtas];
+#pragma unroll
+      for (int c = 0; c < kMapCtas; ++c) of[c] = c < ctas ? peer_word(map + i, c) : 0u;
+#pragma unroll
+      for (int c = 0; c < kMapCtas; ++c) v |= of[c];
       map[i] = v;
     }
     cluster_meet();
@@ -248,7 +253,10 @@ __global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_c
     int n = 0;
     if (s < spans)
 #pragma unroll
-      for (int w = 0; w < kSpan; ++w) n += __popc(map[s * kSpan + w]);
+      for (int w = 0; w < kSpan; ++w) {
+        in_span[s * kSpan + w] = static_cast<uint8_t>(n);  // (224 at most)
+        n += __popc(map[s * kSpan + w]);
+      }
     const int upto = warp_sum_to(n, lane);
     if (lane == 31) warp_held[warp] = upto;
     __syncthreads();
@@ -260,34 +268,37 @@ __global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_c
     __syncthreads();
   }
   const auto rank_of = [&](int x) {  // held pages below x
-    const int w = x >> 5, s = w / kSpan;
-    int n = count[s] + __popc(map[w] & ((1u << (x & 31)) - 1));
-    for (int i = s * kSpan; i < w; ++i) n += __popc(map[i]);
-    return n;
+    const int w = x >> 5;
+    return count[w / kSpan] + in_span[w] + __popc(map[w] & ((1u << (x & 31)) - 1));
   };
   // moves: as many as there are free pages below m
   int k = 0;
   if (a.moves && m < a.pages) k = min(a.most, m - rank_of(m));
-  // the lists, a warp to a word
-  for (int w = me * kWarps + warp; w < (a.pages + 31) / 32; w += ctas * kWarps) {
-    const int x = 32 * w + lane;
-    if (x >= a.pages) continue;
-    const bool is_held = map[w] >> lane & 1u;
-    const int rk = rank_of(x);
-    int pos = -1;
-    if (is_held) {
-      const int i = m - 1 - rk;
-      if (i < k) {
-        a.src[i] = x;
-        pos = rk - (m - k) + (x - rk) - k;
+  // the lists, a warp to a span
+  for (int s = me * kWarps + warp; s < spans; s += ctas * kWarps) {
+    int below = count[s];
+#pragma unroll
+    for (int i = 0; i < kSpan; ++i) {
+      const uint32_t bits = map[s * kSpan + i];
+      const int x = 32 * (s * kSpan + i) + lane;
+      const int rk = below + __popc(bits & ((1u << lane) - 1));
+      below += __popc(bits);
+      if (x >= a.pages) continue;
+      int pos = -1;
+      if (bits >> lane & 1u) {
+        const int j = m - 1 - rk;
+        if (j < k) {
+          a.src[j] = x;
+          pos = rk - (m - k) + (x - rk) - k;
+        }
+      } else {
+        const int j = x - rk;
+        if (j < k) a.dst[j] = x;
+        else pos = j - k + max(0, rk - (m - k));
       }
-    } else {
-      const int i = x - rk;
-      if (i < k) a.dst[i] = x;
-      else pos = i - k + max(0, rk - (m - k));
+      if (pos >= 0) a.free_pages[pos] = x;
+      if (x >= a.pages - m) a.free_pages[x] = -1;
     }
-    if (pos >= 0) a.free_pages[pos] = x;
-    if (x >= a.pages - m) a.free_pages[x] = -1;
   }
   if (me == 0 && tid == 0) {
     *a.free_count = a.pages - m;
@@ -295,24 +306,28 @@ __global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_c
   }
   if (a.moves) {
     for (int i = k + me * kMapThreads + tid; i < a.most; i += ctas * kMapThreads) a.src[i] = a.dst[i] = -1;
-    // the moves' destinations, of all CTAs
+    // the moves of all CTAs; pages from the last one's source on are moved
     if (ctas > 1) cluster_meet();
     else __syncthreads();
+    const int lowest = k > 0 ? __ldcg(a.src + k - 1) : INT32_MAX;
     for (int64_t i = static_cast<int64_t>(me) * kWarps + warp; i < items; i += static_cast<int64_t>(ctas) * kWarps) {
-      const int b = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(b) * pieces) * 256;
+      const int b = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(b) * pieces) * kPiece;
       uint32_t said = 0;
       const int held = held_entries(a, b, said);
       const int64_t at = static_cast<int64_t>(b) * a.width;
+      int32_t v[kPiece / 32];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (int e = 0; e < kPiece / 32; ++e) {
         const int c = c0 + 32 * e + lane;
-        if (c >= held) continue;
-        int32_t v = a.table[at + c];
-        if (v >= 0 && v < a.pages) {
-          const int j = m - 1 - rank_of(v);
-          if (j < k) v = *static_cast<volatile int32_t*>(a.dst + j);
-        }
-        a.new_table[at + c] = v;
+        v[e] = c < held ? a.table[at + c] : -1;
+      }
+#pragma unroll
+      for (int e = 0; e < kPiece / 32; ++e)
+        if (v[e] >= lowest && v[e] < a.pages) v[e] = __ldcg(a.dst + (m - 1 - rank_of(v[e])));
+#pragma unroll
+      for (int e = 0; e < kPiece / 32; ++e) {
+        const int c = c0 + 32 * e + lane;
+        if (c < held) a.new_table[at + c] = v[e];
       }
     }
   }
@@ -430,13 +445,17 @@ cudaError_t launch_page_reclaim(const int32_t* table, int width, const int32_t* 
   const MapArgs a = {table, past, free_pages, free_count, new_table, src, dst, moves,
                      status, batch, width, shift_of(page_size), pages, most};
   const int spans = (pages + 32 * kSpan - 1) / (32 * kSpan);
-  const int smem = (spans * kSpan + spans) * 4;
-  cudaError_t e = ensure_smem(page_map_kernel, (kMaxMapPages / 32 + kMaxMapPages / (32 * kSpan)) * 4);
+  const int smem = spans * (kSpan * 4 + 4 + kSpan);
+  cudaError_t e = ensure_smem(page_map_kernel, kMaxMapPages / (32 * kSpan) * (kSpan * 4 + 4 + kSpan));
   if (e != cudaSuccess) return e;
   // a CTA for each two rounds of its warps over the table or the map
-  const int64_t work = std::max<int64_t>(static_cast<int64_t>(batch) * ((width + 255) / 256), pages / 64);
+  const int64_t work = std::max<int64_t>(static_cast<int64_t>(batch) * ((width + 127) / 128), spans);
   int ctas = 1;
-  while (ctas < kMapCtas && work > ctas * 64) ctas *= 2;
+  while (ctas < kMapCtas && work > ctas * 32) ctas *= 2;
+  if (ctas > 8) {
+    e = ensure_large_cluster(page_map_kernel);
+    if (e != cudaSuccess) return e;
+  }
   return launch(page_map_kernel, a, ctas, kMapThreads, smem, ctas, stream);
 }
 
