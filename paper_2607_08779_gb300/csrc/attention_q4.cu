@@ -30,7 +30,8 @@ sss_kv_cache_t staged(const AttnQ4Plan& p, const sss_kv_cache_q4_t& c, int batch
 }
 
 // Row tiles of 8 or 16 tokens x heads, and the splits of their keys.
-void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int batch, int max_q, int64_t max_kv) {
+void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int dim, int batch,
+               int max_q, int64_t max_kv) {
   const int64_t sms = device_sm_count();
   p.rows = static_cast<int64_t>(group) * max_q <= 8 ? 8 : 16;
   p.hpt = std::min(group, p.rows);
@@ -53,6 +54,22 @@ void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int batch, 
   if (max_kv >= 4096) cluster = std::max<int64_t>(cluster, items <= sms && max_kv >= 12288 ? 8 : 2);
   while (cluster > 1 && (cluster - 1) * kLeast >= max_kv) cluster /= 2;
   p.nsplit = cluster;
+  // Long requests in chunks of 1024 to 2048 keys, about 256 CTAs of them or more, joined by a
+  // second kernel (2.5 us): no cluster then waits for room on one part of the chip, and lengths
+  // that differ even out (16 requests of 130 to 16384 keys and 64 heads: 37.5 us in clusters,
+  // 33.0 in chunks; 64 of 12000 to 16384: 209 and 201; one of 32768: 21.4 and 15.4; 20 of 400 to
+  // 3000: 19.4 and 25.7).  Where the keys take half the time (heads of 64) or tiles are fewer at
+  // a time (16 rows) from twice that length on.
+  const int64_t chunk = std::min<int64_t>(2048, std::max<int64_t>(1024, (max_kv * items / 256 + 127) / 128 * 128));
+  const int64_t least = chunk * (p.rows == 8 && dim == 128 ? 4 : 8);
+  if (max_kv >= least && max_kv * items >= 1024 * 256 && items <= 1024) {
+    p.chunk = chunk;
+    p.nsplit = (max_kv + chunk - 1) / chunk;
+    p.join = true;
+    const size_t rows = static_cast<size_t>(p.nsplit) * tokens * group * kv_heads;
+    p.lse_at = rows * dim * 4;
+    p.ws_bytes = p.lse_at + rows * 4;
+  }
 }
 }  // namespace
 
@@ -60,10 +77,14 @@ AttnQ4Plan plan_attention_q4(int64_t tokens, int heads, const sss_kv_cache_q4_t&
                              int batch, int max_q, int64_t max_kv) {
   AttnQ4Plan p = {};
   p.pages = static_cast<int>(std::min<int64_t>(width, (max_kv + c.page_size - 1) / c.page_size));
-  p.of = plan_attention(tokens, heads, staged(p, c, batch, SSS_OUT_BF16, nullptr), batch, max_q, max_kv);
-  if (!p.of.prompt) {
-    plan_rows(p.of, tokens, heads / c.heads, c.heads, batch, max_q, max_kv);
+  // Four row tiles read the cache four times, mostly in L2; the copy is written and read at
+  // 2 bytes a value.
+  const int group = heads / c.heads;
+  if (static_cast<int64_t>(group) * max_q <= 64 || max_q == 1 || p.pages == 0) {
+    plan_rows(p.of, tokens, group, c.heads, c.dim, batch, max_q, max_kv);
+    p.ws_bytes = p.of.ws_bytes;
   } else {
+    p.of = plan_attention(tokens, heads, staged(p, c, batch, SSS_OUT_BF16, nullptr), batch, max_q, max_kv);
     const size_t bytes = static_cast<size_t>(batch) * p.pages * c.page_size * c.heads * c.dim * 2;
     p.table_at = rounded(p.of.ws_bytes);
     p.k_at = p.table_at + rounded(static_cast<size_t>(batch) * p.pages * 4);
@@ -112,10 +133,14 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
   a.tiles = static_cast<int>(p.of.tiles);
   a.one_tile = p.of.one_tile ? 1 : 0;
   a.nsplit = static_cast<int>(p.of.nsplit);
+  a.chunk = static_cast<int>(p.of.chunk);
+  a.part = static_cast<float*>(workspace);
+  a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.of.lse_at);
   a.rows = p.of.rows;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.stall = (test_stall_mask() & SSS_TEST_STALL_ATTENTION_ROWS) ? 1 : 0;
-  return launch_attn_rows_q4(a, q4_cache(c), dtype, c.dim, stream);
+  const cudaError_t e = launch_attn_rows_q4(a, q4_cache(c), dtype, c.dim, stream);
+  return e == cudaSuccess && p.of.join ? launch_attn_join(a, dtype, c.dim, stream) : e;
 }
 
 }  // namespace sss

@@ -47,7 +47,7 @@ constexpr int kStep = kBlocks * kQ4Slots;   // its keys
 constexpr int kStages = 3;                  // steps in a warp's ring
 constexpr int kAhead = 32 / kBlocks;        // steps whose blocks the lanes hold
 
-template <int D, int R, bool CL>
+template <int D, int R, bool CL>  // (CL: joined in a cluster)
 struct RowsQ4Smem {
   static constexpr int STAGE = kBlocks * Q4Block<D>::kBytes;
   static constexpr int RING = kStages * STAGE;  // of a warp
@@ -133,12 +133,16 @@ __device__ __forceinline__ void peer_store(uint32_t addr, float4 v, uint32_t bar
       : "memory");
 }
 
-// NT tiles of 8 rows (tokens x heads).  CL: the splits of a tile's keys are the CTAs of a
-// cluster.
-template <typename T, int D, int NT, bool CL>
+// How a tile's keys are split over CTAs: not; over those of a cluster, in turn, which join them
+// there; or in chunks, whose results attn_join_kernel joins.
+enum Split { kWhole, kCluster, kChunks };
+
+// NT tiles of 8 rows (tokens x heads).
+template <typename T, int D, int NT, Split SPLIT>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     attn_rows_q4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Q4Cache c4) {
   constexpr int R = 8 * NT;
+  constexpr bool CL = SPLIT == kCluster;
   using S = RowsQ4Smem<D, R, CL>;
   using B = Q4Block<D>;
   constexpr int W = D / 8;      // words of a slot
@@ -171,13 +175,14 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   const auto leave = [&]() {
     if constexpr (CL) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   };
-  // the keys go to the splits and their warps 32 at a time in turn
-  const auto key_of = [&](int s) { return kStep * (warp + kWarps * (CL ? z + a.nsplit * s : s)); };
+  // the keys go to the splits of a cluster and their warps 32 at a time in turn
+  const int chunk0 = SPLIT == kChunks ? z * a.chunk : 0;
+  const auto key_of = [&](int s) { return chunk0 + kStep * (warp + kWarps * (CL ? z + a.nsplit * s : s)); };
   const int64_t width = static_cast<int64_t>(a.table_width) << a.page_shift;
   // the lane's block among those of steps s .. s + kAhead - 1
   const auto lane_key = [&](int s) {
     const int64_t t = s + lane / kBlocks;
-    return kStep * (warp + kWarps * (CL ? z + a.nsplit * t : t)) + kQ4Slots * (lane % kBlocks);
+    return chunk0 + kStep * (warp + kWarps * (CL ? z + a.nsplit * t : t)) + kQ4Slots * (lane % kBlocks);
   };
   const auto entry = [&](const int32_t* table, int s) {
     const int64_t key = lane_key(s);
@@ -197,12 +202,14 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   }
   const int lim1 = attn_limit(rq, i0 + nt - 1);
   const int lim0 = attn_limit(rq, i0);
-  const int steps = (lim1 + kStep - 1) / kStep;
+  if (SPLIT == kChunks && z > 0 && chunk0 >= lim1) return;
+  const int keys = SPLIT == kChunks ? min(a.chunk, lim1 - chunk0) : lim1;  // of the CTA's splits
+  const int steps = (keys + kStep - 1) / kStep;
   // splits with keys
   const int n = CL ? max(1, min(a.nsplit, (steps + kWarps - 1) / kWarps)) : 1;
-  const bool alone = n == 1;  // the tile has no other split
+  const bool alone = SPLIT == kChunks ? lim1 <= a.chunk : n == 1;  // the tile has no other split
   if (CL && alone && z > 0) return leave();
-  const int first = warp + kWarps * z;
+  const int first = CL ? warp + kWarps * z : warp;
   const int turn = CL ? 31 - __clz(kWarps * a.nsplit) : 2;  // (a cluster is a power of two)
   static_assert(kWarps == 4, "turn");
   const int mine = first < steps ? (steps - first - 1 >> turn) + 1 : 0;  // steps of the warp
@@ -648,6 +655,12 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     if (alone) {
       const uint2 u = make_uint2(Pair<T>::pack(acc.x, acc.y), Pair<T>::pack(acc.z, acc.w));
       if (g < nh) *reinterpret_cast<uint2*>(static_cast<T*>(a.out) + at * D + d) = u;
+    } else if constexpr (SPLIT == kChunks) {
+      const int64_t of = z * static_cast<int64_t>(a.tokens) * a.heads + at;
+      if (g < nh) {
+        *reinterpret_cast<float4*>(a.part + of * D + d) = acc;
+        if (d == 0) a.part_lse[of] = lse;
+      }
     } else if constexpr (CL) {
       if (z < n) {
         const int to = x * per_inverse >> 20;
@@ -705,9 +718,10 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   }
 }
 
-template <typename T, int D, int NT, bool CL>
+template <typename T, int D, int NT, Split SPLIT>
 cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
-  auto kern = attn_rows_q4_kernel<T, D, NT, CL>;
+  constexpr bool CL = SPLIT == kCluster;
+  auto kern = attn_rows_q4_kernel<T, D, NT, SPLIT>;
   constexpr int smem = RowsQ4Smem<D, 8 * NT, CL>::TOTAL;
   cudaError_t e = ensure_smem(kern, smem);
   if (e != cudaSuccess) return e;
@@ -726,24 +740,28 @@ cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = a.nsplit;
+  attr[1].val.clusterDim.x = CL ? a.nsplit : 1;
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = a.nsplit > 1 ? 2 : 1;
+  cfg.numAttrs = CL ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, a, c);
 }
-template <typename T, int D>
+template <typename T, int D, Split SPLIT>
 cudaError_t tiles(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
-  if (a.nsplit > 1) return a.rows == 8 ? run<T, D, 1, true>(a, c, stream) : run<T, D, 2, true>(a, c, stream);
-  return a.rows == 8 ? run<T, D, 1, false>(a, c, stream) : run<T, D, 2, false>(a, c, stream);
+  return a.rows == 8 ? run<T, D, 1, SPLIT>(a, c, stream) : run<T, D, 2, SPLIT>(a, c, stream);
+}
+template <typename T, int D>
+cudaError_t splits(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
+  if (a.nsplit == 1) return tiles<T, D, kWhole>(a, c, stream);
+  return a.chunk > 0 ? tiles<T, D, kChunks>(a, c, stream) : tiles<T, D, kCluster>(a, c, stream);
 }
 
 }  // namespace
 
 cudaError_t launch_attn_rows_q4(const AttnArgs& a, const Q4Cache& c, int dtype, int dim, cudaStream_t stream) {
-  if (dtype == SSS_OUT_F16) return dim == 64 ? tiles<__half, 64>(a, c, stream) : tiles<__half, 128>(a, c, stream);
-  return dim == 64 ? tiles<__nv_bfloat16, 64>(a, c, stream) : tiles<__nv_bfloat16, 128>(a, c, stream);
+  if (dtype == SSS_OUT_F16) return dim == 64 ? splits<__half, 64>(a, c, stream) : splits<__half, 128>(a, c, stream);
+  return dim == 64 ? splits<__nv_bfloat16, 64>(a, c, stream) : splits<__nv_bfloat16, 128>(a, c, stream);
 }
 
 }  // namespace sss

@@ -70,7 +70,7 @@ def check(c, got, scale=None, max_q=None):
     dim, dtype = c["q"].shape[2], c["q"].dtype
     w = q4_plain.attention(c["q"], c["k"], c["v"], c["cu"], c["kv"], c["rows"], dim ** -0.5 if scale is None else scale)
     most = int(np.diff(c["cu"]).max()) if max_q is None else max_q
-    many = most > 1 and most * (c["q"].shape[1] // c["k"][0].shape[1]) > 32
+    many = most > 1 and most * (c["q"].shape[1] // c["k"][0].shape[1]) > 64
     with np.errstate(all="ignore"):
         bound = (q4_plain.bound_many if many else q4_plain.bound_rows)(w, dtype, dim, max(c["kv"] + [1]))
     got, out = got.double().numpy(), w["out"]
@@ -135,6 +135,20 @@ def test_wider_bounds_and_twice_the_same(i):
 def test_long(dtype, fresh, kv, hq, hkv, dim, page):
     c = make(fresh, kv, hq, hkv, dim, dtype, page, seed=50)
     check(c, call(c))
+
+
+@pytest.mark.parametrize("fresh,kv,hq,hkv,dim,dtype,page", [
+    ([1] * 6, [9000, 5, 0, 1408, 1409, 5000], 8, 8, 128, BF, 16), ([2, 1, 2], [2, 9001, 3000], 32, 16, 128, FP, 64),
+    ([1] * 4, [17000, 1, 1030, 4097], 16, 16, 64, BF, 128), ([3, 3], [17000, 900], 64, 16, 128, BF, 16),
+])
+def test_keys_in_chunks(fresh, kv, hq, hkv, dim, dtype, page):
+    # long requests among short ones: their chunks are joined by a second kernel
+    c = make(fresh, kv, hq, hkv, dim, dtype, page, seed=51)
+    cache = cache_of(c)
+    assert sss.sss_attention_q4_workspace_bytes(sum(fresh), hq, cache, len(kv), max(fresh), max(kv)) > 0
+    got = call(c, cache=cache)
+    check(c, got)
+    assert torch.equal(got, call(c, cache=cache))
 
 
 @pytest.mark.parametrize("dtype", [BF, FP])

@@ -154,7 +154,7 @@ def test_prompts_then_tokens_and_back():
         at = [0, kvs[0]]
         w = q4_plain.attention(q.cpu(), *[(q4_plain.values(u, s), s) for u, s, _ in packed], cu.tolist(), kvs,
                                lambda b: at[b] + np.arange(kvs[b]), dim ** -0.5)
-        bound = q4_plain.bound_many if max(fresh) * hq // hkv > 32 else q4_plain.bound_rows
+        bound = q4_plain.bound_many if max(fresh) * hq // hkv > 64 else q4_plain.bound_rows
         err = np.abs(out.cpu().double().numpy() - w["out"])
         assert np.max(err / bound(w, BF, dim, 200)) <= 1.0
         past.copy_(kv)

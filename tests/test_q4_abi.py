@@ -91,6 +91,7 @@ def test_attention_workspace():
     c = cache(heads=8, page_stride=8 * 18 * 128)
     size = lambda t, h, w, b, mq, mkv: sss.load().sss_attention_q4_workspace_bytes(t, h, ctypes.byref(c), w, b, mq, mkv)  # noqa: E731
     assert size(64, 32, 100, 64, 1, 1600) == 0               # single tokens read the cache as it is
+    assert size(64, 32, 999, 64, 1, 16000) == 8 * 64 * 32 * (128 + 1) * 4  # long ones leave a chunk's results each
     copy = 2 * 1600 * 8 * 128 * 2
     assert copy <= size(64, 32, 100, 1, 64, 1600) < 2 * copy + (1 << 20) * 64
     assert size(64, 32, 50, 1, 64, 1600) < size(64, 32, 100, 1, 64, 1600) == size(64, 32, 2 ** 31 - 1, 1, 64, 1600)
