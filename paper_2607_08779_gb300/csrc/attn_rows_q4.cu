@@ -63,14 +63,14 @@ __device__ __forceinline__ int key_slot(int i) {
   return (i & 8) + ((i & 1) ? 4 + ((i >> 1 & 3) ^ 3) : (i >> 1 & 3));
 }
 
-// d = A B + (c0, c1) in both of its halves, or d += A B
+// d = A B + c, or d += A B
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                        uint32_t a3, uint32_t b0, uint32_t b1, float c0, float c1) {
+                                        uint32_t a3, uint32_t b0, uint32_t b1, const float (&c)[4]) {
   asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
-      "{%8,%9}, {%10,%11,%10,%11};"
+      "{%8,%9}, {%10,%11,%12,%13};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c0), "f"(c1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(c[2]), "f"(c[3]));
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                         uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   // q' as operands, what the scores' sums start from, and the rows' scales and limits: of
   // the accumulators' rows 2 c and 2 c + 1 of each tile
   uint32_t qf[NT][4][KW];
-  float start[NT][G][2], rscale[NT][2];
+  float start[NT][G][4], rscale[NT][2];
   int lim[NT][2];
 #pragma unroll
   for (int m = 0; m < NT; ++m) {
@@ -328,11 +328,16 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
       const int from = 4 * (2 * c + k);
 #pragma unroll
       for (int g = 0; g < G; ++g)
-        start[m][g][k] = -0x1p-21f * __shfl_sync(0xffffffffu, sums[g], from);
+        start[m][g][k] = start[m][g][2 + k] = -0x1p-21f * __shfl_sync(0xffffffffu, sums[g], from);
       rscale[m][k] = __shfl_sync(0xffffffffu, rs, from);
       lim[m][k] = __shfl_sync(0xffffffffu, limit, from);
     }
   }
+
+#pragma unroll
+  for (int m = 0; m < NT; ++m)  // (the compiler would make the second halves anew for each product)
+#pragma unroll
+    for (int g = 0; g < G; ++g) asm volatile("" : "+f"(start[m][g][2]), "+f"(start[m][g][3]));
 
   float o[NT][4][VW][4];  // rows 2 c, 2 c + 1 of dimensions 2 W e + w and 2 W e + W + w
   float mx[NT][2], ref[NT][2], sum[NT][2];  // (ref: mx, or 0 where that is -inf)
@@ -361,13 +366,15 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   bool waited = true;
 #pragma unroll 1
   for (int s = 0; s < mine; ++s) {
-    int abort = 0;
-    waited = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], parity, &abort));
-    if (!waited) break;
+    if (!__all_sync(0xffffffffu, mbar_try_wait(&full[warp][stage], parity))) {
+      int abort = 0;
+      waited = __all_sync(0xffffffffu, mbar_wait(&full[warp][stage], parity, &abort));
+      if (!waited) break;
+    }
     const unsigned char* at = ring + stage * S::STAGE;
     const int key0 = key_of(s);
-    const bool cut = key0 + kStep > lim0;
     const uint32_t blank = none >> (kBlocks * stage) & ((1u << kBlocks) - 1);
+    const bool rare = key0 + kStep > lim0 || blank != 0;  // (rows that are no token's see nothing then)
 
     // scores
     float x[kBlocks][NT][4];
@@ -416,7 +423,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
 #pragma unroll
             for (int m = 0; m < NT; ++m) {
               if (e == g * PER && w == 0)
-                mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1], start[m][g][0], start[m][g][1]);
+                mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1], start[m][g]);
               else
                 mma_f16(acc[m], a0, a1, a2, a3, qf[m][e][w], qf[m][e][w + 1]);
             }
@@ -435,23 +442,16 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
       for (int m = 0; m < NT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[u][m][i] *= rscale[m][i & 1];
-    if (blank) {  // no page: zeros (what the stage holds is of any kind)
+    if (rare) {  // no page: zeros (what the stage holds is of any kind); not seen: -inf
 #pragma unroll
       for (int u = 0; u < kBlocks; ++u)
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
+          for (int i = 0; i < 4; ++i) {
             if (blank >> u & 1u) x[u][m][i] = 0.f;
-    }
-    if (cut) {
-#pragma unroll
-      for (int u = 0; u < kBlocks; ++u)
-#pragma unroll
-        for (int m = 0; m < NT; ++m)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
             if (key0 + kQ4Slots * u + j0 + 8 * (i >> 1) >= lim[m][i & 1]) x[u][m][i] = -INFINITY;
+          }
     }
     float top[NT][2];
     bool raise = false;
@@ -526,7 +526,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
           }
         }
       }
-      if (cut) {  // what a row does not see may be of any scale
+      if (rare) {  // what a row does not see may be of any scale
 #pragma unroll
         for (int m = 0; m < NT; ++m)
 #pragma unroll
