@@ -6,11 +6,11 @@
 // extremes meet in two exchanges; each lane packs its codes and three more exchanges make
 // words of the cache's layout of them (kv_q4.cuh).  Fetch goes the same way back.
 //
-// Bound by HBM: 2 or 4 bytes a value in and 9/16 out, or the other way round.  A warp takes
-// a run of a token's heads, keys then values, then that of a later token, kUnroll groups of
-// heads at a time with the next ones' loads in flight.
+// Bound by instruction issue and by HBM (2 or 4 bytes a value in and 9/16 out, or the other way
+// round), so an item has little around its values: a warp takes a token's keys or its
+// values, kUnroll groups of heads with all of their loads in flight, and steps from group to
+// group by adding to two addresses.
 #include <algorithm>
-#include <numeric>
 
 #include "kv_q4.cuh"
 #include "rne.cuh"
@@ -19,6 +19,8 @@ namespace sss {
 namespace {
 
 constexpr int kThreads = 128;
+constexpr int kWarps = kThreads / 32;
+constexpr int kUnroll = 4;
 
 struct StoreArgs {
   const void *k, *v;
@@ -27,7 +29,7 @@ struct StoreArgs {
   Q4Cache cache;
   uint32_t* status;
   int64_t tokens;
-  int run, runs;  // groups of heads that a warp takes, and such runs of a token
+  int run;  // heads that a warp takes
 };
 
 // A lane's eight consecutive values, as they come.
@@ -179,71 +181,52 @@ __device__ __forceinline__ uint32_t quantize8(const Raw<T>& v, uint16_t& s16, ui
   return packed(u, q.far);
 }
 
+// Grid: tokens, kWarps to a CTA; runs of heads, of the keys and then of the values.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 8) kv_store_q4_kernel(const __grid_constant__ StoreArgs a) {
+__global__ void __launch_bounds__(kThreads) kv_store_q4_kernel(const __grid_constant__ StoreArgs a) {
   using B = Q4Block<D>;
   constexpr int LANES = D / 8, GH = 32 / LANES;
-  constexpr int U = sizeof(T) == 4 ? 1 : 2;  // groups of heads at a time
+  constexpr int U = sizeof(T) == 4 ? kUnroll / 2 : kUnroll;
   const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
-  const int warp = (blockIdx.x * kThreads + threadIdx.x) >> 5;
-  const int H = a.cache.heads, heads = 2 * H;
-  int64_t t = warp / a.runs;
-  const int h0 = (warp - static_cast<int>(t) * a.runs) * a.run * GH, h1 = min(heads, h0 + a.run * GH);
-  const int64_t step = gridDim.x * (kThreads / 32) / a.runs;  // (a multiple of runs)
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int runs = gridDim.y / 2;
+  const bool is_v = blockIdx.y >= runs;
+  const int h0 = (blockIdx.y - (is_v ? runs : 0)) * a.run, h1 = min(a.cache.heads, h0 + a.run);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (t >= a.tokens) return;
-  const auto load = [&](int64_t tt, int hb, Raw<T> (&x)[U]) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = hb + u * GH + sub;
-      const T* src = h >= H ? static_cast<const T*>(a.v) + tt * a.v_stride + (h - H) * D
-                            : static_cast<const T*>(a.k) + tt * a.k_stride + h * D;
-      x[u].zero();
-      if (h < h1) x[u].load(src + 8 * l);
-    }
-  };
-  const auto slot_of = [&](int64_t tt) { return a.slots ? static_cast<int64_t>(a.slots[tt]) : tt; };
-  uint32_t flags = 0;
-  const int word = q4_word<D>(l);
+  const T* src = (is_v ? static_cast<const T*>(a.v) + t * a.v_stride : static_cast<const T*>(a.k) + t * a.k_stride) +
+                 (h0 + sub) * D + 8 * l;
+  const int64_t slot = a.slots ? a.slots[t] : t;
+  const bool keep = slot >= 0 && slot < a.cache.slots;
+  uint32_t flags = slot >= a.cache.slots ? SSS_FLAG_INDEX : 0u;
+  const int in = static_cast<int>(slot) & ((1 << a.cache.shift) - 1), j = in & 15;
   const int per_head = B::kBytes << (a.cache.shift - 4);  // bytes of a head's blocks in a page
-  int64_t slot = slot_of(t);
-  int hb = h0;
-  Raw<T> next[U];
-  load(t, hb, next);
-  while (true) {
+  const int word = q4_word<D>(l);
+  char* head = a.cache.blocks + (slot >> a.cache.shift) * a.cache.page_stride + (in >> 4) * B::kBytes +
+               static_cast<int64_t>(h0 + sub) * per_head + (is_v ? B::kV : B::kK);
+  const int code_at = j * B::kRow + 4 * (is_v ? q4_value_word<D>(word, j) : word);
+  const int scale_at = B::kKS + j * B::kScales + 2 * (l >> 2);  // (the scales follow the codes)
+  for (int h = h0; h < h1; h += U * GH) {
     Raw<T> x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = next[u];
-    const int64_t at_slot = slot;
-    const int at_h = hb;
-    hb += U * GH;
-    if (hb >= h1) {
-      hb = h0;
-      t += step;
-      if (t < a.tokens) slot = slot_of(t);
+    for (int u = 0; u < U; ++u) {
+      x[u].zero();
+      if (h + u * GH + sub < h1) x[u].load(src + u * GH * D);
     }
-    const bool more = t < a.tokens;
-    if (more) load(t, hb, next);
-    if (at_slot >= a.cache.slots) flags |= SSS_FLAG_INDEX;
-    if (at_slot >= 0 && at_slot < a.cache.slots) {
-      const int in = static_cast<int>(at_slot) & ((1 << a.cache.shift) - 1), j = in & 15;
-      char* page = a.cache.blocks + (at_slot >> a.cache.shift) * a.cache.page_stride + (in >> 4) * B::kBytes;
-      const int vword = q4_value_word<D>(word, j);
+    src += U * GH * D;
+    if (!keep) break;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = at_h + u * GH + sub;
-        uint16_t s16;
-        const uint32_t w = q4_transpose<D>(quantize8(x[u], s16, flags), l);
-        if (h >= h1) continue;
-        const bool is_v = h >= H;
-        char* b = page + static_cast<int64_t>(is_v ? h - H : h) * per_head + (is_v ? B::kV : B::kK);
-        reinterpret_cast<uint32_t*>(b + j * B::kRow)[is_v ? vword : word] = w;
-        if ((l & 3) == 0)  // (the scales follow the codes)
-          reinterpret_cast<uint16_t*>(b + B::kKS + j * B::kScales)[l >> 2] = s16;
+    for (int u = 0; u < U; ++u) {
+      if (h + u * GH >= h1) break;
+      uint16_t s16;
+      const uint32_t w = q4_transpose<D>(quantize8(x[u], s16, flags), l);
+      if (h + u * GH + sub < h1) {
+        *reinterpret_cast<uint32_t*>(head + code_at) = w;
+        if ((l & 3) == 0) *reinterpret_cast<uint16_t*>(head + scale_at) = s16;
       }
+      head += GH * per_head;
     }
-    if (!more) break;
   }
   if (flags && a.status) atomicOr(a.status, flags);
 }
@@ -254,7 +237,7 @@ struct FetchArgs {
   void *k, *v;
   uint32_t* status;
   int64_t rows;
-  int run, runs;
+  int run;
   Q4Stage stage;
 };
 
@@ -276,129 +259,103 @@ __device__ __forceinline__ void store8(T* p, const float (&f)[8]) {
   }
 }
 
-// STAGE: blockIdx.y is a request; row t of the copy is its key t, in a page of its own.
+// As the store's grid, of rows.  STAGE: blockIdx.z is a request; row t of the copy is its key
+// t, in a page of its own.
 template <typename T, int D, bool STAGE>
-__global__ void __launch_bounds__(kThreads, 8) kv_fetch_q4_kernel(const __grid_constant__ FetchArgs a) {
+__global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_constant__ FetchArgs a) {
   using B = Q4Block<D>;
   constexpr int LANES = D / 8, GH = 32 / LANES;
-  constexpr int U = 2;  // groups of heads at a time
   const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
-  const int warp = (blockIdx.x * kThreads + threadIdx.x) >> 5;
-  const int H = a.cache.heads, heads = 2 * H, shift = a.cache.shift;
-  int64_t t = warp / a.runs;
-  const int h0 = (warp - static_cast<int>(t) * a.runs) * a.run * GH, h1 = min(heads, h0 + a.run * GH);
-  const int64_t step = gridDim.x * (kThreads / 32) / a.runs;
+  const int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int runs = gridDim.y / 2, shift = a.cache.shift;
+  const bool is_v = blockIdx.y >= runs;
+  const int h0 = (blockIdx.y - (is_v ? runs : 0)) * a.run, h1 = min(a.cache.heads, h0 + a.run);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (t >= a.rows) return;
   uint32_t flags = 0;
-  int64_t rows = a.rows, first = 0;
-  const int32_t* table = nullptr;
+  int64_t slot, row = t;
   if constexpr (STAGE) {
     const Q4Stage& s = a.stage;
-    const int b = blockIdx.y;
-    table = s.table + static_cast<int64_t>(b) * s.table_width;
-    first = static_cast<int64_t>(b) * s.pages << shift;
-    // the copy's table, of the pages that are real; (what is none, and keys past the
+    const int b = blockIdx.z;
+    const int64_t p = t >> shift;
+    const int32_t page = __ldg(s.table + static_cast<int64_t>(b) * s.table_width + p);
+    const bool real = page >= 0 && page < a.cache.slots >> shift;
+    // the copy's table, of the pages that are real (what is none, and keys past the
     // request's, are the attention's to flag)
-    for (int p = blockIdx.x * kThreads + threadIdx.x; p < s.pages; p += gridDim.x * kThreads) {
-      const int32_t page = table[p];
-      s.new_table[static_cast<int64_t>(b) * s.pages + p] =
-          page >= 0 && page < a.cache.slots >> shift ? b * s.pages + p : -1;
+    if (blockIdx.y == 0 && lane == 0 && (t & ((1 << shift) - 1)) == 0)
+      s.new_table[static_cast<int64_t>(b) * s.pages + p] = real ? b * s.pages + static_cast<int32_t>(p) : -1;
+    if (!real || t >= s.kv_len[b] || t >= s.max_kv) return;
+    row += static_cast<int64_t>(b) * s.pages << shift;
+    slot = (static_cast<int64_t>(page) << shift) + (t & ((1 << shift) - 1));
+  } else {
+    slot = a.slots ? a.slots[t] : t;
+    if (slot >= a.cache.slots) {
+      flags |= SSS_FLAG_INDEX;
+      slot = -1;
     }
-    rows = min(rows, min(static_cast<int64_t>(s.kv_len[b]), s.max_kv));
   }
-  if (t >= rows) return;
-  const auto slot_of = [&](int64_t tt) -> int64_t {
-    if constexpr (STAGE) {
-      const int32_t page = __ldg(table + (tt >> shift));
-      return page >= 0 && page < a.cache.slots >> shift
-                 ? (static_cast<int64_t>(page) << shift) + (tt & ((1 << shift) - 1)) : -1;
-    } else {
-      return a.slots ? static_cast<int64_t>(a.slots[tt]) : tt;
-    }
-  };
-  const int word = q4_word<D>(l), per_head = B::kBytes << (shift - 4);
-  const auto load = [&](int64_t slot, int hb, uint32_t (&w)[U], uint16_t (&s16)[U]) {
+  T* out = static_cast<T*>(is_v ? a.v : a.k);
+  if (out != nullptr) {
+    out += (row * a.cache.heads + h0 + sub) * D + 8 * l;
     const int in = static_cast<int>(slot) & ((1 << shift) - 1), j = in & 15;
-    const char* page = a.cache.blocks + (slot >> shift) * a.cache.page_stride + (in >> 4) * B::kBytes;
-    const bool real = slot >= 0 && slot < a.cache.slots;
+    const int per_head = B::kBytes << (shift - 4), word = q4_word<D>(l);
+    const char* head = a.cache.blocks + (slot >> shift) * a.cache.page_stride + (in >> 4) * B::kBytes +
+                       static_cast<int64_t>(h0 + sub) * per_head + (is_v ? B::kV : B::kK);
+    const int code_at = j * B::kRow + 4 * (is_v ? q4_value_word<D>(word, j) : word);
+    const int scale_at = B::kKS + j * B::kScales + 2 * (l >> 2);
+    for (int h = h0; h < h1; h += kUnroll * GH) {
+      uint32_t w[kUnroll];
+      uint16_t s16[kUnroll];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = hb + u * GH + sub;
-      const bool is_v = h >= H;
-      const char* b = page + static_cast<int64_t>(is_v ? h - H : h) * per_head + (is_v ? B::kV : B::kK);
-      w[u] = 0x88888888u;
-      s16[u] = 0;
-      if (real && h < h1) {
-        w[u] = __ldg(reinterpret_cast<const uint32_t*>(b + j * B::kRow) + (is_v ? q4_value_word<D>(word, j) : word));
-        s16[u] = __ldg(reinterpret_cast<const uint16_t*>(b + B::kKS + j * B::kScales) + (l >> 2));
+      for (int u = 0; u < kUnroll; ++u) {
+        w[u] = 0x88888888u;
+        s16[u] = 0;
+        if (slot >= 0 && h + u * GH + sub < h1) {
+          w[u] = __ldg(reinterpret_cast<const uint32_t*>(head + code_at));
+          s16[u] = __ldg(reinterpret_cast<const uint16_t*>(head + scale_at));
+        }
+        head += GH * per_head;
       }
-    }
-  };
-  // the slot of the row after the next is read beside the next one's words
-  int64_t slot = slot_of(t), ahead = t + step < rows ? slot_of(t + step) : 0;
-  int hb = h0;
-  uint32_t nw[U];
-  uint16_t ns[U];
-  load(slot, hb, nw, ns);
-  while (true) {
-    uint32_t w[U];
-    float s[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      w[u] = nw[u];
-      s[u] = __half2float(__ushort_as_half(ns[u]));
-    }
-    const int64_t row = first + t;
-    const int at_h = hb;
-    if (slot >= a.cache.slots) flags |= SSS_FLAG_INDEX;
-    const bool skip = STAGE && slot < 0;
-    hb += U * GH;
-    if (hb >= h1) {
-      hb = h0;
-      t += step;
-      slot = ahead;
-      if (t + step < rows) ahead = slot_of(t + step);
-    }
-    const bool more = t < rows;
-    if (more) load(slot, hb, nw, ns);
-    if (!skip) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int h = at_h + u * GH + sub;
+      for (int u = 0; u < kUnroll; ++u) {
+        if (h + u * GH >= h1) break;
         const uint32_t c = q4_transpose<D>(w[u], l);
-        float f[8];
+        const float s = __half2float(__ushort_as_half(s16[u]));
+        // A nibble at bits 4 n of a float of 2^23 and more is 2^23 + 16^n u: times s / 16^n, less
+        // s (2^23 / 16^n + 8).  For n = 2, 3 and 4 that constant is exact in fp32, and so is the
+        // result of one multiply-add.
+        const uint32_t at[3] = {c << 8, c >> 4, c >> 16};
+        float f[8], by[3], less[3];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)  // (2^23 + u) - (2^23 + 8), without a conversion
-          f[e] = s[u] * (__uint_as_float((c >> (4 * e) & 15u) | 0x4B000000u) - 8388616.f);
-        if (h >= h1) continue;
-        const bool is_v = h >= H;
-        T* out = static_cast<T*>(is_v ? a.v : a.k);
-        if (out) store8(out + (row * H + (is_v ? h - H : h)) * D + 8 * l, f);
+        for (int n = 0; n < 3; ++n) {
+          by[n] = s * (1.f / (1 << (4 * (n + 2))));
+          less[n] = -s * ((1 << 23 >> (4 * (n + 2))) + 8.f);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          f[e] = __fmaf_rn(__uint_as_float((at[e / 3] & (15u << (4 * (e % 3 + 2)))) | 0x4B000000u),
+                           by[e % 3], less[e % 3]);
+        if (h + u * GH + sub < h1) store8(out, f);
+        out += GH * D;
       }
     }
-    if (!more) break;
   }
   if (flags && a.status) atomicOr(a.status, flags);
 }
 
 template <typename K, typename A>
 cudaError_t launch(K kern, A& a, int64_t rows, int dim, int batch, cudaStream_t stream) {
-  // All of a token's heads to a warp while that gives every SM 32 warps, else as many runs
-  // as do; then as many warps as run at a time.
-  const int gh = 256 / dim, groups = (2 * a.cache.heads + gh - 1) / gh;
-  const int64_t all = int64_t{64} * device_sm_count();
-  a.runs = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(groups, all / std::max<int64_t>(1, rows * batch))));
-  a.run = (groups + a.runs - 1) / a.runs;
-  a.runs = (groups + a.run - 1) / a.run;
-  // (whole CTAs of whole tokens' runs)
-  const int64_t unit = std::lcm<int64_t>(a.runs, kThreads / 32) / (kThreads / 32);
-  const int64_t want = (rows * a.runs * 32 + kThreads - 1) / kThreads;
-  const int64_t most = std::max<int64_t>(1, all / (kThreads / 32) / batch);
-  const int64_t blocks = (std::min(want, most) + unit - 1) / unit * unit;
-  if (blocks > INT32_MAX / kThreads) return cudaErrorNotSupported;
+  // A token's keys (or values) to a warp, or where that gives an SM fewer than 16 warps as many
+  // runs of its heads as do.
+  const int gh = 256 / dim, groups = (a.cache.heads + gh - 1) / gh;
+  const int64_t all = int64_t{16} * device_sm_count();
+  int runs = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(groups, all / std::max<int64_t>(1, 2 * rows * batch))));
+  const int of = (groups + runs - 1) / runs;
+  runs = (groups + of - 1) / of;
+  a.run = of * gh;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks), static_cast<unsigned>(batch));
+  cfg.gridDim = dim3(static_cast<unsigned>((rows + kWarps - 1) / kWarps), static_cast<unsigned>(2 * runs), static_cast<unsigned>(batch));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -425,7 +382,7 @@ cudaError_t fetch(FetchArgs& a, int dim, int batch, cudaStream_t stream) {
 cudaError_t launch_kv_store_q4(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                int in_dtype, int64_t tokens, const sss_kv_cache_q4_t& cache,
                                const int32_t* slots, uint32_t* status, cudaStream_t stream) {
-  StoreArgs a = {k, v, k_stride, v_stride, slots, q4_cache(cache), status, tokens, 1, 1};
+  StoreArgs a = {k, v, k_stride, v_stride, slots, q4_cache(cache), status, tokens, 1};
   switch (in_dtype) {
     case SSS_OUT_F16: return store<__half>(a, cache.dim, stream);
     case SSS_OUT_BF16: return store<__nv_bfloat16>(a, cache.dim, stream);
@@ -436,7 +393,7 @@ cudaError_t launch_kv_store_q4(const void* k, int64_t k_stride, const void* v, i
 cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* slots, int64_t count,
                                void* k, void* v, int out_dtype, uint32_t* status,
                                cudaStream_t stream) {
-  FetchArgs a = {q4_cache(cache), slots, k, v, status, count, 1, 1, {}};
+  FetchArgs a = {q4_cache(cache), slots, k, v, status, count, 1, {}};
   switch (out_dtype) {
     case SSS_OUT_F16: return fetch<__half, false>(a, cache.dim, 1, stream);
     case SSS_OUT_BF16: return fetch<__nv_bfloat16, false>(a, cache.dim, 1, stream);
@@ -446,7 +403,7 @@ cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* sl
 
 cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, int dtype, const Q4Stage& s,
                                cudaStream_t stream) {
-  FetchArgs a = {c, nullptr, s.k, s.v, nullptr, static_cast<int64_t>(s.pages) << c.shift, 1, 1, s};
+  FetchArgs a = {c, nullptr, s.k, s.v, nullptr, static_cast<int64_t>(s.pages) << c.shift, 1, s};
   return dtype == SSS_OUT_F16 ? fetch<__half, true>(a, dim, s.batch, stream)
                               : fetch<__nv_bfloat16, true>(a, dim, s.batch, stream);
 }

@@ -63,9 +63,10 @@ __device__ __forceinline__ uint32_t q4_transpose(uint32_t v, int l) {
   v = __byte_perm(v, o, (l & M2) ? 0x3276 : 0x5410);
   o = __shfl_xor_sync(0xffffffffu, v, M1);
   v = __byte_perm(v, o, (l & M1) ? 0x3715 : 0x6240);
-  o = __shfl_xor_sync(0xffffffffu, v, M0);
-  return (l & M0) ? (v & 0xF0F0F0F0u) | (o >> 4 & 0x0F0F0F0Fu)
-                  : (v & 0x0F0F0F0Fu) | (o << 4 & 0xF0F0F0F0u);
+  // (moved by a nibble before it is sent: one rotation)
+  o = __shfl_xor_sync(0xffffffffu, __funnelshift_l(v, v, (l & M0) ? 4 : 28), M0);
+  const uint32_t keep = (l & M0) ? 0xF0F0F0F0u : 0x0F0F0F0Fu;
+  return (v & keep) | (o & ~keep);
 }
 
 // What sss_attention_q4 leaves of its requests' keys and values for the form of many rows:
