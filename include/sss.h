@@ -627,12 +627,12 @@ sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slot
  * bounds and flags, always with a block table (so with kv_len).  The new tokens' own keys
  * and values are in the cache, as the others are.
  *   dtype [in]  of q and out: SSS_OUT_F16 or SSS_OUT_BF16.
- * A request's tokens times the heads of a group at most 32 (or single tokens): scores are
+ * A request's tokens times the heads of a group at most 64 (or single tokens): scores are
  * sums of q times the codes, scaled in fp32; p_ij times the value's scale is rounded to
- * fp16 (at most 2^-25 off where it is below fp16's normal range; a row's largest p_ij is
- * 1).  More: the keys and values are first written to the workspace as 16-bit
- * values of `dtype`, fp16(s) c rounded once (fp16 cannot hold those of 65520 and more, which
- * only bf16 or fp32 inputs can have left in the cache).
+ * fp16 (for bf16 p_ij is rounded first; at most 2^-25 off where it is below fp16's normal
+ * range; a row's largest p_ij is 1).  More: the keys and values are first written to the
+ * workspace as fp16 values, fp16(s) c rounded once (for bf16 a 16th of it, and q as fp16
+ * with a power of two taken off each row), and p_ij is rounded to fp16.
  * Errors: as sss_attention; SSS_E_UNSUPPORTED also where that copy of the cache would have
  * 2^31 slots or more.
  */

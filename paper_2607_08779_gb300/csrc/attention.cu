@@ -78,7 +78,7 @@ cudaError_t launch_attention(const AttnPlan& p, const void* q, int64_t q_stride,
                              const sss_kv_cache_t& c, const int32_t* cu_q, const int32_t* kv_len,
                              const int32_t* table, int width, int batch, int64_t tokens, int max_q,
                              int64_t max_kv, float scale, void* out, void* workspace,
-                             uint32_t* status, cudaStream_t stream) {
+                             uint32_t* status, cudaStream_t stream, const float* row_scale) {
   AttnArgs a = {};
   a.q = q;
   a.out = out;
@@ -112,11 +112,13 @@ cudaError_t launch_attention(const AttnPlan& p, const void* q, int64_t q_stride,
   a.nsplit = static_cast<int>(p.nsplit);
   a.rows = p.rows;
   a.scale_log2 = scale * 1.4426950408889634f;
+  a.row_scale = row_scale;
   const uint32_t stall = p.prompt ? SSS_TEST_STALL_ATTENTION : SSS_TEST_STALL_ATTENTION_ROWS;
   a.stall = (test_stall_mask() & stall) ? 1 : 0;
   cudaError_t e = p.prompt ? launch_attn_prompt(a, c.dtype, c.dim, stream)
                            : launch_attn_rows(a, c.dtype, c.dim, stream);
-  if (e == cudaSuccess && p.join) e = launch_attn_join(a, c.dtype, c.dim, stream);
+  if (e == cudaSuccess && p.join)
+    e = launch_attn_join(a, row_scale ? SSS_OUT_BF16 : c.dtype, c.dim, stream);
   return e;
 }
 

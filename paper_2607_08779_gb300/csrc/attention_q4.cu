@@ -4,6 +4,11 @@
 // would unpack each key and value once for every tile of rows; they are unpacked once for
 // the call instead, into the workspace, and go the way of a 16-bit cache.  That writes and
 // reads 2 bytes a value, next to 4 flops a value and row: a few per cent.
+//
+// The copy is fp16 for both types of q: fp16(s) c has 14 significant bits at most, of which fp16
+// keeps 11 and bf16 would keep 8 (error of the outputs, against 64 bits: 2.8e-3 to 3.4e-3 with a
+// bf16 copy, where their own rounding is 1.6e-3).  bf16 queries then go with it as fp16 numbers of
+// the same digits: each row gives off a power of two, which its scores' scale takes back.
 #include <algorithm>
 
 #include "attn.cuh"
@@ -15,7 +20,7 @@ namespace {
 size_t rounded(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // the copy in the workspace as a cache
-sss_kv_cache_t staged(const AttnQ4Plan& p, const sss_kv_cache_q4_t& c, int batch, int dtype, void* ws) {
+sss_kv_cache_t staged(const AttnQ4Plan& p, const sss_kv_cache_q4_t& c, int batch, void* ws) {
   sss_kv_cache_t s = {};
   char* at = static_cast<char*>(ws);
   s.k = at + p.k_at;
@@ -25,7 +30,7 @@ sss_kv_cache_t staged(const AttnQ4Plan& p, const sss_kv_cache_q4_t& c, int batch
   s.page_size = c.page_size;
   s.heads = c.heads;
   s.dim = c.dim;
-  s.dtype = dtype;
+  s.dtype = SSS_OUT_F16;
   return s;
 }
 
@@ -84,12 +89,14 @@ AttnQ4Plan plan_attention_q4(int64_t tokens, int heads, const sss_kv_cache_q4_t&
     plan_rows(p.of, tokens, group, c.heads, c.dim, batch, max_q, max_kv);
     p.ws_bytes = p.of.ws_bytes;
   } else {
-    p.of = plan_attention(tokens, heads, staged(p, c, batch, SSS_OUT_BF16, nullptr), batch, max_q, max_kv);
+    p.of = plan_attention(tokens, heads, staged(p, c, batch, nullptr), batch, max_q, max_kv);
     const size_t bytes = static_cast<size_t>(batch) * p.pages * c.page_size * c.heads * c.dim * 2;
     p.table_at = rounded(p.of.ws_bytes);
     p.k_at = p.table_at + rounded(static_cast<size_t>(batch) * p.pages * 4);
     p.v_at = p.k_at + rounded(bytes);
-    p.ws_bytes = p.v_at + rounded(bytes);
+    p.q_at = p.v_at + rounded(bytes);
+    p.scale_at = p.q_at + rounded(static_cast<size_t>(tokens) * heads * c.dim * 2);
+    p.ws_bytes = p.scale_at + rounded(static_cast<size_t>(tokens) * heads * 4);
   }
   return p;
 }
@@ -102,11 +109,22 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
   if (p.of.prompt) {
     char* ws = static_cast<char*>(workspace);
     int32_t* to = reinterpret_cast<int32_t*>(ws + p.table_at);
-    const Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at};
-    cudaError_t e = launch_kv_stage_q4(q4_cache(c), c.dim, dtype, s, stream);
+    // (a 16th of what bf16 or fp32 inputs can have left in the cache is in fp16's range)
+    const bool bf16 = dtype == SSS_OUT_BF16;
+    const float times = bf16 ? 0.0625f : 1.f;
+    float* const scales = reinterpret_cast<float*>(ws + p.scale_at);
+    const Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, times};
+    cudaError_t e = launch_kv_stage_q4(q4_cache(c), c.dim, s, stream);
+    if (e == cudaSuccess && bf16) {
+      e = launch_q_stage(q, q_stride, tokens, heads, c.dim, scale * 1.4426950408889634f, times,
+                         ws + p.q_at, scales, stream);
+      q = ws + p.q_at;
+      q_stride = static_cast<int64_t>(heads) * c.dim;
+    }
     if (e != cudaSuccess) return e;
-    return launch_attention(p.of, q, q_stride, heads, staged(p, c, batch, dtype, ws), cu_q, kv_len,
-                            to, p.pages, batch, tokens, max_q, max_kv, scale, out, ws, status, stream);
+    return launch_attention(p.of, q, q_stride, heads, staged(p, c, batch, ws), cu_q, kv_len,
+                            to, p.pages, batch, tokens, max_q, max_kv, scale, out, ws, status, stream,
+                            bf16 ? scales : nullptr);
   }
   AttnArgs a = {};
   a.q = q;

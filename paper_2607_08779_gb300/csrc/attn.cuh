@@ -39,6 +39,7 @@ struct AttnArgs {
   int stall;        // test hook
   int box_rows;     // of an output box of the prompt form
   float scale_log2;  // scale * log2(e)
+  const float* row_scale;  // nullable [tokens][heads]: in its place, of fp16 operands for bf16 outputs
 };
 
 // A request, with lengths that are safe to index by whatever cu_q and kv_len hold

@@ -248,7 +248,9 @@ __device__ __forceinline__ int next_cta(uint32_t answer) {
   return ok ? static_cast<int>(x) : -1;
 }
 
-template <typename T, int D>
+// OUT: the outputs' type.  Where it is not the operands' they come from a copy whose rows of q
+// have powers of two of their own taken off (a.row_scale), and whose values are a 16th.
+template <typename T, int D, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_prompt_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
   using S = PromptSmem<D>;
@@ -718,6 +720,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // the row's maximum to raise it
     int k0, n, lim, whole;
     float pass;
+    float scale = a.scale_log2;  // of the row's scores
     bool more;
     auto begin = [&](int item) {
       Work w;
@@ -729,6 +732,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool in = g < w.nh && w.i0 + ti < w.n;
       lim = in ? attn_limit(rq, w.i0 + ti) : 0;
       pass = in ? kRaise : INFINITY;  // (a row of no token has no say)
+      if constexpr (!std::is_same<T, OUT>::value)
+        scale = in ? __ldg(a.row_scale + static_cast<int64_t>(w.q0 + w.i0 + ti) * a.heads + w.kh * a.group + w.g0 + g) : 1.f;
       whole = attn_limit(rq, min(w.i0 + s * tt, w.n - 1));
     };
     begin(0);
@@ -772,9 +777,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           t[c] = fmaxf(t[c], __uint_as_float(v[c][31]));
         }
         const float top = fmaxf(max3(t[0], t[1], t[2]), t[3]);
-        if (__any_sync(0xffffffffu, (top - mx) * a.scale_log2 > pass)) {
+        if (__any_sync(0xffffffffu, (top - mx) * scale > pass)) {
           const float to = fmaxf(mx, top);
-          const float f = to == -INFINITY ? 1.f : ex2((mx - to) * a.scale_log2);
+          const float f = to == -INFINITY ? 1.f : ex2((mx - to) * scale);
           mx = to;
 #pragma unroll
           for (int x = 0; x < 4; ++x) sum[x] = make_float2(sum[x].x * f, sum[x].y * f);
@@ -793,14 +798,14 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        const float neg = mx == -INFINITY ? 0.f : -mx * a.scale_log2;
+        const float neg = mx == -INFINITY ? 0.f : -mx * scale;
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t p[16];
 #pragma unroll
           for (int x = 0; x < 16; ++x) {
             float2 y = fma2(__uint_as_float(v[c][2 * x]), __uint_as_float(v[c][2 * x + 1]),
-                            a.scale_log2, neg);
+                            scale, neg);
             y.x = ex2(y.x);
             y.y = ex2(y.y);
             sum[x & 3] = add2(sum[x & 3], y);
@@ -820,7 +825,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool in = g < w.nh && i < w.n;
       const float2 s01 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
       const float total = s01.x + s01.y;
-      const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
+      constexpr float kValues = std::is_same<T, OUT>::value ? 1.f : 16.f;
+      const float r = total == 0.f ? 0.f : kValues / total;  // a row without keys: zeros
+      const float lse = total == 0.f ? -INFINITY : mx * scale + log2f(total);
       const int64_t at = static_cast<int64_t>(w.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
       const int64_t zat = static_cast<int64_t>(w.z) * a.tokens * a.heads + at;
       const uint32_t rows_in = __ballot_sync(0xffffffffu, in);
@@ -900,7 +907,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int x = 0; x < 16; ++x) {
               asm volatile("" : "+r"(o[h][2 * x]), "+r"(o[h][2 * x + 1]));
               const float2 y = mul2(__uint_as_float(o[h][2 * x]), __uint_as_float(o[h][2 * x + 1]), r);
-              p[16 * h + x] = Pair<T>::pack(y.x, y.y) & keep;
+              p[16 * h + x] = Pair<OUT>::pack(y.x, y.y) & keep;
             }
           if (keys > 0 && c == D / 64 - 1) {
             tc_fence_before();
@@ -928,7 +935,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           put(o, 128 * c, c, false);
         }
-        if (in) a.part_lse[zat] = total == 0.f ? -INFINITY : mx * a.scale_log2 + log2f(total);
+        if (in) a.part_lse[zat] = lse;
       }
       if (odd[item & 1]) {  // infinite and NaN values that the row sees
         const uint32_t* notes = first + (item & 1) * D;
@@ -945,7 +952,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (y == 0.f) continue;
           if (alone) {
             uint16_t* at16 = reinterpret_cast<uint16_t*>(base) + d;
-            *at16 = static_cast<uint16_t>(Pair<T>::pack(y + Pair<T>::value(*at16), 0.f));
+            *at16 = static_cast<uint16_t>(Pair<OUT>::pack(y + Pair<OUT>::value(*at16), 0.f));
           } else {
             reinterpret_cast<float*>(base)[d] += y;
           }
@@ -995,7 +1002,7 @@ CUresult encode_heads(EncodeTiledFn enc, CUtensorMap* map, CUtensorMapDataType t
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
-template <typename T, int D>
+template <typename T, int D, typename OUT = T>
 cudaError_t run_prompt(AttnArgs a, cudaStream_t stream) {
   EncodeTiledFn enc = tensor_map_encoder();
   if (enc == nullptr) return cudaErrorNotSupported;
@@ -1017,7 +1024,7 @@ cudaError_t run_prompt(AttnArgs a, cudaStream_t stream) {
       encode_heads(enc, &maps.out, type, a.out, a.heads, D, a.tokens,
                    static_cast<int64_t>(a.heads) * D, bt, bh) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  auto kern = attn_prompt_kernel<T, D>;
+  auto kern = attn_prompt_kernel<T, D, OUT>;
   cudaError_t e = ensure_smem(kern, PromptSmem<D>::TOTAL);
   if (e != cudaSuccess) return e;
   const int64_t blocks = static_cast<int64_t>(a.tiles) * a.kv_heads * a.hchunks * a.nsplit;
@@ -1038,6 +1045,9 @@ cudaError_t run_prompt(AttnArgs a, cudaStream_t stream) {
 }  // namespace
 
 cudaError_t launch_attn_prompt(const AttnArgs& a, int dtype, int dim, cudaStream_t stream) {
+  if (a.row_scale != nullptr)
+    return dim == 64 ? run_prompt<__half, 64, __nv_bfloat16>(a, stream)
+                     : run_prompt<__half, 128, __nv_bfloat16>(a, stream);
   if (dtype == SSS_OUT_F16)
     return dim == 64 ? run_prompt<__half, 64>(a, stream) : run_prompt<__half, 128>(a, stream);
   return dim == 64 ? run_prompt<__nv_bfloat16, 64>(a, stream)

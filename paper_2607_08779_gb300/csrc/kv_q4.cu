@@ -334,7 +334,8 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
       for (int u = 0; u < kUnroll; ++u) {
         if (h + u * GH >= h1) break;
         const uint32_t c = q4_transpose<D>(w[u], l);
-        const float s = __half2float(__ushort_as_half(s16[u]));
+        float s = __half2float(__ushort_as_half(s16[u]));
+        if constexpr (STAGE) s *= a.stage.times;
         // A nibble at bits 4 n of a float of 2^23 and more is 2^23 + 16^n u: times s / 16^n, less
         // s (2^23 / 16^n + 8).  For n = 2, 3 and 4 that constant is exact in fp32, and so is the
         // result of one multiply-add.
@@ -355,6 +356,52 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
     }
   }
   if (flags && a.status) atomicOr(a.status, flags);
+}
+
+// Queries for the copy: a row of D values is D / 8 lanes.
+struct QArgs {
+  const void* q;
+  void* out;
+  float* scales;
+  int64_t q_stride, tokens;
+  int heads;
+  float scale_log2, times;
+};
+template <int D>
+__global__ void __launch_bounds__(kThreads) q_stage_kernel(const __grid_constant__ QArgs a) {
+  constexpr int LANES = D / 8;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x, row = at / LANES;
+  const int l = static_cast<int>(at % LANES);
+  const int64_t t = row / a.heads;
+  const bool in = t < a.tokens;
+  uint4 u = make_uint4(0u, 0u, 0u, 0u);
+  if (in)
+    u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + t * a.q_stride +
+                                             (row - t * a.heads) * D + 8 * l));
+  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+  float f[8], top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(w[i] << 16);
+    f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    top = fmaxf(top, fmaxf(fabsf(f[2 * i]), fabsf(f[2 * i + 1])));
+  }
+#pragma unroll
+  for (int m = LANES / 2; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+  // (a row of infinities or NaN keeps them)
+  const int E = min(max(static_cast<int>(__float_as_uint(top) >> 23 & 255u) - 127, -112), 127);
+  const float up = __int_as_float((14 - E + 127) << 23);
+  __half2 h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i] * up, f[2 * i + 1] * up);
+  memcpy(&u, h, 16);
+  if (!in) return;
+  *reinterpret_cast<uint4*>(static_cast<__half*>(a.out) + row * D + 8 * l) = u;
+  // (kept above zero and below infinity, for what is multiplied by an infinity or zero)
+  if (l == 0)
+    a.scales[row] = fminf(fmaxf(a.scale_log2 * __int_as_float((E - 14 + 127) << 23) / a.times, 1e-37f), 3e38f);
 }
 
 template <typename K, typename A>
@@ -414,11 +461,28 @@ cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* sl
   }
 }
 
-cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, int dtype, const Q4Stage& s,
-                               cudaStream_t stream) {
+cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, const Q4Stage& s, cudaStream_t stream) {
   FetchArgs a = {c, nullptr, s.k, s.v, nullptr, static_cast<int64_t>(s.pages) << c.shift, 1, s};
-  return dtype == SSS_OUT_F16 ? fetch<__half, true>(a, dim, s.batch, stream)
-                              : fetch<__nv_bfloat16, true>(a, dim, s.batch, stream);
+  return fetch<__half, true>(a, dim, s.batch, stream);
+}
+
+cudaError_t launch_q_stage(const void* q, int64_t q_stride, int64_t tokens, int heads, int dim,
+                           float scale_log2, float times, void* out, float* scales,
+                           cudaStream_t stream) {
+  const QArgs a = {q, out, scales, q_stride, tokens, heads, scale_log2, times};
+  const int64_t blocks = (tokens * heads * (dim / 8) + kThreads - 1) / kThreads;
+  if (blocks > INT32_MAX) return cudaErrorNotSupported;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return dim == 64 ? cudaLaunchKernelEx(&cfg, q_stage_kernel<64>, a)
+                   : cudaLaunchKernelEx(&cfg, q_stage_kernel<128>, a);
 }
 
 }  // namespace sss

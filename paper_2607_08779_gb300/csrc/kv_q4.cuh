@@ -77,10 +77,16 @@ struct Q4Stage {
   int pages;          // of a request
   int64_t max_kv;
   int32_t* new_table; // [batch][pages]
-  void *k, *v;        // [batch * pages * page_size][heads][dim]
+  void *k, *v;        // [batch * pages * page_size][heads][dim] fp16
+  float times;        // of the values: 1 or 1/16
 };
-cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, int dtype, const Q4Stage& s,
-                               cudaStream_t stream);
+cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, const Q4Stage& s, cudaStream_t stream);
+
+// bf16 queries as fp16 ones, each row (token, head) with a power of two of its own taken off so that its
+// largest value is between 2^14 and 2^15, and `scale_log2` times that and `times` to scales.
+cudaError_t launch_q_stage(const void* q, int64_t q_stride, int64_t tokens, int heads, int dim,
+                           float scale_log2, float times, void* out, float* scales,
+                           cudaStream_t stream);
 
 // Attention of few rows over the cache.
 struct AttnArgs;

@@ -102,7 +102,8 @@ cudaError_t launch_attention(const AttnPlan& plan, const void* q, int64_t q_stri
                              const sss_kv_cache_t& cache, const int32_t* cu_q,
                              const int32_t* kv_len, const int32_t* table, int width, int batch,
                              int64_t tokens, int max_q, int64_t max_kv, float scale, void* out,
-                             void* workspace, uint32_t* status, cudaStream_t stream);
+                             void* workspace, uint32_t* status, cudaStream_t stream,
+                             const float* row_scale = nullptr);
 
 cudaError_t launch_kv_store_q4(const void* k, int64_t k_stride, const void* v, int64_t v_stride,
                                int in_dtype, int64_t tokens, const sss_kv_cache_q4_t& cache,
@@ -115,7 +116,9 @@ cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* sl
 struct AttnQ4Plan {
   AttnPlan of;     // its rows' form, or that of the 16-bit copy in the workspace
   int pages;       // of the copy, for each request
-  size_t table_at, k_at, v_at, ws_bytes;  // the copy: its table, keys, values
+  size_t table_at, k_at, v_at;  // the copy: its table, keys, values
+  size_t q_at, scale_at;        // and for bf16 the queries and their rows' scales
+  size_t ws_bytes;
 };
 AttnQ4Plan plan_attention_q4(int64_t tokens, int heads, const sss_kv_cache_q4_t& cache, int width,
                              int batch, int max_q, int64_t max_kv);

@@ -102,14 +102,18 @@ def bound_rows(w, dtype, dim, max_kv):
 
 
 def bound_many(w, dtype, dim, max_kv):
-    """Many rows: keys and values rounded to the type first (in fp16 by 2^-25 below its
-    normal range), then the 16-bit operator's own bound."""
-    u = UNIT[dtype]
-    least = 2.0 ** -25 if dtype is torch.float16 else 0.0
-    moved = 2 * (u * w["reach"] + least * w["qsum"])[..., None]  # the scores, and their maximum
-    plain = attn_plain.attention_bound(w["out"], w["size"] * (1 + u), w["reach"] * (1 + u),
-                                       max_kv * 8 * w["most"][..., None], dtype, max_kv)
-    return plain + (u + 1.01 * moved + moved ** 2) * (1 + u) * w["size"] + 2 * least
+    """Many rows: keys and values are rounded to fp16 first (2^-11; below its normal range, of a
+    16th of them for bf16, by 2^-25 of what is held), q is exact but for 2^-39 of its row's largest;
+    scores of dim products in fp32 (each at most 2^-23 of the products' sizes, taken dim + 8
+    times), their scaling and the exponential; p, 2^8 at most, is rounded to fp16 (2^-25 below its normal
+    range, for every key, over a sum of 1 at least); sums of max_kv terms that may be
+    truncated; the output once."""
+    u, h = UNIT[dtype], 2.0 ** -11
+    least = 2.0 ** -25 * (1 if dtype is torch.float16 else 16)
+    e = 2 * ((dim + 8) * 2.0 ** -23 * (1 + h) + h) * w["reach"] + 2 * least * w["qsum"] + 2.0 ** -30 * w["coded"]
+    e = e[..., None] + max_kv * 2.0 ** -23 + 2.0 ** -20
+    tiny = 2.0 ** -25 * max_kv * 8 * w["most"][..., None]
+    return u * np.abs(w["out"]) + (2 * h + h * h + e + e * e) * (1 + u) * w["size"] + tiny + 2 * least + 2.0 ** -24
 
 
 def fork(parents, past, page, free, table):
