@@ -62,7 +62,7 @@ void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int dim, in
   // Long requests in chunks of 1024 to 2048 keys, about 256 CTAs of them or more, joined by a
   // second kernel (2.5 us): no cluster then waits for room on one part of the chip, and lengths
   // that differ even out (16 requests of 130 to 16384 keys and 64 heads: 37.5 us in clusters,
-  // 33.0 in chunks; 64 of 12000 to 16384: 209 and 201; one of 32768: 21.4 and 15.4; 20 of 400 to
+  // 31.4 in chunks; 64 of 12000 to 16384: 209 and 190; one of 32768: 21.4 and 14.6; 20 of 400 to
   // 3000: 19.4 and 25.7).  Where the keys take half the time (heads of 64) or tiles are fewer at
   // a time (16 rows) from twice that length on.
   const int64_t chunk = std::min<int64_t>(2048, std::max<int64_t>(1024, (max_kv * items / 256 + 127) / 128 * 128));

@@ -20,17 +20,21 @@
 //
 // Bound by the issue of its instructions, not far from HBM: 16 keys and values of a head of
 // 128 are 2304 bytes, which an SM's share of the bandwidth brings in 96 cycles.  Four
-// schedulers have 384 issue slots in that time; the step takes about 270 with 8 columns, 16 of
-// them products that keep a scheduler for 7 cycles each.  64 requests of 16384 keys (32 heads
-// of 128 over 8): 233 us, 5.2 TB/s, 77 % of the copy rate; the copies without the arithmetic
-// take 170, the arithmetic on pages in L2 229.  What did not help: the next step's scores
-// beside this one's outputs (236), four CTAs an SM with two stages (249), 16 keys a step (262).
+// schedulers have 384 issue slots in that time; the step takes about 280 with 8 columns, 16 of
+// them products that keep a scheduler for 7 cycles each.  64 requests of 12000 to 16384 keys (32
+// heads of 128 over 8): 190 us, 5.5 TB/s, 81 % of the copy rate (the copies without the
+// arithmetic run at 105 %); 16 of 130 to 16384 (64 heads) 31.4, the longest ones' chunks and the
+// second kernel being last; one of 2047 keys 5.1.  With 16 columns 32 requests of 16384 keys
+// and 4 heads take 102 us, 44 % of that rate.  What did not help: the next step's scores beside
+// this one's outputs (236 us against 233 at the time), four CTAs an SM with shorter rings (249),
+// 16 keys a step (244 against 216).
 // A block of the cache is one bulk copy into a ring that each warp has for itself, with a
 // barrier for each stage and no other wait in the loop.  The codes lie so that each lane's are
 // vector loads without bank conflicts (the keys' order in a tile, key_slot below, is chosen for
 // that), and that neighbours in an operand are the halves of a word (keys) or one byte
-// permutation apart (values).  The rest is as in attn_rows.cu: 32 steps' table entries
-// read ahead, splits of a tile's keys joined in a cluster in a fixed order.
+// permutation apart (values).  The rest is as in attn_rows.cu: 32 blocks' table entries
+// read ahead, splits of a tile's keys joined in a cluster, or chunks of them by
+// attn_join_kernel, in a fixed order.
 #include <algorithm>
 
 #include "attn.cuh"
@@ -42,13 +46,23 @@ namespace {
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kBlocks = 2;                  // of the cache in a warp's step
-constexpr int kStep = kBlocks * kQ4Slots;   // its keys
-constexpr int kStages = 3;                  // steps in a warp's ring
-constexpr int kAhead = 32 / kBlocks;        // steps whose blocks the lanes hold
+// How a tile's keys are split over CTAs: not; over those of a cluster, in turn, which join them
+// there; or in chunks, whose results attn_join_kernel joins.
+enum Split { kWhole, kCluster, kChunks };
 
-template <int D, int R, bool CL>  // (CL: joined in a cluster)
+// A warp's steps: long chunks go 64 keys at a time (64 requests of 12000 to 16384 keys: 202 us
+// by 32, 190 by 64), with fewer votes, branches and waits a key; else 32 spread a request's keys
+// over more warps (one of 2047: 5.2 us, 6.4 by 64).
+template <Split SPLIT>
+struct Ring {
+  static constexpr int kBlocks = SPLIT == kChunks ? 4 : 2;  // of the cache in a step
+  static constexpr int kStages = SPLIT == kChunks ? 2 : 3;  // steps
+};
+
+template <int D, int R, Split SPLIT>
 struct RowsQ4Smem {
+  static constexpr int kBlocks = Ring<SPLIT>::kBlocks, kStages = Ring<SPLIT>::kStages;
+  static constexpr bool CL = SPLIT == kCluster;
   static constexpr int STAGE = kBlocks * Q4Block<D>::kBytes;
   static constexpr int RING = kStages * STAGE;  // of a warp
   static constexpr int LD = D + 4;  // of the warps' outputs, which follow
@@ -133,17 +147,16 @@ __device__ __forceinline__ void peer_store(uint32_t addr, float4 v, uint32_t bar
       : "memory");
 }
 
-// How a tile's keys are split over CTAs: not; over those of a cluster, in turn, which join them
-// there; or in chunks, whose results attn_join_kernel joins.
-enum Split { kWhole, kCluster, kChunks };
-
 // NT tiles of 8 rows (tokens x heads).
 template <typename T, int D, int NT, Split SPLIT>
 __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     attn_rows_q4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Q4Cache c4) {
   constexpr int R = 8 * NT;
   constexpr bool CL = SPLIT == kCluster;
-  using S = RowsQ4Smem<D, R, CL>;
+  using S = RowsQ4Smem<D, R, SPLIT>;
+  constexpr int kBlocks = S::kBlocks, kStages = S::kStages;
+  constexpr int kStep = kBlocks * kQ4Slots;  // keys of a step
+  constexpr int kAhead = 32 / kBlocks;       // steps whose blocks the lanes hold
   using B = Q4Block<D>;
   constexpr int W = D / 8;      // words of a slot
   constexpr int KW = W / 4;     // that a lane has of a key's
@@ -175,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
   const auto leave = [&]() {
     if constexpr (CL) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   };
-  // the keys go to the splits of a cluster and their warps 32 at a time in turn
+  // the keys go to the splits of a cluster and their warps a step at a time in turn
   const int chunk0 = SPLIT == kChunks ? z * a.chunk : 0;
   const auto key_of = [&](int s) { return chunk0 + kStep * (warp + kWarps * (CL ? z + a.nsplit * s : s)); };
   const int64_t width = static_cast<int64_t>(a.table_width) << a.page_shift;
@@ -722,7 +735,7 @@ template <typename T, int D, int NT, Split SPLIT>
 cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
   constexpr bool CL = SPLIT == kCluster;
   auto kern = attn_rows_q4_kernel<T, D, NT, SPLIT>;
-  constexpr int smem = RowsQ4Smem<D, 8 * NT, CL>::TOTAL;
+  constexpr int smem = RowsQ4Smem<D, 8 * NT, SPLIT>::TOTAL;
   cudaError_t e = ensure_smem(kern, smem);
   if (e != cudaSuccess) return e;
   if (CL && a.nsplit > 8) {
