@@ -69,22 +69,24 @@ typedef enum {
 /* bits OR-ed into *dev_status by the kernels */
 #define SSS_FLAG_NONFINITE 0x1u /* a weight group contains NaN or +-Inf; that group's
                                    codes/scale are placeholders (u = 2^(q-1) and s = +0
-                                   for symmetric grids, u = 0 and s = +0 for ASYM)     */
+                                   for symmetric grids, u = 0 and s = +0 for ASYM);
+                                   sss_kv_store_q4: a group of a head does             */
 #define SSS_FLAG_RANGE 0x2u     /* sss_quantize: a stored fp16 scale or min is infinite
                                    (|s| >= 65520), or the fp32 ASYM step overflowed
                                    (codes then 0).  sss_gemv at batch 2..16 and
                                    sss_gemm: a group's fp16 weight operand may overflow
                                    (see those calls); their outputs may then hold
-                                   inf or NaN                                         */
+                                   inf or NaN.  sss_kv_store_q4: see there             */
 #define SSS_FLAG_TIMEOUT 0x4u   /* a bounded pipeline wait of sss_gemm (or
                                    sss_gemm_noalloc), sss_quantize,
-                                   sss_quantize_rotated or sss_attention expired; the
-                                   output is incomplete                               */
-#define SSS_FLAG_INDEX 0x8u     /* sss_page_plan, sss_qk_norm_rope, sss_attention: a length,
-                                   position, slot or page lies outside what the call's
+                                   sss_quantize_rotated, sss_attention or
+                                   sss_attention_q4 expired; the output is incomplete  */
+#define SSS_FLAG_INDEX 0x8u     /* sss_page_plan, sss_qk_norm_rope, sss_attention, and the
+                                   calls on the 4-bit cache and on shared pages: a length,
+                                   position, slot, parent or page lies outside what the call's
                                    arguments allow; what the calls do then is said there */
-#define SSS_FLAG_PAGES 0x10u    /* sss_page_plan: the free pages, or the table's columns, do
-                                   not suffice                                         */
+#define SSS_FLAG_PAGES 0x10u    /* sss_page_plan, sss_page_fork: the free pages, or the
+                                   table's columns, do not suffice                     */
 
 typedef enum { SSS_OUT_F32 = 0, SSS_OUT_F16 = 1, SSS_OUT_BF16 = 2 } sss_dtype_t;
 
@@ -767,7 +769,7 @@ size_t sss_gemm_noalloc_max_scratch_bytes(void);
  * counterpart.  While a bit below is set, every later launch of that kernel
  * family leaves one mbarrier one arrive short: the GEMM on the first
  * stage's weight tile, the attention of many rows on its first value tile (of few
- * rows whose keys are split: on what a CTA's peers store into it).  The decode GEMV kernels (batch 1 and batched) have no data-dependent waits (their
+ * rows whose keys are split over a cluster: on what a CTA's peers store into it).  The decode GEMV kernels (batch 1 and batched) have no data-dependent waits (their
  * warps meet only at CTA-wide barriers), so their bits have no effect.  The wait
  * on that barrier then runs out after its bound (about one second), the kernel
  * raises SSS_FLAG_TIMEOUT in dev_status, lets its own copies and MMAs in flight
@@ -781,8 +783,9 @@ size_t sss_gemm_noalloc_max_scratch_bytes(void);
 #define SSS_TEST_STALL_GEMM 0x4u       /* gemm_kernel (sss_gemm, sss_gemm_noalloc)             */
 #define SSS_TEST_STALL_ATTENTION 0x8u  /* attn_prompt_kernel (sss_attention of many rows): the
                                           first value tile is never handed on              */
-#define SSS_TEST_STALL_ATTENTION_ROWS 0x10u /* attn_rows_kernel (of few rows), where keys are
-                                          split: each CTA expects 16 bytes too many        */
+#define SSS_TEST_STALL_ATTENTION_ROWS 0x10u /* attn_rows_kernel, attn_rows_q4_kernel (of few
+                                          rows), where a cluster shares the keys: each CTA
+                                          expects 16 bytes too many                        */
 void sss_test_set_stall(uint32_t mask);
 
 #ifdef __cplusplus
