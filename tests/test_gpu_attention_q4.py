@@ -151,6 +151,64 @@ def test_keys_in_chunks(fresh, kv, hq, hkv, dim, dtype, page):
     assert torch.equal(got, call(c, cache=cache))
 
 
+@pytest.mark.parametrize("n,most,hq,hkv,dim,dtype", [(64, 300, 8, 8, 64, FP), (44, 700, 128, 8, 128, BF), (320, 90, 1, 1, 128, BF)])
+def test_more_requests_than_sms(n, most, hq, hkv, dim, dtype):
+    # keys of a tile in one CTA
+    c = make([1] * n, [(37 * i) % most for i in range(n)], hq, hkv, dim, dtype, 32, seed=52)
+    check(c, call(c))
+
+
+def test_pages_past_four_gigabytes():
+    # a cache whose bytes are past 2^32, and a request whose pages lie at both of its ends;
+    # one of them is copied to the far end first
+    hq, hkv, dim, page = 8, 8, 128, 256
+    pages = 2 ** 33 // (hkv * (page // 16) * 18 * dim) + 3
+    cache = sss.empty_kv_cache_q4(pages, page, hkv, dim)
+    c = make([1], [700], hq, hkv, dim, BF, page, seed=53, spare=0)
+    near, far = [int(x) for x in c["table"][0, :3]], [pages - 1, 1, pages - 2]
+    small = cache_of(c)
+    for a, b in zip(near, far[:2] + [0]):
+        cache.blocks[b] = small.blocks[a]
+    one = lambda x: torch.tensor([x], dtype=torch.int32, device=DEV)  # noqa: E731
+    sss.sss_page_copy(cache, one(0), one(far[2]))
+    want = call(c)
+    c["table"][0, :3] = torch.tensor(far, dtype=torch.int32)
+    assert torch.equal(call(c, cache=cache), want)
+    slots = torch.tensor(far[0] * page + np.arange(256), dtype=torch.int32, device=DEV)
+    k, v = sss.sss_kv_fetch_q4(cache, slots)
+    assert bool(torch.isfinite(k).all()) and float(k.abs().max()) > 0
+    many = make([90], [700], hq, 1, dim, BF, page, seed=54, spare=0)  # (the copy for many rows, too)
+    check(many, call(many))
+
+
+def test_two_graphs_that_share_a_workspace():
+    # replayed one after the other, each starts from whatever the other left there
+    runs, ws = [], None
+    for fresh, kv, hkv, dtype, seed in (([1] * 5, [9000, 30, 1500, 2048, 4097], 8, BF, 55), ([100, 60], [300, 700], 2, BF, 56),
+                                        ([90], [500], 2, FP, 57)):
+        c = make(fresh, kv, 8, hkv, 128, dtype, 16, seed=seed)
+        runs.append((c, cache_of(c), call(c)))
+    need = [sss.sss_attention_q4_workspace_bytes(sum(np.diff(c["cu"])), 8, cache, len(c["kv"]), int(np.diff(c["cu"]).max()),
+                                                 max(c["kv"])) for c, cache, _ in runs]
+    assert min(need) > 0
+    ws = torch.empty(max(need), dtype=torch.uint8, device=DEV)
+    graphs = []
+    for c, cache, want in runs:
+        ints = lambda x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+        args = (c["q"].to(DEV), cache, ints(c["cu"]), ints(c["kv"]), int(np.diff(c["cu"]).max()), max(c["kv"]), c["table"].to(DEV))
+        out, graph = torch.empty(c["q"].shape, dtype=c["q"].dtype, device=DEV), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sss.sss_attention_q4(*args, out=out, workspace=ws)
+        graphs.append((graph, out, want, args))
+    ws.fill_(0xFF)
+    for i in (0, 1, 2, 1, 0, 2, 0, 0, 1):
+        graph, out, want, _ = graphs[i]
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out.cpu(), want)
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("spread,scale", [(8.0, None), (1.0, 1e-6), (1.0, 3.0), (200.0, 1e-3), (1e-4, 50.0)])
 def test_sharp_flat_and_far_scores(dtype, spread, scale):
