@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
         sums[e / PER] += (__low2float(v) + __high2float(v)) * (e & 1 ? 16.f : 1.f);
       }
     // 2^(E - 14) of the scale, and the 2^24 of the nibbles'
-    const float rs = fminf(a.scale_log2 * __int_as_float((min(E, 127) - 14 + 127) << 23) * 0x1p24f, 3e38f);
+    const float rs = fminf(fmaxf(1e-37f, a.scale_log2 * __int_as_float((min(E, 127) - 14 + 127) << 23) * 0x1p24f), 3e38f);  // (for what is multiplied by infinities)
     const int limit = in ? attn_limit(rq, i0 + i) : 0;
 #pragma unroll
     for (int g = 0; g < G; ++g) {
@@ -353,7 +353,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     for (int g = 0; g < G; ++g) asm volatile("" : "+f"(start[m][g][2]), "+f"(start[m][g][3]));
 
   float o[NT][4][VW][4];  // rows 2 c, 2 c + 1 of dimensions 2 W e + w and 2 W e + W + w
-  float mx[NT][2], ref[NT][2], sum[NT][2];  // (ref: mx, or 0 where that is -inf)
+  float mx[NT][2], ref[NT][2], sum[NT][2];  // (ref: what scaled scores are added to: -mx scaled, or 0)
 #pragma unroll
   for (int m = 0; m < NT; ++m) {
 #pragma unroll
@@ -448,13 +448,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
             x[u][m][i] = g == 0 ? ks[i >> 1][g] * acc[m][i] : x[u][m][i] + ks[i >> 1][g] * acc[m][i];
       }
     }
-    // scale, mask, and raise the maxima where a score passes them
-#pragma unroll
-    for (int u = 0; u < kBlocks; ++u)
-#pragma unroll
-      for (int m = 0; m < NT; ++m)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[u][m][i] *= rscale[m][i & 1];
+    // mask, and raise the maxima (not yet scaled, as the scores) where a score passes them
     if (rare) {  // no page: zeros (what the stage holds is of any kind); not seen: -inf
 #pragma unroll
       for (int u = 0; u < kBlocks; ++u)
@@ -485,9 +479,9 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
           float t = fmaxf(top[m][k], mx[m][k]);
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-          const float f = t == -INFINITY ? 1.f : ex2(mx[m][k] - t);
+          const float f = t == -INFINITY ? 1.f : ex2((mx[m][k] - t) * rscale[m][k]);
           mx[m][k] = t;
-          ref[m][k] = t == -INFINITY ? 0.f : t;
+          ref[m][k] = t == -INFINITY ? 0.f : -t * rscale[m][k];
           sum[m][k] *= f;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -504,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
       for (int m = 0; m < NT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          x[u][m][i] = ex2(x[u][m][i] - ref[m][i & 1]);
+          x[u][m][i] = ex2(__fmaf_rn(x[u][m][i], rscale[m][i & 1], ref[m][i & 1]));
           sum[m][i & 1] += x[u][m][i];
         }
     // outputs
@@ -617,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) sum[m][k] += __shfl_xor_sync(0xffffffffu, sum[m][k], d);
       if (r == 0) {
-        wmax[warp][row] = mx[m][k];
+        wmax[warp][row] = mx[m][k] * rscale[m][k];
         wsum[warp][row] = sum[m][k];
       }
       float* dst = part + (warp * R + row) * LD + VW * r;
