@@ -7,9 +7,10 @@
 // words of the cache's layout of them (kv_q4.cuh).  Fetch goes the same way back.
 //
 // Bound by instruction issue and by HBM (2 or 4 bytes a value in and 9/16 out, or the other way
-// round), so an item has little around its values: a warp takes a token's keys or its
-// values, kUnroll groups of heads with all of their loads in flight, and steps from group to
-// group by adding to two addresses.
+// round), so an item has little around its values: a warp takes 256 / D tokens' keys or their
+// values, kUnroll heads with all of their loads in flight, and steps from head to head by
+// adding to two addresses.  (Tokens beside each other and not heads: no lane is idle whatever
+// their number, and slots in order share sectors.)
 #include <algorithm>
 
 #include "kv_q4.cuh"
@@ -181,51 +182,52 @@ __device__ __forceinline__ uint32_t quantize8(const Raw<T>& v, uint16_t& s16, ui
   return packed(u, q.far);
 }
 
-// Grid: tokens, kWarps to a CTA; runs of heads, of the keys and then of the values.
+// Grid: tokens, kWarps times 256 / D to a CTA; runs of heads, of the keys and then of the values.
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) kv_store_q4_kernel(const __grid_constant__ StoreArgs a) {
   using B = Q4Block<D>;
-  constexpr int LANES = D / 8, GH = 32 / LANES;
+  constexpr int LANES = D / 8, TOKENS = 32 / LANES;
   constexpr int U = sizeof(T) == 4 ? kUnroll / 2 : kUnroll;
-  const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, l = lane % LANES;
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * TOKENS;
+  const int64_t t = first + lane / LANES;
   const int runs = gridDim.y / 2;
   const bool is_v = blockIdx.y >= runs;
   const int h0 = (blockIdx.y - (is_v ? runs : 0)) * a.run, h1 = min(a.cache.heads, h0 + a.run);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (t >= a.tokens) return;
+  if (first >= a.tokens) return;
+  const bool in = t < a.tokens;
   const T* src = (is_v ? static_cast<const T*>(a.v) + t * a.v_stride : static_cast<const T*>(a.k) + t * a.k_stride) +
-                 (h0 + sub) * D + 8 * l;
-  const int64_t slot = a.slots ? a.slots[t] : t;
+                 h0 * D + 8 * l;
+  const int64_t slot = !in ? -1 : a.slots ? a.slots[t] : t;
   const bool keep = slot >= 0 && slot < a.cache.slots;
   uint32_t flags = slot >= a.cache.slots ? SSS_FLAG_INDEX : 0u;
-  const int in = static_cast<int>(slot) & ((1 << a.cache.shift) - 1), j = in & 15;
+  const int at = static_cast<int>(slot) & ((1 << a.cache.shift) - 1), j = at & 15;
   const int per_head = B::kBytes << (a.cache.shift - 4);  // bytes of a head's blocks in a page
   const int word = q4_word<D>(l);
-  char* head = a.cache.blocks + (slot >> a.cache.shift) * a.cache.page_stride + (in >> 4) * B::kBytes +
-               static_cast<int64_t>(h0 + sub) * per_head + (is_v ? B::kV : B::kK);
+  char* head = a.cache.blocks + (slot >> a.cache.shift) * a.cache.page_stride + (at >> 4) * B::kBytes +
+               static_cast<int64_t>(h0) * per_head + (is_v ? B::kV : B::kK);
   const int code_at = j * B::kRow + 4 * (is_v ? q4_value_word<D>(word, j) : word);
   const int scale_at = B::kKS + j * B::kScales + 2 * (l >> 2);  // (the scales follow the codes)
-  for (int h = h0; h < h1; h += U * GH) {
+  for (int h = h0; h < h1; h += U) {
     Raw<T> x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       x[u].zero();
-      if (h + u * GH + sub < h1) x[u].load(src + u * GH * D);
+      if (keep && h + u < h1) x[u].load(src + u * D);
     }
-    src += U * GH * D;
-    if (!keep) break;
+    src += U * D;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (h + u * GH >= h1) break;
+      if (h + u >= h1) break;
       uint16_t s16;
       const uint32_t w = q4_transpose<D>(quantize8(x[u], s16, flags), l);
-      if (h + u * GH + sub < h1) {
+      if (keep) {
         *reinterpret_cast<uint32_t*>(head + code_at) = w;
         if ((l & 3) == 0) *reinterpret_cast<uint16_t*>(head + scale_at) = s16;
       }
-      head += GH * per_head;
+      head += per_head;
     }
   }
   if (flags && a.status) atomicOr(a.status, flags);
@@ -277,31 +279,35 @@ __device__ __forceinline__ void store8(T* p, float (&f)[8], bool in) {
 template <typename T, int D, bool STAGE>
 __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_constant__ FetchArgs a) {
   using B = Q4Block<D>;
-  constexpr int LANES = D / 8, GH = 32 / LANES;
-  const int lane = threadIdx.x & 31, sub = lane / LANES, l = lane % LANES;
-  const int64_t t = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+  constexpr int LANES = D / 8, TOKENS = 32 / LANES;
+  const int lane = threadIdx.x & 31, l = lane % LANES;
+  const int64_t first = (static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * TOKENS;
+  const int64_t t = first + lane / LANES;
   const int runs = gridDim.y / 2, shift = a.cache.shift;
   const bool is_v = blockIdx.y >= runs;
   const int h0 = (blockIdx.y - (is_v ? runs : 0)) * a.run, h1 = min(a.cache.heads, h0 + a.run);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (t >= a.rows) return;
+  if (first >= a.rows) return;
+  bool in = t < a.rows;  // the row is written
   uint32_t flags = 0;
-  int64_t slot, row = t;
+  int64_t slot = -1, row = t;
   if constexpr (STAGE) {
     const Q4Stage& s = a.stage;
     const int b = blockIdx.z;
-    const int64_t p = t >> shift;
+    const int64_t p = first >> shift;  // (a warp's rows are of one page)
     const int32_t page = __ldg(s.table + static_cast<int64_t>(b) * s.table_width + p);
     const bool real = page >= 0 && page < a.cache.slots >> shift;
     // the copy's table, of the pages that are real (what is none, and keys past the
     // request's, are the attention's to flag)
-    if (blockIdx.y == 0 && lane == 0 && (t & ((1 << shift) - 1)) == 0)
+    if (blockIdx.y == 0 && lane == 0 && (first & ((1 << shift) - 1)) == 0)
       s.new_table[static_cast<int64_t>(b) * s.pages + p] = real ? b * s.pages + static_cast<int32_t>(p) : -1;
-    if (!real || t >= s.kv_len[b] || t >= s.max_kv) return;
+    const int64_t keys = min(static_cast<int64_t>(s.kv_len[b]), s.max_kv);
+    if (!real || first >= keys) return;
+    in = t < keys;
     row += static_cast<int64_t>(b) * s.pages << shift;
     slot = (static_cast<int64_t>(page) << shift) + (t & ((1 << shift) - 1));
-  } else {
+  } else if (in) {
     slot = a.slots ? a.slots[t] : t;
     if (slot >= a.cache.slots) {
       flags |= SSS_FLAG_INDEX;
@@ -310,36 +316,36 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
   }
   T* out = static_cast<T*>(is_v ? a.v : a.k);
   if (out != nullptr) {
-    out += (row * a.cache.heads + h0 + sub) * D + 8 * l;
-    const int in = static_cast<int>(slot) & ((1 << shift) - 1), j = in & 15;
+    out += (row * a.cache.heads + h0) * D + 8 * l;
+    const int at = static_cast<int>(slot) & ((1 << shift) - 1), j = at & 15;
     const int per_head = B::kBytes << (shift - 4), word = q4_word<D>(l);
-    const char* head = a.cache.blocks + (slot >> shift) * a.cache.page_stride + (in >> 4) * B::kBytes +
-                       static_cast<int64_t>(h0 + sub) * per_head + (is_v ? B::kV : B::kK);
+    const char* head = a.cache.blocks + (slot >> shift) * a.cache.page_stride + (at >> 4) * B::kBytes +
+                       static_cast<int64_t>(h0) * per_head + (is_v ? B::kV : B::kK);
     const int code_at = j * B::kRow + 4 * (is_v ? q4_value_word<D>(word, j) : word);
     const int scale_at = B::kKS + j * B::kScales + 2 * (l >> 2);
-    for (int h = h0; h < h1; h += kUnroll * GH) {
+    for (int h = h0; h < h1; h += kUnroll) {
       uint32_t w[kUnroll];
       uint16_t s16[kUnroll];
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
         w[u] = 0x88888888u;
         s16[u] = 0;
-        if (slot >= 0 && h + u * GH + sub < h1) {
+        if (in && slot >= 0 && h + u < h1) {
           w[u] = __ldg(reinterpret_cast<const uint32_t*>(head + code_at));
           s16[u] = __ldg(reinterpret_cast<const uint16_t*>(head + scale_at));
         }
-        head += GH * per_head;
+        head += per_head;
       }
 #pragma unroll
       for (int u = 0; u < kUnroll; ++u) {
-        if (h + u * GH >= h1) break;
+        if (h + u >= h1) break;
         const uint32_t c = q4_transpose<D>(w[u], l);
         float s = __half2float(__ushort_as_half(s16[u]));
         if constexpr (STAGE) s *= a.stage.times;
         // A nibble at bits 4 n of a float of 2^23 and more is 2^23 + 16^n u: times s / 16^n, less
         // s (2^23 / 16^n + 8).  For n = 2, 3 and 4 that constant is exact in fp32, and so is the
         // result of one multiply-add.
-        const uint32_t at[3] = {c << 8, c >> 4, c >> 16};
+        const uint32_t part[3] = {c << 8, c >> 4, c >> 16};
         float f[8], by[3], less[3];
 #pragma unroll
         for (int n = 0; n < 3; ++n) {
@@ -348,10 +354,10 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          f[e] = __fmaf_rn(__uint_as_float((at[e / 3] & (15u << (4 * (e % 3 + 2)))) | 0x4B000000u),
+          f[e] = __fmaf_rn(__uint_as_float((part[e / 3] & (15u << (4 * (e % 3 + 2)))) | 0x4B000000u),
                            by[e % 3], less[e % 3]);
-        store8(out, f, h + u * GH + sub < h1);
-        out += GH * D;
+        store8(out, f, in);
+        out += D;
       }
     }
   }
@@ -406,16 +412,15 @@ __global__ void __launch_bounds__(kThreads) q_stage_kernel(const __grid_constant
 
 template <typename K, typename A>
 cudaError_t launch(K kern, A& a, int64_t rows, int dim, int batch, cudaStream_t stream) {
-  // A token's keys (or values) to a warp, or where that gives an SM fewer than 16 warps as many
-  // runs of its heads as do.
-  const int gh = 256 / dim, groups = (a.cache.heads + gh - 1) / gh;
-  const int64_t all = int64_t{16} * device_sm_count();
-  int runs = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(groups, all / std::max<int64_t>(1, 2 * rows * batch))));
-  const int of = (groups + runs - 1) / runs;
-  runs = (groups + of - 1) / of;
-  a.run = of * gh;
+  // All heads to a warp, or where that gives an SM fewer than 16 warps as many runs of them as do.
+  const int64_t all = int64_t{16} * device_sm_count(), tokens = kWarps * 256 / dim;  // of a CTA
+  const int64_t warps = std::max<int64_t>(1, 2 * batch * ((rows + 256 / dim - 1) / (256 / dim)));
+  const int heads = a.cache.heads;
+  int runs = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(heads, all / warps)));
+  a.run = (heads + runs - 1) / runs;
+  runs = (heads + a.run - 1) / a.run;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((rows + kWarps - 1) / kWarps), static_cast<unsigned>(2 * runs), static_cast<unsigned>(batch));
+  cfg.gridDim = dim3(static_cast<unsigned>((rows + tokens - 1) / tokens), static_cast<unsigned>(2 * runs), static_cast<unsigned>(batch));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];

@@ -9,7 +9,7 @@ from test_kernel_order import kernel_text
 
 
 @pytest.mark.parametrize("file,name,reads", [
-    ("kv_q4.cu", "kv_store_q4_kernel", ("a.slots[", "load(t")), ("kv_q4.cu", "kv_fetch_q4_kernel", ("a.slots[", "table[p]", "kv_len")),
+    ("kv_q4.cu", "kv_store_q4_kernel", ("a.slots[", "x[u].load(")), ("kv_q4.cu", "kv_fetch_q4_kernel", ("a.slots[", "s.table +", "s.kv_len[")),
     ("attn_rows_q4.cu", "attn_rows_q4_kernel", ("attn_tile(", "page = entry(")),
     ("page_share.cu", "page_fork_kernel", ("a.parents[", "a.past[", "a.table")), ("page_share.cu", "page_map_kernel", ("a.table", "held_entries(")),
     ("page_share.cu", "page_copy_kernel", ("a.src[", "a.dst[")),
