@@ -22,10 +22,10 @@
 // 128 are 2304 bytes, which an SM's share of the bandwidth brings in 96 cycles.  Four
 // schedulers have 384 issue slots in that time; the step takes about 280 with 8 columns, 16 of
 // them products that keep a scheduler for 7 cycles each.  64 requests of 12000 to 16384 keys (32
-// heads of 128 over 8): 190 us, 5.5 TB/s, 81 % of the copy rate (the copies without the
-// arithmetic run at 105 %); 16 of 130 to 16384 (64 heads) 31.4, the longest ones' chunks and the
+// heads of 128 over 8): 188 us, 5.6 TB/s, 82 % of the copy rate (the copies without the
+// arithmetic run at 105 %); 16 of 130 to 16384 (64 heads) 31.0, the longest ones' chunks and the
 // second kernel being last; one of 2047 keys 5.1.  With 16 columns 32 requests of 16384 keys
-// and 4 heads take 102 us, 44 % of that rate.  What did not help: the next step's scores beside
+// and 4 heads take 107 us, 42 % of that rate.  What did not help: the next step's scores beside
 // this one's outputs (236 us against 233 at the time), four CTAs an SM with shorter rings (249),
 // 16 keys a step (244 against 216).
 // A block of the cache is one bulk copy into a ring that each warp has for itself, with a
