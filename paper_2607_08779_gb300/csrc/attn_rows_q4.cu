@@ -22,10 +22,11 @@
 // 128 are 2304 bytes, which an SM's share of the bandwidth brings in 96 cycles.  Four
 // schedulers have 384 issue slots in that time; the step takes about 280 with 8 columns, 16 of
 // them products that keep a scheduler for 7 cycles each.  64 requests of 12000 to 16384 keys (32
-// heads of 128 over 8): 188 us, 5.6 TB/s, 82 % of the copy rate (the copies without the
-// arithmetic run at 105 %); 16 of 130 to 16384 (64 heads) 31.0, the longest ones' chunks and the
-// second kernel being last; one of 2047 keys 5.1.  With 16 columns 32 requests of 16384 keys
-// and 4 heads take 107 us, 42 % of that rate.  What did not help: the next step's scores beside
+// heads of 128 over 8): 185 us, 5.6 TB/s, 84 % of the copy rate (the copies without the
+// arithmetic run at 105 %); 16 of 130 to 16384 (64 heads) 30.9, the longest ones' chunks and the
+// second kernel being last; one of 2047 keys 4.8.  With 16 columns 32 requests of 16384 keys
+// and 4 heads take 100 us, 45 % of that rate; a CTA more an SM with heads of 64 (64 requests of
+// 8000 to 16384 keys: 107 us, 99.6).  What did not help: the next step's scores beside
 // this one's outputs (236 us against 233 at the time), four CTAs an SM with shorter rings (249),
 // 16 keys a step (244 against 216).
 // A block of the cache is one bulk copy into a ring that each warp has for itself, with a
@@ -149,7 +150,7 @@ __device__ __forceinline__ void peer_store(uint32_t addr, float4 v, uint32_t bar
 
 // NT tiles of 8 rows (tokens x heads).
 template <typename T, int D, int NT, Split SPLIT>
-__global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
+__global__ void __launch_bounds__(kThreads, (NT == 1 ? 3 : 2) + (D == 64 ? 1 : 0))
     attn_rows_q4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Q4Cache c4) {
   constexpr int R = 8 * NT;
   constexpr bool CL = SPLIT == kCluster;
@@ -316,9 +317,6 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
     // 2^(14 - E) for a largest size of 2^E and more
     const int E = max(static_cast<int>(__float_as_uint(top) >> 23 & 255u) - 127, -112);
     const float up = __int_as_float((14 - min(E, 127) + 127) << 23);
-    float sums[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) sums[g] = 0.f;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -326,31 +324,30 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
         const float f = e & 1 ? up * 0.0625f : up;
         const __half2 v = __floats2half2_rn(x[e][0][w] * f, x[e][1][w] * f);
         qf[m][e][w] = *reinterpret_cast<const uint32_t*>(&v);
-        sums[e / PER] += (__low2float(v) + __high2float(v)) * (e & 1 ? 16.f : 1.f);
       }
     // 2^(E - 14) of the scale, and the 2^24 of the nibbles'
     const float rs = fminf(fmaxf(1e-37f, a.scale_log2 * __int_as_float((min(E, 127) - 14 + 127) << 23) * 0x1p24f), 3e38f);  // (for what is multiplied by infinities)
     const int limit = in ? attn_limit(rq, i0 + i) : 0;
+    // -8 times q's sums: products with codes that are all -8
 #pragma unroll
     for (int g = 0; g < G; ++g) {
-      sums[g] += __shfl_xor_sync(0xffffffffu, sums[g], 1);
-      sums[g] += __shfl_xor_sync(0xffffffffu, sums[g], 2);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) start[m][g][k] = 0.f;
+#pragma unroll
+      for (int e = g * PER; e < g * PER + PER; ++e)
+#pragma unroll
+        for (int w = 0; w < KW; w += 2) {
+          const uint32_t less = e & 1 ? 0x80808080u : 0x80088008u;
+          mma_f16(start[m][g], less, less, less, less, qf[m][e][w], qf[m][e][w + 1]);
+        }
     }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int from = 4 * (2 * c + k);
-#pragma unroll
-      for (int g = 0; g < G; ++g)
-        start[m][g][k] = start[m][g][2 + k] = -0x1p-21f * __shfl_sync(0xffffffffu, sums[g], from);
       rscale[m][k] = __shfl_sync(0xffffffffu, rs, from);
       lim[m][k] = __shfl_sync(0xffffffffu, limit, from);
     }
   }
-
-#pragma unroll
-  for (int m = 0; m < NT; ++m)  // (the compiler would make the second halves anew for each product)
-#pragma unroll
-    for (int g = 0; g < G; ++g) asm volatile("" : "+f"(start[m][g][2]), "+f"(start[m][g][3]));
 
   float o[NT][4][VW][4];  // rows 2 c, 2 c + 1 of dimensions 2 W e + w and 2 W e + W + w
   float mx[NT][2], ref[NT][2], sum[NT][2];  // (ref: what scaled scores are added to: -mx scaled, or 0)
@@ -619,9 +616,14 @@ __global__ void __launch_bounds__(kThreads, NT == 1 ? 3 : 2)
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int w = 0; w < VW; ++w)
-            dst[2 * W * e + W * h + w] = o[m][e][w][2 * h + k] * (e & 1 ? 0x1p20f : 0x1p24f);
+        {
+          constexpr float kUnit[2] = {0x1p24f, 0x1p20f};
+          float* to = dst + 2 * W * e + W * h;
+          if constexpr (VW == 2)
+            *reinterpret_cast<float2*>(to) = make_float2(o[m][e][0][2 * h + k] * kUnit[e & 1], o[m][e][1][2 * h + k] * kUnit[e & 1]);
+          else
+            *to = o[m][e][0][2 * h + k] * kUnit[e & 1];
+        }
     }
   __syncthreads();
   // pieces of 16 bytes; with CL those of a split follow one another in `gather`
