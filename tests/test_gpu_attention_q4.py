@@ -277,6 +277,33 @@ def test_lengths_that_cannot_be():
     assert int(status) == sss.FLAG_INDEX and not got[1].any()
 
 
+@pytest.mark.parametrize("fresh", [[1, 3], [100, 20], [1]])
+def test_no_keys_and_no_pages(fresh):
+    # no keys at all: zeros; keys, but a cache without pages: zeros, flagged
+    c = make(fresh, [0] * len(fresh), 8, 2, 64, BF, 16, seed=77)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for max_kv in (0, 500):
+        assert not call(c, max_kv=max_kv, status=status).any() and int(status) == 0
+    empty = sss.empty_kv_cache_q4(0, 16, 2, 64)
+    c["kv"] = [max(fresh) + 5] * len(fresh)
+    c["table"] = torch.zeros((len(fresh), 20), dtype=torch.int32)
+    assert not call(c, cache=empty, status=status).any() and int(status) == sss.FLAG_INDEX
+
+
+@pytest.mark.parametrize("cu", [[0, 3, 2, 6], [0, 2, 9, 9], [-1, 2, 4, 6], [0, 6, 6, 6]])
+def test_tokens_that_cannot_be(cu):
+    # requests that point past the tokens or backwards are left out, the others are right
+    c = make([2, 2, 2], [20, 30, 40], 8, 2, 128, BF, 16, seed=78)
+    cache, want = cache_of(c), call(c, max_q=6)
+    c["cu"] = cu
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    got = call(c, cache=cache, max_q=6, status=status)
+    for b in range(3):
+        if cu[b] == 2 * b and cu[b + 1] == 2 * b + 2:
+            assert torch.equal(got[2 * b:2 * b + 2], want[2 * b:2 * b + 2])
+    assert int(status) == (0 if cu == [0, 6, 6, 6] else sss.FLAG_INDEX)
+
+
 @pytest.mark.parametrize("many", [False, True])
 def test_rows_of_no_request_are_left_alone(many):
     c = make([2, 3], [30, 70], 8 if many else 4, 1, 64, BF, 16, seed=72)

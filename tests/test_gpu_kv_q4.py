@@ -76,6 +76,10 @@ def test_no_slots_given_no_tokens_and_one_side():
     sss.sss_kv_store_q4(k.to(DEV), v.to(DEV), c)
     assert np.array_equal(c.blocks.cpu().numpy(), expect(k, v, list(range(20)), c))
     sss.sss_kv_store_q4(k[:0].to(DEV), v[:0].to(DEV), c, ints([]))
+    less, status = filled(1, 16, 3, 128), ints([0])  # more tokens than slots
+    sss.sss_kv_store_q4(k.to(DEV), v.to(DEV), less, dev_status=status)
+    assert int(status) == sss.FLAG_INDEX
+    assert np.array_equal(less.blocks.cpu().numpy(), expect(k[:16], v[:16], list(range(16)), less))
     only = torch.full((2, 3, 128), 9.0, device=DEV)
     a, b = sss.sss_kv_fetch_q4(c, ints([3, 19]), v=only)
     assert a is None and b is only
