@@ -164,7 +164,7 @@ __global__ void __launch_bounds__(kForkThreads) page_fork_kernel(const __grid_co
 //   one that moved away: rk(x) - (m - k), and the x - rk(x) - k free ones below it.
 // Bound by latency: a few waits of the cluster, and the table's entries, whose bits are set and
 // (with moves) looked up in shared memory.  16 requests, 4000 pages: 4.6 us; 256 requests of up
-// to 1024 entries, 51,000 pages, with moves: 16.0 us.
+// to 1024 entries, 51,000 pages, with moves: 13.6 us.
 // ---------------------------------------------------------------------------
 
 constexpr int kMapThreads = 1024;
@@ -213,7 +213,7 @@ __global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_c
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __syncthreads();
   // the rows' entries, a warp to a piece of them
-  constexpr int kWarps = kMapThreads / 32, kPiece = 128;
+  constexpr int kWarps = kMapThreads / 32, kPiece = 512;  // (128: 16.0 us, 13.6 so)
   const int pieces = (a.width + kPiece - 1) / kPiece;
   const int64_t items = static_cast<int64_t>(a.batch) * pieces;
   for (int64_t i = static_cast<int64_t>(me) * kWarps + warp; i < items; i += static_cast<int64_t>(ctas) * kWarps) {
