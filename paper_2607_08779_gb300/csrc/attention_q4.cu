@@ -46,28 +46,40 @@ void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int dim, in
   p.tiles = p.one_tile ? batch : std::min(tokens / p.tpt + batch,
                                           static_cast<int64_t>(batch) * ((max_q + int64_t{p.tpt} - 1) / p.tpt));
   const int64_t items = std::max<int64_t>(1, p.tiles * kv_heads * p.hchunks);
-  // A cluster of as many CTAs as leave them all at work at a time (three an SM), halved until
-  // all but one of them have the 128 keys that its warps take in a step: 4 above 384, 8 above
-  // 896, 16 above 1920 (one request of 500 keys: 4.3 us in fours, 4.8 in eights; of 8192: 8.4 in
-  // sixteens, 10.6 in eights).  More waves of CTAs cost 2 to 5 us each (64 requests of 300 to
-  // 500 keys and 8 key/value heads: 12.7 us whole, 20.4 in pairs; 32 of 256 to 2000: 21.0 us
-  // whole, 17.9 in pairs; 16 of 4000 to 8192: 39.9 in fours, 43.3 in eights), which long and
-  // so as a rule unlike requests are worth (64 of 1000 to 8192: 91 us whole, 81 in pairs, 85
-  // in fours; 16 of 130 to 16384: 43.7 in fours, 38.2 in eights).
+  // How many CTAs (a cluster of them) share a tile's keys, and of how many warps.  Few tiles: one
+  // CTA of 8 warps an SM, as many as that leaves room for (one request of 8192 keys and one
+  // key/value head: 6.2 us, 7.5 with 4 warps; 4 of 1400 to 4096 and 8 heads 8.4 and 9.6; 8 of 500 to
+  // 1500 7.1 and 8.4), but for 16 tiles of long requests, where more of 4 warps find room (2 of
+  // 2700 to 8192 and 8 heads: 10.7 us in sixteens, 12.6).  More tiles: CTAs of 4 warps, three
+  // an SM; more waves of them cost 2 to 5 us each (64 requests of 300 to 500 keys and 8
+  // heads: 12.5 us whole, 20.4 in pairs; 32 of 256 to 2000: 21.0 whole, 17.6 in pairs; 16 of 270 to
+  // 800: 8.4 in pairs, 10.8 in fours).  Each CTA but one has 128 keys (one request of 500:
+  // 4.2 us in fours, 4.7 in eights).
   constexpr int64_t kLeast = 128;
-  int64_t cluster = items <= 8 ? 16 : items <= 32 ? 8 : items <= sms ? 4 : items <= 2 * sms ? 2 : 1;
-  if (max_kv >= 4096) cluster = std::max<int64_t>(cluster, items <= sms && max_kv >= 12288 ? 8 : 2);
+  int64_t cluster;
+  p.warps = max_kv >= 1024 && items <= 64 ? 8 : 4;
+  if (p.warps == 8 && items > 8 && items <= 16 && max_kv >= 4096) {
+    p.warps = 4;
+    cluster = p.rows == 8 ? 16 : 8;
+  } else if (p.warps == 8) {
+    cluster = items <= 4 ? 16 : items <= 8 ? 8 : items <= 32 ? 4 : 2;
+  } else {
+    cluster = items <= 8 ? 16 : items <= 32 ? 8 : items <= sms ? (max_kv >= 2048 ? 4 : 2) : items <= 2 * sms ? 2 : 1;
+    if (max_kv >= 4096) cluster = std::max<int64_t>(cluster, 2);
+  }
   while (cluster > 1 && (cluster - 1) * kLeast >= max_kv) cluster /= 2;
   p.nsplit = cluster;
   // Long requests in chunks of 1024 to 2048 keys, about 256 CTAs of them or more, joined by a
   // second kernel (2.5 us): no cluster then waits for room on one part of the chip, and lengths
   // that differ even out (16 requests of 130 to 16384 keys and 64 heads: 37.5 us in clusters,
-  // 31.4 in chunks; 64 of 12000 to 16384: 209 and 190; one of 32768: 21.4 and 14.6; 20 of 400 to
+  // 30.9 in chunks; 64 of 12000 to 16384: 209 and 185; one of 32768: 21.4 and 14.4; 20 of 400 to
   // 3000: 19.4 and 25.7).  Where the keys take half the time (heads of 64) or tiles are fewer at
-  // a time (16 rows) from twice that length on.
+  // a time (16 rows) from twice that length on; with 8 warps from 12 steps of a warp on (4 of 2700
+  // to 8192, 8 steps: 12.7 us so, 14.6 in chunks).
   const int64_t chunk = std::min<int64_t>(2048, std::max<int64_t>(1024, (max_kv * items / 256 + 127) / 128 * 128));
   const int64_t least = chunk * (p.rows == 8 && dim == 128 ? 4 : 8);
-  if (max_kv >= least && max_kv * items >= 1024 * 256 && items <= 1024) {
+  const bool many = p.warps == 8 ? max_kv / (cluster * 256) >= 12 : max_kv * items >= 1024 * 256;
+  if (max_kv >= least && many && items <= 1024) {
     p.chunk = chunk;
     p.nsplit = (max_kv + chunk - 1) / chunk;
     p.join = true;
@@ -155,6 +167,7 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
   a.part = static_cast<float*>(workspace);
   a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.of.lse_at);
   a.rows = p.of.rows;
+  a.warps = p.of.warps;
   a.scale_log2 = scale * 1.4426950408889634f;
   a.stall = (test_stall_mask() & SSS_TEST_STALL_ATTENTION_ROWS) ? 1 : 0;
   const cudaError_t e = launch_attn_rows_q4(a, q4_cache(c), dtype, c.dim, stream);

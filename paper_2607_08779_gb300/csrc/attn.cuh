@@ -36,6 +36,7 @@ struct AttnArgs {
   int table_width, page_shift;
   int chunk, nsplit;
   int rows;         // of the row form's tiles: 16 or 32
+  int warps;        // of its CTAs, over 4 bits: 4 or 8
   int stall;        // test hook
   int box_rows;     // of an output box of the prompt form
   float scale_log2;  // scale * log2(e)

@@ -45,8 +45,6 @@
 namespace sss {
 namespace {
 
-constexpr int kWarps = 4;
-constexpr int kThreads = 32 * kWarps;
 // How a tile's keys are split over CTAs: not; over those of a cluster, in turn, which join them
 // there; or in chunks, whose results attn_join_kernel joins.
 enum Split { kWhole, kCluster, kChunks };
@@ -60,14 +58,14 @@ struct Ring {
   static constexpr int kStages = SPLIT == kChunks ? 2 : 3;  // steps
 };
 
-template <int D, int R, Split SPLIT>
+template <int D, int R, Split SPLIT, int WARPS>
 struct RowsQ4Smem {
   static constexpr int kBlocks = Ring<SPLIT>::kBlocks, kStages = Ring<SPLIT>::kStages;
   static constexpr bool CL = SPLIT == kCluster;
   static constexpr int STAGE = kBlocks * Q4Block<D>::kBytes;
   static constexpr int RING = kStages * STAGE;  // of a warp
   static constexpr int LD = D + 4;  // of the warps' outputs, which follow
-  static constexpr int RINGS = std::max(kWarps * RING, kWarps * R * LD * 4);
+  static constexpr int RINGS = WARPS * std::max(RING, R * LD * 4);
   // the splits' pieces of the values that this one joins (their number rounded up)
   static constexpr int TOTAL = RINGS + (CL ? (R * D / 4 + 16) * 16 : 0);
 };
@@ -149,12 +147,13 @@ __device__ __forceinline__ void peer_store(uint32_t addr, float4 v, uint32_t bar
 }
 
 // NT tiles of 8 rows (tokens x heads).
-template <typename T, int D, int NT, Split SPLIT>
-__global__ void __launch_bounds__(kThreads, (NT == 1 ? 3 : 2) + (D == 64 ? 1 : 0))
+template <typename T, int D, int NT, Split SPLIT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2) + (D == 64 ? 1 : 0))
     attn_rows_q4_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ Q4Cache c4) {
   constexpr int R = 8 * NT;
   constexpr bool CL = SPLIT == kCluster;
-  using S = RowsQ4Smem<D, R, SPLIT>;
+  constexpr int kWarps = WARPS, kThreads = 32 * WARPS;
+  using S = RowsQ4Smem<D, R, SPLIT, WARPS>;
   constexpr int kBlocks = S::kBlocks, kStages = S::kStages;
   constexpr int kStep = kBlocks * kQ4Slots;  // keys of a step
   constexpr int kAhead = 32 / kBlocks;       // steps whose blocks the lanes hold
@@ -224,8 +223,7 @@ __global__ void __launch_bounds__(kThreads, (NT == 1 ? 3 : 2) + (D == 64 ? 1 : 0
   const bool alone = SPLIT == kChunks ? lim1 <= a.chunk : n == 1;  // the tile has no other split
   if (CL && alone && z > 0) return leave();
   const int first = CL ? warp + kWarps * z : warp;
-  const int turn = CL ? 31 - __clz(kWarps * a.nsplit) : 2;  // (a cluster is a power of two)
-  static_assert(kWarps == 4, "turn");
+  const int turn = 31 - __clz(CL ? kWarps * a.nsplit : kWarps);  // (powers of two)
   const int mine = first < steps ? (steps - first - 1 >> turn) + 1 : 0;  // steps of the warp
   const int32_t* table = a.table + static_cast<int64_t>(b) * a.table_width;
   unsigned char* ring = smem + warp * S::RING;
@@ -727,11 +725,11 @@ __global__ void __launch_bounds__(kThreads, (NT == 1 ? 3 : 2) + (D == 64 ? 1 : 0
   }
 }
 
-template <typename T, int D, int NT, Split SPLIT>
+template <typename T, int D, int NT, Split SPLIT, int WARPS>
 cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
   constexpr bool CL = SPLIT == kCluster;
-  auto kern = attn_rows_q4_kernel<T, D, NT, SPLIT>;
-  constexpr int smem = RowsQ4Smem<D, 8 * NT, SPLIT>::TOTAL;
+  auto kern = attn_rows_q4_kernel<T, D, NT, SPLIT, WARPS>;
+  constexpr int smem = RowsQ4Smem<D, 8 * NT, SPLIT, WARPS>::TOTAL;
   cudaError_t e = ensure_smem(kern, smem);
   if (e != cudaSuccess) return e;
   if (CL && a.nsplit > 8) {
@@ -742,7 +740,7 @@ cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
   if (grid.y > 65535 || grid.z > 65535) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(32 * WARPS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
@@ -756,14 +754,15 @@ cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
   cfg.numAttrs = CL ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, a, c);
 }
-template <typename T, int D, Split SPLIT>
+template <typename T, int D, Split SPLIT, int WARPS = 4>
 cudaError_t tiles(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
-  return a.rows == 8 ? run<T, D, 1, SPLIT>(a, c, stream) : run<T, D, 2, SPLIT>(a, c, stream);
+  return a.rows == 8 ? run<T, D, 1, SPLIT, WARPS>(a, c, stream) : run<T, D, 2, SPLIT, WARPS>(a, c, stream);
 }
 template <typename T, int D>
 cudaError_t splits(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
   if (a.nsplit == 1) return tiles<T, D, kWhole>(a, c, stream);
-  return a.chunk > 0 ? tiles<T, D, kChunks>(a, c, stream) : tiles<T, D, kCluster>(a, c, stream);
+  if (a.chunk > 0) return tiles<T, D, kChunks>(a, c, stream);
+  return a.warps == 8 ? tiles<T, D, kCluster, 8>(a, c, stream) : tiles<T, D, kCluster>(a, c, stream);
 }
 
 }  // namespace

@@ -88,7 +88,8 @@ cudaError_t launch_qk_norm_rope(const void* q, int64_t q_stride, const void* k, 
 // How a call of sss_attention is laid out (from its sizes alone; see attn.cuh).
 struct AttnPlan {
   bool prompt;               // the form on tcgen05; else the row form
-  int rows;                  // of the row form's tiles: 16 or 32
+  int rows;                  // of the row form's tiles: 16 or 32 (over 4 bits 8 or 16)
+  int warps;                 // of its CTAs, over 4 bits: 4 or 8
   int hpt, hchunks, tpt;     // heads and tokens of a tile, tiles of a group of heads
   bool one_tile;             // a request is one tile
   int64_t tiles;             // an upper bound of the token tiles
