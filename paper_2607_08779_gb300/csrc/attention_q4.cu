@@ -8,7 +8,8 @@
 // The copy is fp16 for both types of q: fp16(s) c has 14 significant bits at most, of which fp16
 // keeps 11 and bf16 would keep 8 (error of the outputs, against 64 bits: 2.8e-3 to 3.4e-3 with a
 // bf16 copy, where their own rounding is 1.6e-3).  bf16 queries then go with it as fp16 numbers of
-// the same digits: each row gives off a power of two, which its scores' scale takes back.
+// the same digits: each row gives off a power of two, which its scores' scale takes back.  They are
+// staged by the launch that copies the keys.
 #include <algorithm>
 
 #include "attn.cuh"
@@ -125,14 +126,19 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
     const bool bf16 = dtype == SSS_OUT_BF16;
     const float times = bf16 ? 0.0625f : 1.f;
     float* const scales = reinterpret_cast<float*>(ws + p.scale_at);
-    const Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, times};
-    cudaError_t e = launch_kv_stage_q4(q4_cache(c), c.dim, s, stream);
-    if (e == cudaSuccess && bf16) {
-      e = launch_q_stage(q, q_stride, tokens, heads, c.dim, scale * 1.4426950408889634f, times,
-                         ws + p.q_at, scales, stream);
+    Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, times};
+    if (bf16) {
+      s.q = q;
+      s.q_stride = q_stride;
+      s.tokens = tokens;
+      s.q_heads = heads;
+      s.scale_log2 = scale * 1.4426950408889634f;
+      s.q_out = ws + p.q_at;
+      s.scales = scales;
       q = ws + p.q_at;
       q_stride = static_cast<int64_t>(heads) * c.dim;
     }
+    const cudaError_t e = launch_kv_stage_q4(q4_cache(c), c.dim, s, stream);
     if (e != cudaSuccess) return e;
     return launch_attention(p.of, q, q_stride, heads, staged(p, c, batch, ws), cu_q, kv_len,
                             to, p.pages, batch, tokens, max_q, max_kv, scale, out, ws, status, stream,

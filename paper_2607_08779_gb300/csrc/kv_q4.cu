@@ -34,7 +34,8 @@ struct StoreArgs {
   Q4Cache cache;
   uint32_t* status;
   int64_t tokens;
-  int run;  // heads that a warp takes
+  int run;   // heads that a warp takes
+  int runs;  // of them
 };
 
 // A lane's eight consecutive values, as they come.
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(kThreads) kv_store_q4_kernel(const __grid_cons
   const int lane = threadIdx.x & 31, l = lane % LANES;
   const int64_t first = (static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * TOKENS;
   const int64_t t = first + lane / LANES;
-  const int runs = gridDim.y / 2;
+  const int runs = a.runs;
   const bool is_v = blockIdx.y >= runs;
   const int h0 = (blockIdx.y - (is_v ? runs : 0)) * a.run, h1 = min(a.cache.heads, h0 + a.run);
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -243,7 +244,7 @@ struct FetchArgs {
   void *k, *v;
   uint32_t* status;
   int64_t rows;
-  int run;
+  int run, runs;
   Q4Stage stage;
 };
 
@@ -278,20 +279,67 @@ __device__ __forceinline__ void store8(T* p, float (&f)[8], bool in) {
   }
 }
 
+// Queries for the copy (see Q4Stage): a row of D values is D / 8 lanes.  CTA `cta` of `ctas`.
+template <int D>
+__device__ __forceinline__ void stage_queries(const Q4Stage& a, int64_t cta, int64_t ctas) {
+  constexpr int LANES = D / 8;
+  const int l = threadIdx.x % LANES, heads = a.q_heads;
+  const int64_t rows = a.tokens * heads;
+  for (int64_t r0 = cta * (kThreads / LANES); r0 < rows; r0 += ctas * (kThreads / LANES)) {
+    const int64_t row = r0 + threadIdx.x / LANES, t = row / heads;
+    const bool in = row < rows;
+    uint4 u = make_uint4(0u, 0u, 0u, 0u);
+    if (in)
+      u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + t * a.q_stride +
+                                               (row - t * heads) * D + 8 * l));
+    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+    float f[8], top = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f[2 * i] = __uint_as_float(w[i] << 16);
+      f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+      top = fmaxf(top, fmaxf(fabsf(f[2 * i]), fabsf(f[2 * i + 1])));
+    }
+#pragma unroll
+    for (int m = LANES / 2; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+    // (a row of infinities or NaN keeps them)
+    const int E = min(max(static_cast<int>(__float_as_uint(top) >> 23 & 255u) - 127, -112), 127);
+    const float up = __int_as_float((14 - E + 127) << 23);
+    __half2 h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i] * up, f[2 * i + 1] * up);
+    memcpy(&u, h, 16);
+    if (!in) continue;
+    *reinterpret_cast<uint4*>(static_cast<__half*>(a.q_out) + row * D + 8 * l) = u;
+    // (kept above zero and below infinity, for what is multiplied by an infinity or zero)
+    if (l == 0)
+      a.scales[row] = fminf(fmaxf(a.scale_log2 * __int_as_float((E - 14 + 127) << 23) / a.times, 1e-37f), 3e38f);
+  }
+}
+
 // As the store's grid, of rows.  STAGE: blockIdx.z is a request; row t of the copy is its key
-// t, in a page of its own.
-template <typename T, int D, bool STAGE>
+// t, in a page of its own.  QUERIES: the grid's rows behind the 2 * runs are the queries' (a variant
+// of its own, as the others take 1 us more with it).
+template <typename T, int D, bool STAGE, bool QUERIES>
 __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_constant__ FetchArgs a) {
   using B = Q4Block<D>;
   constexpr int LANES = D / 8, TOKENS = 32 / LANES;
   const int lane = threadIdx.x & 31, l = lane % LANES;
   const int64_t first = (static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5)) * TOKENS;
   const int64_t t = first + lane / LANES;
-  const int runs = gridDim.y / 2, shift = a.cache.shift;
+  const int runs = a.runs, shift = a.cache.shift;
   const bool is_v = blockIdx.y >= runs;
   const int h0 = (blockIdx.y - (is_v ? runs : 0)) * a.run, h1 = min(a.cache.heads, h0 + a.run);
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if constexpr (QUERIES) {
+    if (blockIdx.y >= 2 * runs) {
+      const int64_t layer = static_cast<int64_t>(gridDim.x) * gridDim.z;
+      stage_queries<D>(a.stage, (blockIdx.y - 2 * runs) * layer + static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x,
+                       (gridDim.y - 2 * runs) * layer);
+      return;
+    }
+  }
   if (first >= a.rows) return;
   bool in = t < a.rows;  // the row is written
   uint32_t flags = 0;
@@ -368,54 +416,8 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
   if (flags && a.status) atomicOr(a.status, flags);
 }
 
-// Queries for the copy: a row of D values is D / 8 lanes.
-struct QArgs {
-  const void* q;
-  void* out;
-  float* scales;
-  int64_t q_stride, tokens;
-  int heads;
-  float scale_log2, times;
-};
-template <int D>
-__global__ void __launch_bounds__(kThreads) q_stage_kernel(const __grid_constant__ QArgs a) {
-  constexpr int LANES = D / 8;
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x, row = at / LANES;
-  const int l = static_cast<int>(at % LANES);
-  const int64_t t = row / a.heads;
-  const bool in = t < a.tokens;
-  uint4 u = make_uint4(0u, 0u, 0u, 0u);
-  if (in)
-    u = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.q) + t * a.q_stride +
-                                             (row - t * a.heads) * D + 8 * l));
-  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-  float f[8], top = 0.f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    f[2 * i] = __uint_as_float(w[i] << 16);
-    f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    top = fmaxf(top, fmaxf(fabsf(f[2 * i]), fabsf(f[2 * i + 1])));
-  }
-#pragma unroll
-  for (int m = LANES / 2; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-  // (a row of infinities or NaN keeps them)
-  const int E = min(max(static_cast<int>(__float_as_uint(top) >> 23 & 255u) - 127, -112), 127);
-  const float up = __int_as_float((14 - E + 127) << 23);
-  __half2 h[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) h[i] = __floats2half2_rn(f[2 * i] * up, f[2 * i + 1] * up);
-  memcpy(&u, h, 16);
-  if (!in) return;
-  *reinterpret_cast<uint4*>(static_cast<__half*>(a.out) + row * D + 8 * l) = u;
-  // (kept above zero and below infinity, for what is multiplied by an infinity or zero)
-  if (l == 0)
-    a.scales[row] = fminf(fmaxf(a.scale_log2 * __int_as_float((E - 14 + 127) << 23) / a.times, 1e-37f), 3e38f);
-}
-
 template <typename K, typename A>
-cudaError_t launch(K kern, A& a, int64_t rows, int dim, int batch, cudaStream_t stream) {
+cudaError_t launch(K kern, A& a, int64_t rows, int dim, int batch, cudaStream_t stream, int64_t queries = 0) {
   // All heads to a warp, or where that gives an SM fewer than 16 warps as many runs of them as do.
   const int64_t all = int64_t{16} * device_sm_count(), tokens = kWarps * 256 / dim;  // of a CTA
   const int64_t warps = std::max<int64_t>(1, 2 * batch * ((rows + 256 / dim - 1) / (256 / dim)));
@@ -424,7 +426,13 @@ cudaError_t launch(K kern, A& a, int64_t rows, int dim, int batch, cudaStream_t 
   a.run = (heads + runs - 1) / runs;
   runs = (heads + a.run - 1) / a.run;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((rows + tokens - 1) / tokens), static_cast<unsigned>(2 * runs), static_cast<unsigned>(batch));
+  a.runs = runs;
+  // (the queries: as many more rows of the grid as give them eight CTAs an SM or all they need; in a
+  // launch of their own two prompts of 14 to 83 tokens, 12 heads, took 12.2 us, so 10.8; one of 4000, 32 heads, 123 and 120)
+  const unsigned ctas = static_cast<unsigned>((rows + tokens - 1) / tokens);
+  const int64_t of_queries = std::min<int64_t>((queries * (dim / 8) + kThreads - 1) / kThreads, 8 * device_sm_count());
+  const int64_t layer = std::max<int64_t>(1, static_cast<int64_t>(ctas) * batch);
+  cfg.gridDim = dim3(ctas, static_cast<unsigned>(2 * runs + (of_queries + layer - 1) / layer), static_cast<unsigned>(batch));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr[1];
@@ -440,10 +448,11 @@ cudaError_t store(StoreArgs& a, int dim, cudaStream_t stream) {
   return dim == 64 ? launch(kv_store_q4_kernel<T, 64>, a, a.tokens, dim, 1, stream)
                    : launch(kv_store_q4_kernel<T, 128>, a, a.tokens, dim, 1, stream);
 }
-template <typename T, bool STAGE>
+template <typename T, bool STAGE, bool QUERIES = false>
 cudaError_t fetch(FetchArgs& a, int dim, int batch, cudaStream_t stream) {
-  return dim == 64 ? launch(kv_fetch_q4_kernel<T, 64, STAGE>, a, a.rows, dim, batch, stream)
-                   : launch(kv_fetch_q4_kernel<T, 128, STAGE>, a, a.rows, dim, batch, stream);
+  const int64_t queries = QUERIES ? a.stage.tokens * a.stage.q_heads : 0;
+  return dim == 64 ? launch(kv_fetch_q4_kernel<T, 64, STAGE, QUERIES>, a, a.rows, dim, batch, stream, queries)
+                   : launch(kv_fetch_q4_kernel<T, 128, STAGE, QUERIES>, a, a.rows, dim, batch, stream, queries);
 }
 
 }  // namespace
@@ -462,7 +471,7 @@ cudaError_t launch_kv_store_q4(const void* k, int64_t k_stride, const void* v, i
 cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* slots, int64_t count,
                                void* k, void* v, int out_dtype, uint32_t* status,
                                cudaStream_t stream) {
-  FetchArgs a = {q4_cache(cache), slots, k, v, status, count, 1, {}};
+  FetchArgs a = {q4_cache(cache), slots, k, v, status, count, 1, 1, {}};
   switch (out_dtype) {
     case SSS_OUT_F16: return fetch<__half, false>(a, cache.dim, 1, stream);
     case SSS_OUT_BF16: return fetch<__nv_bfloat16, false>(a, cache.dim, 1, stream);
@@ -471,27 +480,8 @@ cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* sl
 }
 
 cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, const Q4Stage& s, cudaStream_t stream) {
-  FetchArgs a = {c, nullptr, s.k, s.v, nullptr, static_cast<int64_t>(s.pages) << c.shift, 1, s};
-  return fetch<__half, true>(a, dim, s.batch, stream);
-}
-
-cudaError_t launch_q_stage(const void* q, int64_t q_stride, int64_t tokens, int heads, int dim,
-                           float scale_log2, float times, void* out, float* scales,
-                           cudaStream_t stream) {
-  const QArgs a = {q, out, scales, q_stride, tokens, heads, scale_log2, times};
-  const int64_t blocks = (tokens * heads * (dim / 8) + kThreads - 1) / kThreads;
-  if (blocks > INT32_MAX) return cudaErrorNotSupported;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return dim == 64 ? cudaLaunchKernelEx(&cfg, q_stage_kernel<64>, a)
-                   : cudaLaunchKernelEx(&cfg, q_stage_kernel<128>, a);
+  FetchArgs a = {c, nullptr, s.k, s.v, nullptr, static_cast<int64_t>(s.pages) << c.shift, 1, 1, s};
+  return s.q ? fetch<__half, true, true>(a, dim, s.batch, stream) : fetch<__half, true>(a, dim, s.batch, stream);
 }
 
 }  // namespace sss

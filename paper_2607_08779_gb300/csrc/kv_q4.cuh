@@ -79,14 +79,17 @@ struct Q4Stage {
   int32_t* new_table; // [batch][pages]
   void *k, *v;        // [batch * pages * page_size][heads][dim] fp16
   float times;        // of the values: 1 or 1/16
+  // bf16 queries (else null) as fp16 ones, dense, each row (token, head) with a power of two of
+  // its own taken off so that its largest value is between 2^14 and 2^15; and `scale_log2`
+  // times that over `times` for each row.
+  const void* q;
+  int64_t q_stride, tokens;
+  int q_heads;
+  float scale_log2;
+  void* q_out;        // [tokens][q_heads][dim]
+  float* scales;      // [tokens][q_heads]
 };
 cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, const Q4Stage& s, cudaStream_t stream);
-
-// bf16 queries as fp16 ones, each row (token, head) with a power of two of its own taken off so that its
-// largest value is between 2^14 and 2^15, and `scale_log2` times that and `times` to scales.
-cudaError_t launch_q_stage(const void* q, int64_t q_stride, int64_t tokens, int heads, int dim,
-                           float scale_log2, float times, void* out, float* scales,
-                           cudaStream_t stream);
 
 // Attention of few rows over the cache.
 struct AttnArgs;

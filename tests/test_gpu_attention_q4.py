@@ -158,6 +158,15 @@ def test_more_requests_than_sms(n, most, hq, hkv, dim, dtype):
     check(c, call(c))
 
 
+@pytest.mark.parametrize("fresh,kv,hq,hkv,dim", [
+    ([700], [700], 56, 2, 64), ([13] * 41, [13 + i % 5 for i in range(41)], 32, 2, 128),
+    ([70, 0, 1], [71, 500, 1], 48, 1, 128), ([3001], [3001], 5, 1, 64),
+])
+def test_more_rows_of_queries_than_of_keys(fresh, kv, hq, hkv, dim):
+    c = make(fresh, kv, hq, hkv, dim, BF, 16, seed=53)
+    check(c, call(c))
+
+
 def test_pages_past_four_gigabytes():
     # a cache whose bytes are past 2^32, and a request whose pages lie at both of its ends;
     # one of them is copied to the far end first
