@@ -657,9 +657,13 @@ size_t sss_attention_q4_workspace_bytes(int64_t tokens, int32_t heads,
  * sss_page_fork -- the rows of a new block table from those of the old one: beams or
  * samples that go on from their parents.  Row r takes over the pages of past[p] tokens of
  * p = parents[r].  Full pages are shared.  A last page that is only partly filled is
- * written to by the tokens that follow: the first row with that parent keeps it, each
- * other one gets a free page in its place (from the front of free_pages, rows in order)
- * and the entry (src[r], dst[r]) for sss_page_copy.  Pages of rows that nobody takes over are
+ * written to by the tokens that follow, so one row alone may hold it: the first of the new rows
+ * that end in it keeps it, unless a new row holds it as a full page; each other one gets a free
+ * page in its place (from the front of free_pages, rows in order) and the entry (src[r],
+ * dst[r]) for sss_page_copy.  So a length may be cut into a page that other rows share (a request
+ * that is rolled back, drafted tokens that are rejected): fork the rows before they get new
+ * tokens, each from itself (parents 0, 1, 2 ...) if nothing else changes.  sss_page_plan alone
+ * would have them write to the shared page.  Pages of rows that nobody takes over are
  * found by sss_page_reclaim on the new table.
  *   parents      [in]  device int32 [rows]; negative: the row is empty.
  *   past         [in]  device int32 [batch].

@@ -3,7 +3,9 @@
 //
 // Nothing keeps counts of a page's holders: the table says who holds what.  Forking reads
 // rows and writes rows; the free pages are those that no row names.  So a request ends, a
-// beam is dropped or a length cut by changing the table's rows and lengths alone.
+// beam is dropped or a length cut by changing the table's rows and lengths alone.  (A row that
+// was cut into a page which others hold goes through a fork, of itself if need be, before it
+// gets new tokens: that is where pages are given their writers.)
 #include <algorithm>
 
 #include "kv_q4.cuh"
@@ -13,25 +15,36 @@ namespace {
 
 // ---------------------------------------------------------------------------
 // Fork.  Row r takes the pages of past[p] tokens of its parent p: all shared, but a last
-// one that is partly filled, which only the first row of each parent keeps.  The free
-// pages that the others take are numbered by an exclusive sum over the rows.
+// one that is partly filled, which one row alone may hold: the first of those that end in
+// it, unless a row holds all of it (a length may have been cut into a page that other
+// rows share, so it is the page that counts and not the parent).  The free pages that the others
+// take are numbered by an exclusive sum over the rows.
 //
 // Bound by latency where rows are few, by the tables' bytes where they are long (each
-// row's entries read once and written once).  As in page_plan.cu one launch without a
-// grid-wide wait: every CTA looks through all rows by itself, kForkThreads at a time, and
-// writes its share of the table.  Whether a parent was met in earlier chunks is a bit in
-// shared memory; within the chunk the warps look in turn, so that a row finds those before it.
-// 16 rows of 128 entries: 2.6 us; 512 of 2049: 5.9 us.
+// parent's entries are looked at, each row's read and written).  One launch.  Its first cluster
+// says who ends in what: each of its CTAs puts the rows' last pages in a hash table of its own, with the
+// first row of each, and looks up its share of the parents' full pages in it; what it finds is a bit
+// for that first row in every CTA.  The first CTA then numbers the rows.  The other CTAs write the new
+// table meanwhile, all of it but those last pages' entries, which the first CTA writes.
+// 16 rows of 128 entries: 3.9 us; 64 of 513 from 64 parents 5.2; 512 of 2049 7.6; 1024 of 257 from 256
+// parents 7.1.  Looking at an entry costs a dozen instructions and a read of shared memory at a place of
+// its own: 49,000 of them take one SM 8 us.
 // ---------------------------------------------------------------------------
 
-constexpr int kForkThreads = 256;
-constexpr int kMaxParents = 65536;  // bits in shared memory
+constexpr int kForkThreads = 1024;     // 256 where rows and tables are small
+constexpr int kForkCtas = 16;          // of the first cluster
+constexpr int kForkPiece = 256;        // entries that a warp takes at a time
+constexpr int kMaxRows = 65536;
+constexpr int kForkChunk = 8192;       // rows whose pages are in the hash table at a time
+constexpr int32_t kNoKey = INT32_MIN;  // (of it: free)
 
 struct ForkArgs {
   const int32_t *parents, *past, *free_pages, *table;
   int32_t *new_table, *new_past, *src, *dst, *used;
   uint32_t* status;
   int rows, batch, nfree, width, shift;
+  int slots;    // of the hash table, a power of two
+  int cluster;  // CTAs of the first cluster
 };
 
 __device__ __forceinline__ int warp_sum_to(int v, int lane) {
@@ -42,114 +55,245 @@ __device__ __forceinline__ int warp_sum_to(int v, int lane) {
   }
   return v;
 }
+__device__ __forceinline__ void cluster_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t of_rank(const uint32_t* p, int rank) {
+  uint32_t addr = static_cast<uint32_t>(__cvta_generic_to_shared(p));
+  asm("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(addr) : "r"(rank));
+  return addr;
+}
 
-__global__ void __launch_bounds__(kForkThreads) page_fork_kernel(const __grid_constant__ ForkArgs a) {
-  constexpr int kWarps = kForkThreads / 32;
-  __shared__ uint32_t met[kMaxParents / 32];
-  __shared__ int parent_of[kForkThreads];
-  __shared__ int held_of[kForkThreads];   // entries of the row
-  __shared__ int last_of[kForkThreads];   // its last one where that is a page of its own, or -1
-  __shared__ int warp_takes[kWarps];
+// row r's parent and its tokens, whatever the call holds; -1 and 0 of an empty row
+__device__ __forceinline__ int parent_of_row(const ForkArgs& a, int r, int64_t& past, uint32_t& flags) {
+  past = 0;
+  int parent = a.parents[r];
+  if (parent >= a.batch) {
+    flags |= SSS_FLAG_INDEX;
+    parent = -1;
+  }
+  if (parent < 0) return -1;
+  past = a.past[parent];
+  const int64_t most = static_cast<int64_t>(a.width) << a.shift;
+  if (past < 0 || past > most) {
+    flags |= SSS_FLAG_INDEX;
+    past = past < 0 ? 0 : most;
+  }
+  return parent;
+}
+// what a row ends in: its last page where that is partly filled (an entry that is none: another
+// negative number for each parent), or kNoKey
+__device__ __forceinline__ int32_t last_page(const ForkArgs& a, int parent, int64_t past) {
+  if (parent < 0 || (past & ((1 << a.shift) - 1)) == 0) return kNoKey;
+  const int32_t page = a.table[static_cast<int64_t>(parent) * a.width + (past >> a.shift)];
+  return page >= 0 ? page : -2 - parent;
+}
+// where a key is looked for first in the hash table; its slot there, from that one on, `add`: it is
+// put there, else -1 where it is not
+__device__ __forceinline__ int first_slot(int slots, int32_t key) {
+  const uint32_t h = static_cast<uint32_t>(key) * 2654435761u;
+  return static_cast<int>((h ^ h >> 15) & (slots - 1));
+}
+__device__ __forceinline__ int slot_of(int32_t* keys, int slots, int32_t key, int h, bool add) {
+  for (int i = 0; i < slots; ++i) {  // (at most half of them are taken)
+    const int at = (h + i) & (slots - 1);
+    const int32_t old = add ? atomicCAS(&keys[at], kNoKey, key) : keys[at];
+    if (old == key) return at;
+    if (old == kNoKey) return add ? at : -1;
+  }
+  return -1;
+}
+// The new table but for the entries of partly filled last pages: CTA `cta` of `ctas`.
+__device__ __forceinline__ void write_rows(const ForkArgs& a, int cta, int ctas) {
+  const int lane = threadIdx.x & 31, warps = blockDim.x / 32;
+  const uint32_t pieces = (a.width + int64_t{kForkPiece} - 1) / kForkPiece;
+  const uint32_t items = static_cast<uint32_t>(a.rows) * pieces;  // (2^32 are more than fit in memory)
+  for (uint32_t i = cta * warps + (threadIdx.x >> 5); i < items; i += ctas * warps) {
+    const int r = static_cast<int>(i / pieces), c0 = static_cast<int>(i - r * pieces) * kForkPiece;
+    int64_t past;
+    uint32_t said = 0;
+    const int parent = parent_of_row(a, r, past, said);
+    const int whole = static_cast<int>(past >> a.shift);
+    const int open = (past & ((1 << a.shift) - 1)) != 0 ? whole : -1;
+    const int32_t* in = a.table + static_cast<int64_t>(max(parent, 0)) * a.width;
+    int32_t* out = a.new_table + static_cast<int64_t>(r) * a.width;
+    int32_t v[kForkPiece / 32];
+#pragma unroll
+    for (int k = 0; k < kForkPiece / 32; ++k) {
+      const int c = c0 + 32 * k + lane;
+      v[k] = c < whole ? __ldg(in + c) : -1;
+    }
+#pragma unroll
+    for (int k = 0; k < kForkPiece / 32; ++k) {
+      const int c = c0 + 32 * k + lane;
+      if (c < a.width && c != open) out[c] = v[k];
+    }
+  }
+}
+
+__global__ void __launch_bounds__(kForkThreads, 1) page_fork_kernel(const __grid_constant__ ForkArgs a) {
+  extern __shared__ __align__(16) int32_t hashed[];  // the hash table: keys, then first rows
+  __shared__ uint32_t met[kMaxRows / 32];    // parents of a row
+  __shared__ uint32_t full[kMaxRows / 32];   // first rows whose page some row holds all of
+  __shared__ uint32_t keeps[kMaxRows / 32];  // rows that keep their last page
+  __shared__ int warp_takes[kForkThreads / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int P = 1 << a.shift;
-  const bool writer = blockIdx.x == 0;
+  const int threads = blockDim.x, warps = threads / 32;
+  const int ctas = a.cluster, me = blockIdx.x;
+  const bool looks = me < ctas;  // a CTA of the first cluster
+  int32_t *keys = hashed, *firsts = hashed + a.slots;
   uint32_t flags = 0;
-  int taken = 0;
-  for (int i = tid; i < (a.batch + 31) / 32; i += kForkThreads) met[i] = 0;
+  if (looks) {
+    for (int i = tid; i < (a.batch + 31) / 32; i += threads) met[i] = 0;
+    for (int i = tid; i < (a.rows + 31) / 32; i += threads) full[i] = keeps[i] = 0;
+    for (int i = tid; i < a.slots; i += threads) {
+      keys[i] = kNoKey;
+      firsts[i] = INT32_MAX;
+    }
+    if (ctas > 1) cluster_meet();  // (before a peer's first bit)
+    else __syncthreads();
+  }
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  for (int r0 = 0; r0 < a.rows; r0 += kForkThreads) {
-    const int r = r0 + tid;
-    int parent = -1;
-    int64_t past = 0;
-    if (r < a.rows) {
-      parent = a.parents[r];
-      if (parent >= a.batch) {
-        flags |= SSS_FLAG_INDEX;
-        parent = -1;
-      }
-      if (parent >= 0) {
-        past = a.past[parent];
-        const int64_t most = static_cast<int64_t>(a.width) << a.shift;
-        if (past < 0 || past > most) {
-          flags |= SSS_FLAG_INDEX;
-          past = past < 0 ? 0 : most;
-        }
-      }
+  if (!looks) {
+    write_rows(a, me - ctas, gridDim.x - ctas);
+    return;
+  }
+  // a row's parent, tokens and last page; a thread looks once where it has one row
+  const bool one = a.rows <= threads;
+  int parent = -1;
+  int64_t past = 0;
+  int32_t key = kNoKey;
+  const auto look = [&](int r) {
+    parent = parent_of_row(a, r, past, flags);
+    key = last_page(a, parent, past);
+  };
+  // the parents' full pages, a warp to a piece of them, the next one's entries under way
+  const uint32_t pieces = (a.width + int64_t{kForkPiece} - 1) / kForkPiece;
+  const uint32_t items = static_cast<uint32_t>(a.batch) * pieces;
+  struct Piece {
+    int b, c0, past;
+    int32_t v[kForkPiece / 32];
+  };
+  const auto load = [&](Piece& p, uint32_t i) {
+    if (i >= items) return;
+    p.b = static_cast<int>(i / pieces);
+    p.c0 = static_cast<int>(i - p.b * pieces) * kForkPiece;
+    p.past = a.past[p.b];
+    const int32_t* row = a.table + static_cast<int64_t>(p.b) * a.width;
+#pragma unroll
+    for (int k = 0; k < kForkPiece / 32; ++k) {
+      const int c = p.c0 + 32 * k + lane;
+      p.v[k] = c < a.width ? row[c] : -1;
     }
-    __syncthreads();  // (the chunk before is read)
-    parent_of[tid] = parent;
-    // is this the parent's first row?
-    bool first = (__match_any_sync(0xffffffffu, parent) & ((1u << lane) - 1)) == 0;
-    for (int w = 0; w < kWarps && r0 + 32 * w < a.rows; ++w) {
-      if (w == warp && parent >= 0) {
-        first = first && (met[parent >> 5] >> (parent & 31) & 1u) == 0;
-        if (first) atomicOr(&met[parent >> 5], 1u << (parent & 31));
-      }
+  };
+  const uint32_t item0 = me * warps + warp;
+  for (int chunk = 0; chunk < a.rows; chunk += kForkChunk) {
+    const int end = min(a.rows, chunk + kForkChunk);
+    Piece p, next;
+    load(next, item0);
+    // the chunk's rows into the table; then the others, for what of it they end in too
+    for (int r = chunk + tid; r < end; r += threads) {
+      look(r);
+      if (parent >= 0) atomicOr(&met[parent >> 5], 1u << (parent & 31));
+      if (key != kNoKey) atomicMin(&firsts[slot_of(keys, a.slots, key, first_slot(a.slots, key), true)], r);
+    }
+    if (a.rows > kForkChunk) {
       __syncthreads();
-    }
-    const bool open = (past & (P - 1)) != 0;  // the last page is partly filled
-    bool take = parent >= 0 && open && !first;
-    int from = -1;
-    if (take) {
-      from = a.table[static_cast<int64_t>(parent) * a.width + (past >> a.shift)];
-      if (from < 0) {  // nothing to copy
-        flags |= SSS_FLAG_INDEX;
-        take = false;
-        past &= ~static_cast<int64_t>(P - 1);
+      for (int r = tid; r < a.rows; r += threads) {
+        if (r >= chunk && r < end) continue;
+        look(r);
+        if (parent >= 0) atomicOr(&met[parent >> 5], 1u << (parent & 31));
+        const int at = key == kNoKey ? -1 : slot_of(keys, a.slots, key, first_slot(a.slots, key), false);
+        if (at >= 0) atomicMin(&firsts[at], r);
       }
+    }
+    __syncthreads();
+    for (uint32_t i = item0; i < items; i += ctas * warps) {
+      p = next;
+      load(next, i + ctas * warps);
+      if (!(met[p.b >> 5] >> (p.b & 31) & 1u)) continue;
+      const int left = (max(0, p.past) >> a.shift) - p.c0 - lane;  // full pages from the lane's first on
+      uint32_t hit = 0;  // entries whose first slot is not free (few: most slots are)
+#pragma unroll
+      for (int k = 0; k < kForkPiece / 32; ++k)
+        if (keys[first_slot(a.slots, p.v[k])] != kNoKey && p.v[k] >= 0 && 32 * k < left) hit |= 1u << k;
+#pragma unroll
+      for (int k = 0; k < kForkPiece / 32; ++k) {
+        if (!(hit >> k & 1u)) continue;
+        const int at = slot_of(keys, a.slots, p.v[k], first_slot(a.slots, p.v[k]), false);
+        if (at < 0) continue;
+        const int first = firsts[at];
+        if (ctas == 1) {
+          atomicOr(&full[first >> 5], 1u << (first & 31));
+          continue;
+        }
+        for (int c = 0; c < ctas; ++c)
+          asm volatile("red.relaxed.cluster.shared::cluster.or.b32 [%0], %1;" ::"r"(of_rank(&full[first >> 5], c)),
+                       "r"(1u << (first & 31))
+                       : "memory");
+      }
+    }
+    if (ctas > 1) cluster_meet();
+    else __syncthreads();
+    if (me == 0) {
+      for (int r = chunk + tid; r < end; r += threads) {
+        if (!one) look(r);
+        if (key == kNoKey || firsts[slot_of(keys, a.slots, key, first_slot(a.slots, key), false)] != r) continue;
+        if (!(full[r >> 5] >> (r & 31) & 1u)) atomicOr(&keeps[r >> 5], 1u << (r & 31));
+      }
+    }
+    __syncthreads();
+    if (end == a.rows) break;
+    for (int i = tid; i < a.slots; i += threads) {
+      keys[i] = kNoKey;
+      firsts[i] = INT32_MAX;
+    }
+    __syncthreads();
+  }
+  if (me > 0) return;
+  // the rows in order: which pages they end with
+  int taken = 0;
+  for (int r0 = 0; r0 < a.rows; r0 += threads) {
+    const int r = r0 + tid;
+    bool take = false;
+    if (r < a.rows) {
+      if (!one) look(r);
+      take = key != kNoKey && !(keeps[r >> 5] >> (r & 31) & 1u);
+    }
+    const bool none = take && key < 0;  // nothing to copy
+    if (none) {
+      flags |= SSS_FLAG_INDEX;
+      take = false;
     }
     const int upto = warp_sum_to(take ? 1 : 0, lane);
     if (lane == 31) warp_takes[warp] = upto;
     __syncthreads();
-    int at = taken + upto - 1;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      at += w < warp ? warp_takes[w] : 0;
-      taken += warp_takes[w];
-    }
-    int to = -1;
-    if (take) {
-      to = at < a.nfree ? a.free_pages[at] : -1;
-      if (to < 0) {
-        flags |= SSS_FLAG_PAGES;
-        from = -1;
-        past &= ~static_cast<int64_t>(P - 1);
+    const int takes = lane < warps ? warp_takes[lane] : 0;
+    const int sums = warp_sum_to(takes, lane);
+    const int at = taken + __shfl_sync(0xffffffffu, sums - takes, warp) + upto - 1;
+    taken += __shfl_sync(0xffffffffu, sums, 31);
+    if (r < a.rows) {
+      int from = -1, to = -1, held = static_cast<int>(past);
+      const int whole = held >> a.shift;
+      int32_t* last = a.new_table + static_cast<int64_t>(r) * a.width + whole;
+      if (take) {
+        to = at < a.nfree ? a.free_pages[at] : -1;
+        if (to >= 0) from = key;
+        else flags |= SSS_FLAG_PAGES;
+        to = max(to, -1);
       }
-    }
-    held_of[tid] = static_cast<int>((past + P - 1) >> a.shift);
-    last_of[tid] = to;
-    if (writer && r < a.rows) {
-      a.new_past[r] = static_cast<int32_t>(past);
+      if (none || (take && to < 0)) held = whole << a.shift;  // it ends with its last full page
+      if (key != kNoKey) *last = take || none ? to : key >= 0 ? key : a.table[static_cast<int64_t>(parent) * a.width + whole];
+      a.new_past[r] = held;
       a.src[r] = from;
       a.dst[r] = to;
     }
     __syncthreads();
-    // the chunk's rows, a warp to a piece of 256 entries
-    const int rows = min(kForkThreads, a.rows - r0), pieces = (a.width + 255) / 256;
-    const int64_t items = static_cast<int64_t>(rows) * pieces;
-    for (int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + warp; i < items;
-         i += static_cast<int64_t>(gridDim.x) * kWarps) {
-      const int row = static_cast<int>(i / pieces), c0 = static_cast<int>(i - static_cast<int64_t>(row) * pieces) * 256;
-      const int p = parent_of[row], held = held_of[row], last = last_of[row];
-      const int32_t* in = a.table + static_cast<int64_t>(max(p, 0)) * a.width;
-      int32_t* out = a.new_table + static_cast<int64_t>(r0 + row) * a.width;
-      int32_t v[8];
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int c = c0 + 32 * k + lane;
-        v[k] = c < held ? __ldg(in + c) : -1;
-        if (c == held - 1 && last >= 0) v[k] = last;
-      }
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int c = c0 + 32 * k + lane;
-        if (c < a.width) out[c] = v[k];
-      }
-    }
   }
-  if (writer && tid == 0) *a.used = min(taken, a.nfree);
-  if (flags && a.status && writer) atomicOr(a.status, flags);
+  if (tid == 0) *a.used = min(taken, a.nfree);
+  if (flags && a.status) atomicOr(a.status, flags);
 }
 
 // ---------------------------------------------------------------------------
@@ -178,14 +322,9 @@ struct MapArgs {
   int batch, width, shift, pages, most;
 };
 
-__device__ __forceinline__ void cluster_meet() {
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
 __device__ __forceinline__ uint32_t peer_word(const uint32_t* p, int rank) {
-  uint32_t addr = static_cast<uint32_t>(__cvta_generic_to_shared(p)), v;
-  asm("mapa.shared::cluster.u32 %0, %0, %1;" : "+r"(addr) : "r"(rank));
-  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  uint32_t v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(of_rank(p, rank)) : "memory");
   return v;
 }
 // the entries of row b that hold pages
@@ -436,11 +575,27 @@ cudaError_t launch_page_fork(const int32_t* parents, int rows, const int32_t* pa
                              const int32_t* table, int width, int32_t* new_table,
                              int32_t* new_past, int32_t* src, int32_t* dst, int32_t* used,
                              uint32_t* status, cudaStream_t stream) {
-  const ForkArgs a = {parents, past, free_pages, table, new_table, new_past, src, dst, used,
-                      status, rows, batch, nfree, width, shift_of(page_size)};
-  const int64_t items = static_cast<int64_t>(std::min(rows, kForkThreads)) * ((width + 255) / 256);
-  const int64_t ctas = std::max<int64_t>(1, std::min<int64_t>((items + 7) / 8, 2 * device_sm_count()));
-  return launch(page_fork_kernel, a, ctas, kForkThreads, 0, 1, stream);
+  ForkArgs a = {parents, past, free_pages, table, new_table, new_past, src, dst, used,
+                status, rows, batch, nfree, width, shift_of(page_size), 64, 1};
+  while (a.slots < 2 * kForkChunk && a.slots < 8 * rows) a.slots *= 2;
+  cudaError_t e = ensure_smem(page_fork_kernel, 2 * kForkChunk * 8);
+  if (e != cudaSuccess) return e;
+  const int64_t pieces = (width + int64_t{kForkPiece} - 1) / kForkPiece;
+  const int64_t parts = batch * pieces, items = rows * pieces;
+  // A thread to a row, and CTAs until a warp has one piece to look at (64 rows of 513 from 64 parents, 8
+  // CTAs of 512 threads: 5.2 us, 16 of 256 5.9, 8 of 1024 6.0, two pieces a warp 6.2; 1024 of 257 from 256
+  // parents, 8 of 1024 threads 7.0, 16 of 512 10.5, two pieces a warp 8.6; 4 of 20 from one, 256 threads 3.1,
+  // 512 3.3, 1024 3.6).
+  const int threads = rows <= 256 && parts <= 8 ? 256 : rows <= 512 ? 512 : kForkThreads, warps = threads / 32;
+  while (a.cluster < kForkCtas && parts > int64_t{a.cluster} * warps) a.cluster *= 2;
+  if (a.cluster > 8) {
+    e = ensure_large_cluster(page_fork_kernel);
+    if (e != cudaSuccess) return e;
+  }
+  // (CTAs that write: about one an SM, in whole clusters)
+  const int64_t writers = std::min<int64_t>((items + warps - 1) / warps, device_sm_count());
+  const int64_t ctas = (1 + (writers + a.cluster - 1) / a.cluster) * a.cluster;
+  return launch(page_fork_kernel, a, ctas, threads, a.slots * 8, a.cluster, stream);
 }
 
 cudaError_t launch_page_reclaim(const int32_t* table, int width, const int32_t* past, int batch,

@@ -1168,7 +1168,8 @@ def sss_page_fork(parents, past, page_size: int, free_pages, block_table, new_ta
                   dst, used, dev_status=None, stream=None) -> None:
     """Rows of a block table from their parents': int32 parents [rows], past [batch], the
     block table [batch, width] and free_pages to new_table [rows, width], new_past, src
-    and dst [rows] (for sss_page_copy) and used [1]."""
+    and dst [rows] (for sss_page_copy) and used [1].  A partly filled last page has one holder
+    then, also where lengths were cut into pages that rows share."""
     fn = "sss_page_fork"
     if stream is None:
         st = (_fast or _binding()).page_fork(parents, past, page_size, free_pages, block_table,
