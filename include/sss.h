@@ -76,7 +76,8 @@ typedef enum {
                                    (codes then 0).  sss_gemv at batch 2..16 and
                                    sss_gemm: a group's fp16 weight operand may overflow
                                    (see those calls); their outputs may then hold
-                                   inf or NaN.  sss_kv_store_q4: see there             */
+                                   inf or NaN.  sss_kv_store_q4, sss_attention_q4: see
+                                   there                                               */
 #define SSS_FLAG_TIMEOUT 0x4u   /* a bounded pipeline wait of sss_gemm (or
                                    sss_gemm_noalloc), sss_quantize,
                                    sss_quantize_rotated, sss_attention or
@@ -634,7 +635,8 @@ sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slot
  * fp16 (for bf16 p_ij is rounded first; at most 2^-25 off where it is below fp16's normal
  * range; a row's largest p_ij is 1).  More: the keys and values are first written to the
  * workspace as fp16 values, fp16(s) c rounded once (for bf16 a 16th of it, and q as fp16
- * with a power of two taken off each row), and p_ij is rounded to fp16.
+ * with a power of two taken off each row), and p_ij is rounded to fp16.  With fp16 queries a
+ * key or value above 65504 in size counts as 65504 there: SSS_FLAG_RANGE.
  * Errors: as sss_attention; SSS_E_UNSUPPORTED also where that copy of the cache would have
  * 2^31 slots or more.
  */

@@ -126,7 +126,7 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
     const bool bf16 = dtype == SSS_OUT_BF16;
     const float times = bf16 ? 0.0625f : 1.f;
     float* const scales = reinterpret_cast<float*>(ws + p.scale_at);
-    Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, times};
+    Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, status, times};
     if (bf16) {
       s.q = q;
       s.q_stride = q_stride;

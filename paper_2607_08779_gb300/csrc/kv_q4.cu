@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
     const int32_t page = __ldg(s.table + static_cast<int64_t>(b) * s.table_width + p);
     const bool real = page >= 0 && page < a.cache.slots >> shift;
     // the copy's table, of the pages that are real (what is none, and keys past the
-    // request's, are the attention's to flag)
+    // request's, are the attention's to flag; what fp16 does not hold is flagged here)
     if (blockIdx.y == 0 && lane == 0 && (first & ((1 << shift) - 1)) == 0)
       s.new_table[static_cast<int64_t>(b) * s.pages + p] = real ? b * s.pages + static_cast<int32_t>(p) : -1;
     const int64_t keys = min(static_cast<int64_t>(s.kv_len[b]), s.max_kv);
@@ -408,6 +408,16 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
         for (int e = 0; e < 8; ++e)
           f[e] = __fmaf_rn(__uint_as_float((part[e / 3] & (15u << (4 * (e % 3 + 2)))) | 0x4B000000u),
                            by[e % 3], less[e % 3]);
+        if constexpr (STAGE) {  // (a scale of 8188 or less keeps the copy in fp16's range)
+          if ((s16[u] & 0x7fffu) > 0x6FFFu && (s16[u] & 0x7fffu) < 0x7C00u) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              if (fabsf(f[e]) <= 65504.f) continue;
+              f[e] = copysignf(65504.f, f[e]);
+              flags |= SSS_FLAG_RANGE;
+            }
+          }
+        }
         store8(out, f, in);
         out += D;
       }
@@ -480,7 +490,7 @@ cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* sl
 }
 
 cudaError_t launch_kv_stage_q4(const Q4Cache& c, int dim, const Q4Stage& s, cudaStream_t stream) {
-  FetchArgs a = {c, nullptr, s.k, s.v, nullptr, static_cast<int64_t>(s.pages) << c.shift, 1, 1, s};
+  FetchArgs a = {c, nullptr, s.k, s.v, s.status, static_cast<int64_t>(s.pages) << c.shift, 1, 1, s};
   return s.q ? fetch<__half, true, true>(a, dim, s.batch, stream) : fetch<__half, true>(a, dim, s.batch, stream);
 }
 
