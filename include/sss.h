@@ -634,9 +634,9 @@ sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slot
  * sums of q times the codes, scaled in fp32; p_ij times the value's scale is rounded to
  * fp16 (for bf16 p_ij is rounded first; at most 2^-25 off where it is below fp16's normal
  * range; a row's largest p_ij is 1).  More: the keys and values are first written to the
- * workspace as fp16 values, fp16(s) c rounded once (for bf16 a 16th of it, and q as fp16
- * with a power of two taken off each row), and p_ij is rounded to fp16.  With fp16 queries a
- * key or value above 65504 in size counts as 65504 there: SSS_FLAG_RANGE.
+ * workspace as fp16 values, fp16(s) c rounded once (and bf16 q as fp16 with a power of two
+ * taken off each row), and p_ij is rounded to fp16.  A key or value above 65504 in size
+ * counts as 65504 there: SSS_FLAG_RANGE.
  * Errors: as sss_attention; SSS_E_UNSUPPORTED also where that copy of the cache would have
  * 2^31 slots or more.
  */

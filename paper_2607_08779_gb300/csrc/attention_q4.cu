@@ -9,7 +9,10 @@
 // keeps 11 and bf16 would keep 8 (error of the outputs, against 64 bits: 2.8e-3 to 3.4e-3 with a
 // bf16 copy, where their own rounding is 1.6e-3).  bf16 queries then go with it as fp16 numbers of
 // the same digits: each row gives off a power of two, which its scores' scale takes back.  They are
-// staged by the launch that copies the keys.
+// staged by the launch that copies the keys.  Small values lose nothing: fp16(s) c is a multiple of
+// 2^-24, fp16's least number, and is rounded where it has more than 11 bits, never below.  Large
+// ones (beyond 65504, a scale above 8188) are cut and flagged; a copy of a 16th of them, which holds
+// them all, lost four bits of what is below 2^-10 (values of about 1e-4: an error of 3e-3 against 2e-4).
 #include <algorithm>
 
 #include "attn.cuh"
@@ -122,11 +125,9 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
   if (p.of.prompt) {
     char* ws = static_cast<char*>(workspace);
     int32_t* to = reinterpret_cast<int32_t*>(ws + p.table_at);
-    // (a 16th of what bf16 or fp32 inputs can have left in the cache is in fp16's range)
     const bool bf16 = dtype == SSS_OUT_BF16;
-    const float times = bf16 ? 0.0625f : 1.f;
     float* const scales = reinterpret_cast<float*>(ws + p.scale_at);
-    Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, status, times};
+    Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, status};
     if (bf16) {
       s.q = q;
       s.q_stride = q_stride;

@@ -249,7 +249,7 @@ __device__ __forceinline__ int next_cta(uint32_t answer) {
 }
 
 // OUT: the outputs' type.  Where it is not the operands' they come from a copy whose rows of q
-// have powers of two of their own taken off (a.row_scale), and whose values are a 16th.
+// have powers of two of their own taken off (a.row_scale).
 template <typename T, int D, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_prompt_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
@@ -825,8 +825,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool in = g < w.nh && i < w.n;
       const float2 s01 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
       const float total = s01.x + s01.y;
-      constexpr float kValues = std::is_same<T, OUT>::value ? 1.f : 16.f;
-      const float r = total == 0.f ? 0.f : kValues / total;  // a row without keys: zeros
+      const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
       const float lse = total == 0.f ? -INFINITY : mx * scale + log2f(total);
       const int64_t at = static_cast<int64_t>(w.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
       const int64_t zat = static_cast<int64_t>(w.z) * a.tokens * a.heads + at;

@@ -313,7 +313,7 @@ __device__ __forceinline__ void stage_queries(const Q4Stage& a, int64_t cta, int
     *reinterpret_cast<uint4*>(static_cast<__half*>(a.q_out) + row * D + 8 * l) = u;
     // (kept above zero and below infinity, for what is multiplied by an infinity or zero)
     if (l == 0)
-      a.scales[row] = fminf(fmaxf(a.scale_log2 * __int_as_float((E - 14 + 127) << 23) / a.times, 1e-37f), 3e38f);
+      a.scales[row] = fminf(fmaxf(a.scale_log2 * __int_as_float((E - 14 + 127) << 23), 1e-37f), 3e38f);
   }
 }
 
@@ -392,8 +392,7 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
       for (int u = 0; u < kUnroll; ++u) {
         if (h + u >= h1) break;
         const uint32_t c = q4_transpose<D>(w[u], l);
-        float s = __half2float(__ushort_as_half(s16[u]));
-        if constexpr (STAGE) s *= a.stage.times;
+        const float s = __half2float(__ushort_as_half(s16[u]));
         // A nibble at bits 4 n of a float of 2^23 and more is 2^23 + 16^n u: times s / 16^n, less
         // s (2^23 / 16^n + 8).  For n = 2, 3 and 4 that constant is exact in fp32, and so is the
         // result of one multiply-add.

@@ -79,10 +79,9 @@ struct Q4Stage {
   int32_t* new_table; // [batch][pages]
   void *k, *v;        // [batch * pages * page_size][heads][dim] fp16, 65504 at most (else flagged)
   uint32_t* status;
-  float times;        // of the values: 1 or 1/16
   // bf16 queries (else null) as fp16 ones, dense, each row (token, head) with a power of two of
   // its own taken off so that its largest value is between 2^14 and 2^15; and `scale_log2`
-  // times that over `times` for each row.
+  // times that for each row.
   const void* q;
   int64_t q_stride, tokens;
   int q_heads;

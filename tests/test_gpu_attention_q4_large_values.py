@@ -23,7 +23,7 @@ def large(fresh, kv, name, scale, dtype, seed):
     return c
 
 
-@pytest.mark.parametrize("dtype", [FP])
+@pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("name", ["k", "v"])
 @pytest.mark.parametrize("scale,over", [(8188.0, False), (-8188.0, False), (8192.0, True), (-9000.0, True), (65504.0, True)])
 @pytest.mark.parametrize("fresh,kv", [([70], [300]), ([40, 1], [100, 90])])
