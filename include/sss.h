@@ -632,8 +632,9 @@ sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slot
  *   dtype [in]  of q and out: SSS_OUT_F16 or SSS_OUT_BF16.
  * A request's tokens times the heads of a group at most 64 (or single tokens): scores are
  * sums of q times the codes, scaled in fp32; p_ij times the value's scale is rounded to
- * fp16 (for bf16 p_ij is rounded first; at most 2^-25 off where it is below fp16's normal
- * range; a row's largest p_ij is 1).  More: the keys and values are first written to the
+ * fp16 (for bf16 p_ij is rounded first) with a power of two taken off the row: at most 2^-35 off
+ * where it is below fp16's normal range, a row's largest p_ij being 1, as long as the scales
+ * that the row sees are below 32, and 2^-39 of the largest scale from there on.  More: the keys and values are first written to the
  * workspace as fp16 values, fp16(s) c rounded once (and bf16 q as fp16 with a power of two
  * taken off each row), and p_ij is rounded to fp16.  A key or value above 65504 in size
  * counts as 65504 there: SSS_FLAG_RANGE.

@@ -10,6 +10,11 @@
 //   outputs  o_id = sum_j (p_ij t_jg) v'_jd, with p t rounded to fp16 for the product (for
 //            bf16 outputs p is rounded first: the product of two halves is one instruction for
 //            two rows, and an error of 2^-10 at most is a quarter of the output's own).
+// p is 2^10 where a row's score is its largest, so that p t is a normal number of fp16 down to p t =
+// 2^-24 of that: the cache's least scale.  (With p of 1 there values of 1e-4 lost up to 2 %, and many
+// keys of little weight all they had.)  Where a row sees a scale of 32 or more its p is lowered, and what
+// it has added up with it, as where its maximum is raised.  To look at a step's scales costs 1 to 2 %
+// (64 requests of 12000 to 16384 keys: 185 us without, 187).
 // A nibble u = code + 8 becomes a 16-bit operand by one AND: in bits 0-3 of a half it is the
 // (subnormal) number u 2^-24, in bits 4-7 u 2^-20, exactly.  For the keys the 8 that are too
 // much are taken off by what the sums start from, -8 times q's sums; for the values by a
@@ -69,6 +74,22 @@ struct RowsQ4Smem {
   // the splits' pieces of the values that this one joins (their number rounded up)
   static constexpr int TOTAL = RINGS + (CL ? (R * D / 4 + 16) * 16 : 0);
 };
+
+// The power of two of a row's largest p, at most kTop: lowered (to -1 at least) for a scale of 32 and more,
+// whose bits without the sign these take, so that p times a scale is below 2^15; and the
+// largest scale that leaves it as it is.
+constexpr int kTop = 10;
+__device__ __forceinline__ int top_for(int top, uint32_t scale) {
+  return min(top, 29 - min(static_cast<int>(scale >> 10), 30));
+}
+__device__ __forceinline__ uint32_t scale_for(int top) {
+  return (static_cast<uint32_t>(30 - top) << 10) - 1u;
+}
+// the larger of each half's sizes, the first not negative (a NaN counts for nothing)
+__device__ __forceinline__ uint32_t larger2(uint32_t a, uint32_t b) {
+  const __half2 v = __hmax2(*reinterpret_cast<const __half2*>(&a), __habs2(*reinterpret_cast<const __half2*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
 
 // The slot of a step that is row (or operand column) i of a tile: four slots in order for the
 // even ones, four in reverse for the odd.
@@ -165,6 +186,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
   constexpr int PER = 4 / G;    // nibble places to a group
   extern __shared__ __align__(128) unsigned char smem[];
   __shared__ float wmax[kWarps][R], wsum[kWarps][R];
+  __shared__ int lims[kWarps][R];
   __shared__ float split_lse[CL ? 16 : 1][R];  // of every split
   __shared__ uint64_t arrived;                 // what the splits store here
   __shared__ uint64_t full[kWarps][kStages];
@@ -326,6 +348,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
     // 2^(E - 14) of the scale, and the 2^24 of the nibbles'
     const float rs = fminf(fmaxf(1e-37f, a.scale_log2 * __int_as_float((min(E, 127) - 14 + 127) << 23) * 0x1p24f), 3e38f);  // (for what is multiplied by infinities)
     const int limit = in ? attn_limit(rq, i0 + i) : 0;
+    if (c == 0) lims[warp][row] = limit;
     // -8 times q's sums: products with codes that are all -8
 #pragma unroll
     for (int g = 0; g < G; ++g) {
@@ -348,7 +371,14 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
   }
 
   float o[NT][4][VW][4];  // rows 2 c, 2 c + 1 of dimensions 2 W e + w and 2 W e + W + w
-  float mx[NT][2], ref[NT][2], sum[NT][2];  // (ref: what scaled scores are added to: -mx scaled, or 0)
+  // ref: what scaled scores are added to, -mx scaled and the row's power of two, or 0
+  float mx[NT][2], ref[NT][2], sum[NT][2];
+  // The rows' powers of two are in wmax until the warps are joined, and are looked up there once one
+  // was lowered; fits2: the largest scale, twice, that leaves all of them as they are.
+  constexpr uint32_t kFits2 = ((30u - kTop) << 10) * 0x10001u - 0x10001u;
+  if (lane < R) wmax[warp][lane] = kTop;
+  __syncwarp();
+  uint32_t fits2 = kFits2;
 #pragma unroll
   for (int m = 0; m < NT; ++m) {
 #pragma unroll
@@ -383,6 +413,14 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
     const int key0 = key_of(s);
     const uint32_t blank = none >> (kBlocks * stage) & ((1u << kBlocks) - 1);
     const bool rare = key0 + kStep > lim0 || blank != 0;  // (rows that are no token's see nothing then)
+    // the values' scales: is one too large for p?  (two to a lane; for heads of 64 each to two lanes)
+    uint32_t most2 = fits2;
+#pragma unroll
+    for (int u = 0; u < kBlocks; ++u) {
+      uint32_t w;
+      lds(w, at + u * B::kBytes + B::kVS + 4 * (lane % (kQ4Slots * G / 2)));
+      most2 = larger2(most2, w);
+    }
 
     // scores
     float x[kBlocks][NT][4];
@@ -456,7 +494,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
           }
     }
     float top[NT][2];
-    bool raise = false;
+    bool raise = most2 != fits2;
 #pragma unroll
     for (int m = 0; m < NT; ++m)
 #pragma unroll
@@ -467,6 +505,33 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
         raise = raise || top[m][k] > mx[m][k];
       }
     if (__any_sync(0xffffffffu, raise)) {
+      // the step's largest scales of keys before `end`, the lane's two
+      const auto seen2 = [&](int end) {
+        uint32_t w = 0;
+#pragma unroll 1
+        for (int u = 0; u < kBlocks; ++u) {
+          const int word = lane % (kQ4Slots * G / 2), slot = word / (G / 2);
+          uint32_t v;
+          lds(v, at + u * B::kBytes + B::kVS + 4 * word);
+          if (!(blank >> u & 1u) && key0 + kQ4Slots * u + slot < end) w = larger2(w, v);
+        }
+        return w;
+      };
+      if (__any_sync(0xffffffffu, most2 != fits2) &&
+          __any_sync(0xffffffffu, larger2(fits2, seen2(lim1)) != fits2)) {  // lower p for the rows that see it
+        uint32_t high = 0;
+#pragma unroll 1
+        for (int row = 0; row < R; ++row) {
+          const uint32_t w = seen2(lims[warp][row]);
+          const uint32_t big = __reduce_max_sync(0xffffffffu, max(w & 0xFFFFu, w >> 16));
+          const int now = top_for(static_cast<int>(wmax[warp][row]), big);
+          high = max(high, static_cast<uint32_t>(now + 1));
+          __syncwarp();
+          if (lane == 0) wmax[warp][row] = static_cast<float>(now);
+        }
+        __syncwarp();
+        fits2 = scale_for(static_cast<int>(high) - 1) * 0x10001u - 1u;  // (not kFits2 again)
+      }
 #pragma unroll
       for (int m = 0; m < NT; ++m)
 #pragma unroll
@@ -474,9 +539,13 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
           float t = fmaxf(top[m][k], mx[m][k]);
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, d));
-          const float f = t == -INFINITY ? 1.f : ex2((mx[m][k] - t) * rscale[m][k]);
+          // (rounded down: no p passes its power of two, however large the scores)
+          float power = kTop;
+          if (fits2 != kFits2) power = wmax[warp][8 * m + 2 * c + k];
+          const float to = t == -INFINITY ? 0.f : __fmaf_rd(-t, rscale[m][k], power);
+          const float f = mx[m][k] == -INFINITY ? 1.f : ex2(to - ref[m][k]);
           mx[m][k] = t;
-          ref[m][k] = t == -INFINITY ? 0.f : -t * rscale[m][k];
+          ref[m][k] = to;
           sum[m][k] *= f;
 #pragma unroll
           for (int e = 0; e < 4; ++e)
@@ -606,7 +675,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
 #pragma unroll
       for (int d = 4; d < 32; d <<= 1) sum[m][k] += __shfl_xor_sync(0xffffffffu, sum[m][k], d);
       if (r == 0) {
-        wmax[warp][row] = mx[m][k] * rscale[m][k];
+        wmax[warp][row] = mx[m][k] == -INFINITY ? -INFINITY : -ref[m][k];
         wsum[warp][row] = sum[m][k];
       }
       float* dst = part + (warp * R + row) * LD + VW * r;
