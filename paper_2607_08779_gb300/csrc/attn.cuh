@@ -31,7 +31,8 @@ struct AttnArgs {
   int heads, kv_heads, group;
   int hpt, hchunks, tpt;
   int hpt_inverse;  // row * hpt_inverse >> 16 = row / hpt for rows < 32
-  int tiles;        // an upper bound of the launch's token tiles
+  int tiles;        // an upper bound of the call's token tiles
+  int tile0;        // the launch's first (a grid holds 65535)
   int one_tile;     // max_q <= tpt: tile b is request b's only one
   int table_width, page_shift;
   int chunk, nsplit;

@@ -224,12 +224,13 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
     return key < width && key < a.max_kv ? __ldg(table + (key >> a.page_shift)) : 0;
   };
   int page = 0;
-  if (a.one_tile && blockIdx.z < a.batch)
-    page = entry(a.table + static_cast<int64_t>(blockIdx.z) * a.table_width, 0);
+  const int tile = a.tile0 + blockIdx.z;
+  if (a.one_tile && tile < a.batch)
+    page = entry(a.table + static_cast<int64_t>(tile) * a.table_width, 0);
   int b, i0;
   uint32_t flags = 0;
   AttnRequest rq;
-  const bool found = attn_tile(a, blockIdx.z, b, i0, rq, flags);
+  const bool found = attn_tile(a, tile, b, i0, rq, flags);
   const int nt = found ? min(a.tpt, rq.n - i0) : 0;  // tokens of the tile
   if (nt <= 0) {
     if (flags && a.status && warp == 0) atomicOr(a.status, flags);
@@ -795,7 +796,7 @@ __global__ void __launch_bounds__(32 * WARPS, WARPS == 8 ? 1 : (NT == 1 ? 3 : 2)
 }
 
 template <typename T, int D, int NT, Split SPLIT, int WARPS>
-cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
+cudaError_t run(AttnArgs a, const Q4Cache& c, cudaStream_t stream) {
   constexpr bool CL = SPLIT == kCluster;
   auto kern = attn_rows_q4_kernel<T, D, NT, SPLIT, WARPS>;
   constexpr int smem = RowsQ4Smem<D, 8 * NT, SPLIT, WARPS>::TOTAL;
@@ -805,10 +806,7 @@ cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
     e = ensure_large_cluster(kern);
     if (e != cudaSuccess) return e;
   }
-  const dim3 grid(a.nsplit, a.kv_heads * a.hchunks, a.tiles);
-  if (grid.y > 65535 || grid.z > 65535) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
   cfg.blockDim = dim3(32 * WARPS);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = stream;
@@ -821,7 +819,12 @@ cudaError_t run(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
   attr[1].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = CL ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kern, a, c);
+  constexpr int kMost = 65535;  // of a grid's z
+  for (; e == cudaSuccess && a.tile0 < a.tiles; a.tile0 += kMost) {
+    cfg.gridDim = dim3(a.nsplit, a.kv_heads * a.hchunks, std::min(kMost, a.tiles - a.tile0));
+    e = cudaLaunchKernelEx(&cfg, kern, a, c);
+  }
+  return e;
 }
 template <typename T, int D, Split SPLIT, int WARPS = 4>
 cudaError_t tiles(const AttnArgs& a, const Q4Cache& c, cudaStream_t stream) {
