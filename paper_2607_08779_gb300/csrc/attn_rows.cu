@@ -168,12 +168,13 @@ __global__ void __launch_bounds__(kThreads, 2) attn_rows_kernel(const __grid_con
     return key < width && key < a.max_kv ? __ldg(table + (key >> a.page_shift)) : 0;
   };
   int page = 0;
-  if (a.table && a.one_tile && blockIdx.z < a.batch)
-    page = entry(a.table + static_cast<int64_t>(blockIdx.z) * a.table_width, lane);
+  const int tile = a.tile0 + blockIdx.z;
+  if (a.table && a.one_tile && tile < a.batch)
+    page = entry(a.table + static_cast<int64_t>(tile) * a.table_width, lane);
   int b, i0;
   uint32_t flags = 0;
   AttnRequest rq;
-  const bool found = attn_tile(a, blockIdx.z, b, i0, rq, flags);
+  const bool found = attn_tile(a, tile, b, i0, rq, flags);
   const int nt = found ? min(a.tpt, rq.n - i0) : 0;  // tokens of the tile
   if (nt <= 0) {
     if (flags && a.status && warp == 0) atomicOr(a.status, flags);
@@ -595,7 +596,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) attn_join_kernel(const __grid
 template <typename K>
 cudaError_t launch(K kern, const AttnArgs& a, dim3 grid, int threads, int smem,
                    cudaStream_t stream, int cluster = 1) {
-  if (grid.y > 65535 || grid.z > 65535) return cudaErrorNotSupported;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
   cfg.blockDim = dim3(threads);
@@ -614,7 +614,7 @@ cudaError_t launch(K kern, const AttnArgs& a, dim3 grid, int threads, int smem,
 }
 
 template <typename T, int D, int MT, bool CL>
-cudaError_t run_rows(const AttnArgs& a, cudaStream_t stream) {
+cudaError_t run_rows(AttnArgs a, cudaStream_t stream) {
   auto kern = attn_rows_kernel<T, D, MT, CL>;
   constexpr int smem = RowsSmem<D, 16 * MT, CL>::TOTAL;
   cudaError_t e = ensure_smem(kern, smem);
@@ -623,8 +623,11 @@ cudaError_t run_rows(const AttnArgs& a, cudaStream_t stream) {
     e = ensure_large_cluster(kern);
     if (e != cudaSuccess) return e;
   }
-  return launch(kern, a, dim3(a.nsplit, a.kv_heads * a.hchunks, a.tiles), kThreads, smem, stream,
-                a.nsplit);
+  constexpr int kMost = 65535;  // of a grid's z (more tiles than requests: only over a cache without slots)
+  for (; e == cudaSuccess && a.tile0 < a.tiles; a.tile0 += kMost)
+    e = launch(kern, a, dim3(a.nsplit, a.kv_heads * a.hchunks, std::min(kMost, a.tiles - a.tile0)), kThreads,
+               smem, stream, a.nsplit);
+  return e;
 }
 template <typename T, int D, int MT>
 cudaError_t rows_mode(const AttnArgs& a, cudaStream_t stream) {
