@@ -638,8 +638,14 @@ sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slot
  * workspace as fp16 values, fp16(s) c rounded once (and bf16 q as fp16 with a power of two
  * taken off each row), and p_ij is rounded to fp16.  A key or value above 65504 in size
  * counts as 65504 there: SSS_FLAG_RANGE.
- * Errors: as sss_attention; SSS_E_UNSUPPORTED also where that copy of the cache would have
- * 2^31 slots or more.
+ * That copy makes most of the workspace: 4 bytes a key and dimension of a key/value head, for
+ * max_kv keys (whole pages, as the table has) of each request, or of more than one request for
+ * the cache's slots where those are fewer.  It goes by the call as a whole: one request of
+ * many tokens takes the others' keys with it, so in a step that mixes chunks of prompts with single
+ * tokens, calls of their own for either (parts of cu_q, kv_len and the table's rows) are smaller
+ * and faster.
+ * Errors: as sss_attention; SSS_E_UNSUPPORTED also where batch times max_kv (whole pages, as the
+ * table has) is 2^31 or more with many rows.
  */
 sss_status_t sss_attention_q4(const void* q, int64_t q_stride, int32_t heads, int32_t dtype,
                               const sss_kv_cache_q4_t* cache, const int32_t* cu_q,

@@ -3,7 +3,9 @@
 // Few rows (single or drafted tokens) read the cache as it is: attn_rows_q4.cu.  Many rows
 // would unpack each key and value once for every tile of rows; they are unpacked once for
 // the call instead, into the workspace, and go the way of a 16-bit cache.  That writes and
-// reads 2 bytes a value, next to 4 flops a value and row: a few per cent.
+// reads 2 bytes a value, next to 4 flops a value and row: a few per cent of a batch of prompts.
+// (Of a step that mixes a chunk with single tokens it is more: max_q says which way the whole
+// call goes, so the single tokens' keys are copied too.)
 //
 // The copy is fp16 for both types of q: fp16(s) c has 14 significant bits at most, of which fp16
 // keeps 11 and bf16 would keep 8 (error of the outputs, against 64 bits: 2.8e-3 to 3.4e-3 with a
@@ -29,7 +31,7 @@ sss_kv_cache_t staged(const AttnQ4Plan& p, const sss_kv_cache_q4_t& c, int batch
   char* at = static_cast<char*>(ws);
   s.k = at + p.k_at;
   s.v = at + p.v_at;
-  s.slots = static_cast<int64_t>(batch) * p.pages * c.page_size;
+  s.slots = (p.whole ? c.pages : static_cast<int64_t>(batch) * p.pages) * c.page_size;
   s.stride = static_cast<int64_t>(c.heads) * c.dim;
   s.page_size = c.page_size;
   s.heads = c.heads;
@@ -105,10 +107,15 @@ AttnQ4Plan plan_attention_q4(int64_t tokens, int heads, const sss_kv_cache_q4_t&
     plan_rows(p.of, tokens, group, c.heads, c.dim, batch, max_q, max_kv);
     p.ws_bytes = p.of.ws_bytes;
   } else {
-    p.of = plan_attention(tokens, heads, staged(p, c, batch, nullptr), batch, max_q, max_kv);
-    const size_t bytes = static_cast<size_t>(batch) * p.pages * c.page_size * c.heads * c.dim * 2;
+    // `pages` for each request, as many as the bounds allow, or the cache's where those are fewer (the
+    // bounds of a captured step are far above its lengths: 64 requests of up to 131072 keys and 8 heads of
+    // 128 would take 32 GB, over a cache of 200,000 slots 0.8)
+    p.whole = batch > 1 && c.pages > 0 && c.pages < static_cast<int64_t>(batch) * p.pages;
+    const sss_kv_cache_t copy = staged(p, c, batch, nullptr);
+    p.of = plan_attention(tokens, heads, copy, batch, max_q, max_kv);
+    const size_t bytes = static_cast<size_t>(copy.slots) * c.heads * c.dim * 2;
     p.table_at = rounded(p.of.ws_bytes);
-    p.k_at = p.table_at + rounded(static_cast<size_t>(batch) * p.pages * 4);
+    p.k_at = p.table_at + (p.whole ? 0 : rounded(static_cast<size_t>(batch) * p.pages * 4));
     p.v_at = p.k_at + rounded(bytes);
     p.q_at = p.v_at + rounded(bytes);
     p.scale_at = p.q_at + rounded(static_cast<size_t>(tokens) * heads * c.dim * 2);
@@ -124,7 +131,7 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
                                 void* workspace, uint32_t* status, cudaStream_t stream) {
   if (p.of.prompt) {
     char* ws = static_cast<char*>(workspace);
-    int32_t* to = reinterpret_cast<int32_t*>(ws + p.table_at);
+    int32_t* to = p.whole ? nullptr : reinterpret_cast<int32_t*>(ws + p.table_at);
     const bool bf16 = dtype == SSS_OUT_BF16;
     float* const scales = reinterpret_cast<float*>(ws + p.scale_at);
     Q4Stage s = {kv_len, table, width, batch, p.pages, max_kv, to, ws + p.k_at, ws + p.v_at, status};
@@ -142,8 +149,8 @@ cudaError_t launch_attention_q4(const AttnQ4Plan& p, const void* q, int64_t q_st
     const cudaError_t e = launch_kv_stage_q4(q4_cache(c), c.dim, s, stream);
     if (e != cudaSuccess) return e;
     return launch_attention(p.of, q, q_stride, heads, staged(p, c, batch, ws), cu_q, kv_len,
-                            to, p.pages, batch, tokens, max_q, max_kv, scale, out, ws, status, stream,
-                            bf16 ? scales : nullptr);
+                            p.whole ? table : to, p.whole ? width : p.pages, batch, tokens, max_q, max_kv,
+                            scale, out, ws, status, stream, bf16 ? scales : nullptr);
   }
   AttnArgs a = {};
   a.q = q;

@@ -317,8 +317,8 @@ __device__ __forceinline__ void stage_queries(const Q4Stage& a, int64_t cta, int
   }
 }
 
-// As the store's grid, of rows.  STAGE: blockIdx.z is a request; row t of the copy is its key
-// t, in a page of its own.  QUERIES: the grid's rows behind the 2 * runs are the queries' (a variant
+// As the store's grid, of rows.  STAGE: blockIdx.z is a request, t its key t, in a page of its own
+// of the copy, or in the cache's place.  QUERIES: the grid's rows behind the 2 * runs are the queries' (a variant
 // of its own, as the others take 1 us more with it).
 template <typename T, int D, bool STAGE, bool QUERIES>
 __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_constant__ FetchArgs a) {
@@ -352,13 +352,14 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
     const bool real = page >= 0 && page < a.cache.slots >> shift;
     // the copy's table, of the pages that are real (what is none, and keys past the
     // request's, are the attention's to flag; what fp16 does not hold is flagged here)
-    if (blockIdx.y == 0 && lane == 0 && (first & ((1 << shift) - 1)) == 0)
+    if (s.new_table != nullptr && blockIdx.y == 0 && lane == 0 && (first & ((1 << shift) - 1)) == 0)
       s.new_table[static_cast<int64_t>(b) * s.pages + p] = real ? b * s.pages + static_cast<int32_t>(p) : -1;
     const int64_t keys = min(static_cast<int64_t>(s.kv_len[b]), s.max_kv);
     if (!real || first >= keys) return;
     in = t < keys;
-    row += static_cast<int64_t>(b) * s.pages << shift;
     slot = (static_cast<int64_t>(page) << shift) + (t & ((1 << shift) - 1));
+    // (a page that requests share is copied by each of them: the same bytes)
+    row = s.new_table != nullptr ? row + (static_cast<int64_t>(b) * s.pages << shift) : slot;
   } else if (in) {
     slot = a.slots ? a.slots[t] : t;
     if (slot >= a.cache.slots) {

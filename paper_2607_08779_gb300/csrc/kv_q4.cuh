@@ -70,14 +70,15 @@ __device__ __forceinline__ uint32_t q4_transpose(uint32_t v, int l) {
 }
 
 // What sss_attention_q4 leaves of its requests' keys and values for the form of many rows:
-// 16-bit values in pages of its own, request b's from page b * pages on, and their table.
+// 16-bit values in pages of its own, request b's from page b * pages on, and their table; or in
+// the cache's pages, where the cache has fewer.
 struct Q4Stage {
   const int32_t *kv_len, *table;
   int table_width, batch;
   int pages;          // of a request
   int64_t max_kv;
-  int32_t* new_table; // [batch][pages]
-  void *k, *v;        // [batch * pages * page_size][heads][dim] fp16, 65504 at most (else flagged)
+  int32_t* new_table; // [batch][pages], or null: the cache's pages
+  void *k, *v;        // [slots][heads][dim] fp16, 65504 at most (else flagged)
   uint32_t* status;
   // bf16 queries (else null) as fp16 ones, dense, each row (token, head) with a power of two of
   // its own taken off so that its largest value is between 2^14 and 2^15; and `scale_log2`

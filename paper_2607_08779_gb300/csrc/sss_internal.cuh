@@ -117,6 +117,7 @@ cudaError_t launch_kv_fetch_q4(const sss_kv_cache_q4_t& cache, const int32_t* sl
 struct AttnQ4Plan {
   AttnPlan of;     // its rows' form, or that of the 16-bit copy in the workspace
   int pages;       // of the copy, for each request
+  bool whole;      // the copy is of the cache's pages instead, those that the requests hold
   size_t table_at, k_at, v_at;  // the copy: its table, keys, values
   size_t q_at, scale_at;        // and for bf16 the queries and their rows' scales
   size_t ws_bytes;
