@@ -636,7 +636,8 @@ sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slot
  * where it is below fp16's normal range, a row's largest p_ij being 1, as long as the scales
  * that the row sees are below 32, and 2^-39 of the largest scale from there on.  More: the keys and values are first written to the
  * workspace as fp16 values, fp16(s) c rounded once (and bf16 q as fp16 with a power of two
- * taken off each row), and p_ij is rounded to fp16.  A key or value above 65504 in size
+ * taken off each row), and p_ij is rounded to fp16 (a row's largest being 1 to 2^8; for bf16 with
+ * a power of two more, so lost below 2^-32 only).  A key or value above 65504 in size
  * counts as 65504 there: SSS_FLAG_RANGE.
  * That copy makes most of the workspace: 4 bytes a key and dimension of a key/value head, for
  * max_kv keys (whole pages, as the table has) of each request, or of more than one request for

@@ -249,7 +249,8 @@ __device__ __forceinline__ int next_cta(uint32_t answer) {
 }
 
 // OUT: the outputs' type.  Where it is not the operands' they come from a copy whose rows of q
-// have powers of two of their own taken off (a.row_scale).
+// have powers of two of their own taken off (a.row_scale); p is 2^kUp times as large then, 2^15
+// at most, so that as an fp16 number it is lost below 2^-32 of the row's largest, not below 2^-25.
 template <typename T, int D, typename OUT>
 __global__ void __launch_bounds__(kThreads, 1)
     attn_prompt_kernel(const __grid_constant__ AttnMaps maps, const __grid_constant__ AttnArgs a) {
@@ -736,6 +737,12 @@ __global__ void __launch_bounds__(kThreads, 1)
         scale = in ? __ldg(a.row_scale + static_cast<int64_t>(w.q0 + w.i0 + ti) * a.heads + w.kh * a.group + w.g0 + g) : 1.f;
       whole = attn_limit(rq, min(w.i0 + s * tt, w.n - 1));
     };
+    // what a scaled score is added to
+    constexpr float kUp = std::is_same<T, OUT>::value ? 0.f : 7.f;
+    const auto less = [&](float mx) {
+      if constexpr (kUp == 0.f) return mx == -INFINITY ? 0.f : -mx * scale;
+      return mx == -INFINITY ? 0.f : __fmaf_rd(-mx, scale, kUp);  // (down: p stays in range however large the scores)
+    };
     begin(0);
     for (int item = 0; more; ++item) {
       float mx = -INFINITY;
@@ -798,7 +805,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        const float neg = mx == -INFINITY ? 0.f : -mx * scale;
+        const float neg = less(mx);
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           uint32_t p[16];
@@ -826,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const float2 s01 = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
       const float total = s01.x + s01.y;
       const float r = total == 0.f ? 0.f : 1.f / total;  // a row without keys: zeros
-      const float lse = total == 0.f ? -INFINITY : mx * scale + log2f(total);
+      const float lse = total == 0.f ? -INFINITY : (kUp == 0.f ? mx * scale : -less(mx)) + log2f(total);
       const int64_t at = static_cast<int64_t>(w.q0 + i) * a.heads + w.kh * a.group + w.g0 + g;
       const int64_t zat = static_cast<int64_t>(w.z) * a.tokens * a.heads + at;
       const uint32_t rows_in = __ballot_sync(0xffffffffu, in);

@@ -86,6 +86,17 @@ def test_small_values_of_many_rows(dtype, step, fresh, kv, hq, hkv, dim):
     check(c, call(c, scale=scale), scale)
 
 
+@pytest.mark.parametrize("fresh,kv,hq,hkv,dim", [([70], [4000], 8, 2, 128), ([33, 90], [2900, 700], 4, 1, 64)])
+@pytest.mark.parametrize("gap", [20, 27])
+def test_keys_of_very_little_weight_in_many_rows(fresh, kv, hq, hkv, dim, gap):
+    # bf16 queries: p is lost below 2^-32 of the row's largest (and rounded by 2^-33 of it, times a value of 8 steps)
+    c, scale = flat_but_one(fresh, kv, hq, hkv, dim, BF, 1.0, gap, seed=84)
+    got = call(c, scale=scale).double().numpy()
+    w = q4_plain.attention(c["q"], c["k"], c["v"], c["cu"], c["kv"], c["rows"], scale)
+    limit = bound(w, BF, dim, 0, True) + max(kv) * 2.0 ** -23 * w["size"] + max(kv) * 2.0 ** -30 * w["most"][..., None]
+    assert np.max(np.abs(got - w["out"]) / limit) <= 1.0
+
+
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("size", [1e-6, 1e-4, 1e-3])
 @pytest.mark.parametrize("fresh,kv", [([1, 1], [700, 90]), ([2, 1], [1500, 33]), ([70, 5], [300, 80])])
