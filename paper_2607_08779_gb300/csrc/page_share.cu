@@ -314,6 +314,7 @@ __global__ void __launch_bounds__(kForkThreads, 1) page_fork_kernel(const __grid
 constexpr int kMapThreads = 1024;
 constexpr int kMapCtas = 16;
 constexpr int kSpan = 8;  // words of the map to one running count
+constexpr int kMapPiece = 512;  // entries that a warp takes at a time (128: 16.0 us for the last case above)
 
 struct MapArgs {
   const int32_t *table, *past;
@@ -352,7 +353,7 @@ __global__ void __launch_bounds__(kMapThreads, 1) page_map_kernel(const __grid_c
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   __syncthreads();
   // the rows' entries, a warp to a piece of them
-  constexpr int kWarps = kMapThreads / 32, kPiece = 512;  // (128: 16.0 us, 13.6 so)
+  constexpr int kWarps = kMapThreads / 32, kPiece = kMapPiece;
   const int pieces = (a.width + kPiece - 1) / kPiece;
   const int64_t items = static_cast<int64_t>(a.batch) * pieces;
   for (int64_t i = static_cast<int64_t>(me) * kWarps + warp; i < items; i += static_cast<int64_t>(ctas) * kWarps) {
@@ -608,12 +609,14 @@ cudaError_t launch_page_reclaim(const int32_t* table, int width, const int32_t* 
   const int smem = spans * (kSpan * 4 + 4 + kSpan);
   cudaError_t e = ensure_smem(page_map_kernel, kMaxMapPages / (32 * kSpan) * (kSpan * 4 + 4 + kSpan));
   if (e != cudaSuccess) return e;
-  // a CTA for every three rounds of its warps over the table or the map (16 requests of up to
-  // 4096 tokens: 4.2 us with one CTA, 5.2 with two; 256 of up to 16384: 160 us with one, 47 with
-  // four, 28 with eight, 18 with sixteen)
-  const int64_t work = std::max<int64_t>(static_cast<int64_t>(batch) * ((width + 127) / 128), spans);
+  // CTAs until three of four of their warps, at most, have a piece of the table, or a span of the map
+  // (16 requests of up to 4096 tokens: 4.6 us with one CTA, 6.1 with two.  64 of up to 8192 with moves: 33.2,
+  // 21.3, 13.5, 12.4 and 12.0 us with 1, 2, 4, 8 and 16; 256 of up to 16384: 91.7, 53.2, 30.7, 19.1 and
+  // 13.6.  From 48 pieces a CTA on instead: 256 of up to 1000 tokens 10.9 us, so 10.1; 8 of up to 32768
+  // 18.5, so 14.4.)
+  const int64_t work = std::max<int64_t>(static_cast<int64_t>(batch) * ((width + kMapPiece - 1) / kMapPiece), spans);
   int ctas = 1;
-  while (ctas < kMapCtas && work > ctas * 96) ctas *= 2;
+  while (ctas < kMapCtas && work > ctas * 24) ctas *= 2;
   if (ctas > 8) {
     e = ensure_large_cluster(page_map_kernel);
     if (e != cudaSuccess) return e;
