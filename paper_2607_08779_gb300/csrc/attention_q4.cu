@@ -55,8 +55,11 @@ void plan_rows(AttnPlan& p, int64_t tokens, int group, int kv_heads, int dim, in
   // How many CTAs (a cluster of them) share a tile's keys, and of how many warps.  Few tiles: one
   // CTA of 8 warps an SM, as many as that leaves room for (one request of 8192 keys and one
   // key/value head: 6.2 us, 7.5 with 4 warps; 4 of 1400 to 4096 and 8 heads 8.4 and 9.6; 8 of 500 to
-  // 1500 7.1 and 8.4), but for 16 tiles of long requests, where more of 4 warps find room (2 of
-  // 2700 to 8192 and 8 heads: 10.7 us in sixteens, 12.6).  More tiles: CTAs of 4 warps, three
+  // 1500 7.1 and 8.4), but for 9 to 16 tiles of long requests, where clusters of 16 (or 8) CTAs of 4
+  // warps find room, four CTAs of 8 being half a wave (up to 8192 keys, 9, 10, 12, 16 and 16 tiles: 8.4, 8.6,
+  // 10.4, 10.4 and 11.9 us so, 12.6, 12.6, 12.6, 12.5 and 13.0 with 8; up to 4096 6.4 to 8.8 and 8.3 to
+  // 8.6; up to 3000 and 16 tiles 7.3 to 8.5 and 7.2 to 7.5; 8 tiles of up to 4096 6.4 to 7.2 and 6.3 to 6.5, 24
+  // and 32 12.0 and 13.0, and 8.4 and 8.7).  More tiles: CTAs of 4 warps, three
   // an SM; more waves of them cost 2 to 5 us each (64 requests of 300 to 500 keys and 8
   // heads: 12.5 us whole, 20.4 in pairs; 32 of 256 to 2000: 21.0 whole, 17.6 in pairs; 16 of 270 to
   // 800: 8.4 in pairs, 10.8 in fours).  Each CTA but one has 128 keys (one request of 500:
