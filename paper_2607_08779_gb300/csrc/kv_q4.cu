@@ -279,6 +279,15 @@ __device__ __forceinline__ void store8(T* p, float (&f)[8], bool in) {
   }
 }
 
+// the same as fp16 values, 65504 at most
+__device__ __forceinline__ void store8_finite(__half* p, const float (&f)[8], bool in) {
+  uint32_t h[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;" : "=r"(h[i]) : "f"(f[2 * i + 1]), "f"(f[2 * i]));
+  if (in) *reinterpret_cast<uint4*>(p) = make_uint4(h[0], h[1], h[2], h[3]);
+}
+
 // Queries for the copy (see Q4Stage): a row of D values is D / 8 lanes.  CTA `cta` of `ctas`.
 template <int D>
 __device__ __forceinline__ void stage_queries(const Q4Stage& a, int64_t cta, int64_t ctas) {
@@ -315,6 +324,25 @@ __device__ __forceinline__ void stage_queries(const Q4Stage& a, int64_t cta, int
     if (l == 0)
       a.scales[row] = fminf(fmaxf(a.scale_log2 * __int_as_float((E - 14 + 127) << 23), 1e-37f), 3e38f);
   }
+}
+
+// Whether one of a lane's values of these heads is beyond fp16's range, by whole warps.  (Inlined, or as a
+// test of each value where it is written, prompts of 4000 tokens and 32 heads took 123 us, so 120.)
+template <int D>
+__device__ __noinline__ uint32_t range_flags(const char* head, int per_head, int heads, int code_at,
+                                             int scale_at, bool in) {
+  const int l = threadIdx.x % (D / 8);
+  uint32_t flags = 0;
+#pragma unroll 1
+  for (int h = 0; h < heads; ++h, head += per_head) {
+    uint32_t c = in ? __ldg(reinterpret_cast<const uint32_t*>(head + code_at)) : 0x88888888u;
+    const float s = in ? __half2float(__ushort_as_half(__ldg(reinterpret_cast<const uint16_t*>(head + scale_at)))) : 0.f;
+    c = q4_transpose<D>(c, l);
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e)
+      if (fabsf(s) * fabsf(static_cast<float>(c >> (4 * e) & 15u) - 8.f) > 65504.f) flags |= SSS_FLAG_RANGE;
+  }
+  return flags;
 }
 
 // As the store's grid, of rows.  STAGE: blockIdx.z is a request, t its key t, in a page of its own
@@ -376,6 +404,7 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
                        static_cast<int64_t>(h0) * per_head + (is_v ? B::kV : B::kK);
     const int code_at = j * B::kRow + 4 * (is_v ? q4_value_word<D>(word, j) : word);
     const int scale_at = B::kKS + j * B::kScales + 2 * (l >> 2);
+    uint32_t most = 0;  // of the scales' sizes (of the copy's alone)
     for (int h = h0; h < h1; h += kUnroll) {
       uint32_t w[kUnroll];
       uint16_t s16[kUnroll];
@@ -408,19 +437,19 @@ __global__ void __launch_bounds__(kThreads) kv_fetch_q4_kernel(const __grid_cons
         for (int e = 0; e < 8; ++e)
           f[e] = __fmaf_rn(__uint_as_float((part[e / 3] & (15u << (4 * (e % 3 + 2)))) | 0x4B000000u),
                            by[e % 3], less[e % 3]);
-        if constexpr (STAGE) {  // (a scale of 8188 or less keeps the copy in fp16's range)
-          if ((s16[u] & 0x7fffu) > 0x6FFFu && (s16[u] & 0x7fffu) < 0x7C00u) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              if (fabsf(f[e]) <= 65504.f) continue;
-              f[e] = copysignf(65504.f, f[e]);
-              flags |= SSS_FLAG_RANGE;
-            }
-          }
+        if constexpr (STAGE) {
+          most = max(most, s16[u] & 0x7fffu);
+          store8_finite(out, f, in);
+        } else {
+          store8(out, f, in);
         }
-        store8(out, f, in);
         out += D;
       }
+    }
+    // a scale of 8188 or less keeps the copy in fp16's range; else the warp looks for what was cut
+    if (STAGE && __any_sync(0xffffffffu, most > 0x6FFFu)) {
+      const int steps = (h1 - h0 + kUnroll - 1) / kUnroll;
+      flags |= range_flags<D>(head - static_cast<int64_t>(steps) * kUnroll * per_head, per_head, h1 - h0, code_at, scale_at, in);
     }
   }
   if (flags && a.status) atomicOr(a.status, flags);
