@@ -27,11 +27,11 @@
 // 128 are 2304 bytes, which an SM's share of the bandwidth brings in 96 cycles.  Four
 // schedulers have 384 issue slots in that time; the step takes about 280 with 8 columns, 16 of
 // them products that keep a scheduler for 7 cycles each.  64 requests of 12000 to 16384 keys (32
-// heads of 128 over 8): 185 us, 5.6 TB/s, 84 % of the copy rate (the copies without the
+// heads of 128 over 8): 187 us, 5.6 TB/s, 83 % of the copy rate (the copies without the
 // arithmetic run at 105 %); 16 of 130 to 16384 (64 heads) 30.9, the longest ones' chunks and the
-// second kernel being last; one of 2047 keys 4.8.  With 16 columns 32 requests of 16384 keys
-// and 4 heads take 100 us, 45 % of that rate; a CTA more an SM with heads of 64 (64 requests of
-// 8000 to 16384 keys: 107 us, 99.6).  What did not help: the next step's scores beside
+// second kernel being last; one of 2047 keys 5.1.  With 16 columns 32 requests of 16384 keys
+// and 4 heads take 99 us, 45 % of that rate; heads of 64 (64 requests of 8000 to 16384 keys) 102, a CTA
+// more an SM having taken 7 % off.  What did not help: the next step's scores beside
 // this one's outputs (236 us against 233 at the time), four CTAs an SM with shorter rings (249),
 // 16 keys a step (244 against 216).
 // A block of the cache is one bulk copy into a ring that each warp has for itself, with a

@@ -12,8 +12,8 @@
 // adding to two addresses.  (Tokens beside each other and not heads: no lane is idle whatever
 // their number, and slots in order share sectors.)
 //
-// 8191 tokens of 8 heads of 128 in bf16: store 10.8 us, 4.0 TB/s (issue slots 72 % taken, the
-// integer pipe 66 %), fetch 7.0 us, 6.2 TB/s; in fp32 13.9 and 10.2 us, 5.5 TB/s.  16 tokens: 1.8
+// 8191 tokens of 8 heads of 128 in bf16: store 10.9 us, 3.9 TB/s (issue slots 69 % taken, the
+// integer pipe 64 %), fetch 6.9 us, 6.2 TB/s; in fp32 13.5 and 10.3 us.  16 tokens: 1.8
 // and 1.5 us, a launch.  With the next token's loads in flight in resident warps 18.4 and 14.0.
 #include <algorithm>
 
