@@ -433,6 +433,8 @@ typedef struct {
  *   block_table  [in,out] device int32 [batch][table_width]: entries below
  *                      ceil(past / page_size) are read, the taken pages' written,
  *                      others left alone.
+ *                      A partly filled last page is written to by the new tokens: no
+ *                      other request may hold it (sss_page_fork sees to that).
  *   cu_q         [out] device int32 [batch + 1]: the first token of each request
  *                      among the step's, and their number.
  *   kv_len       [out] device int32 [batch]: past + fresh (of the tokens that cu_q has).

@@ -100,3 +100,15 @@ def test_rows_that_were_rolled_back_write_apart():
             assert torch.equal(got[:n], before[b]) and torch.equal(got[n], held[b])
         assert int(status) == 0
         sss.sss_kv_store_q4(start, start, cache, slots)
+
+
+def test_tables_without_columns_and_wide_ones():
+    got, status = call_fork([0, 0, 1], [0, 0], 16, [3], np.zeros((2, 0), np.int64))
+    assert status == 0 and got[1].tolist() == [0, 0, 0] and got[4].tolist() == [0]
+    got, status = call_fork([0], [5], 16, [3], np.zeros((1, 0), np.int64))
+    assert status == sss.FLAG_INDEX and got[1].tolist() == [0]
+    rng = np.random.default_rng(7)
+    table = rng.permutation(600000).reshape(2, 300000)
+    table[1, :200000] = table[0, :200000]
+    for past in ([16 * 200000 - 3, 16 * 199999 + 2], [16 * 250000 + 1, 16 * 100000 + 7], [16 * 300000, 16 * 300000 - 1]):
+        check([0, 1, 0], past, 16, np.arange(600000, 600010), table)
