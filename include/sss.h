@@ -633,20 +633,21 @@ sss_status_t sss_kv_fetch_q4(const sss_kv_cache_q4_t* cache, const int32_t* slot
  * and values are in the cache, as the others are.
  *   dtype [in]  of q and out: SSS_OUT_F16 or SSS_OUT_BF16.
  * A request's tokens times the heads of a group at most 64 (or single tokens): scores are
- * sums of q times the codes, scaled in fp32; p_ij times the value's scale is rounded to
- * fp16 (for bf16 p_ij is rounded first) with a power of two taken off the row: at most 2^-35 off
- * where it is below fp16's normal range, a row's largest p_ij being 1, as long as the scales
- * that the row sees are below 32, and 2^-39 of the largest scale from there on.  More: the keys and values are first written to the
- * workspace as fp16 values, fp16(s) c rounded once (and bf16 q as fp16 with a power of two
- * taken off each row), and p_ij is rounded to fp16 (a row's largest being 1 to 2^8; for bf16 with
- * a power of two more, so lost below 2^-32 only).  A key or value above 65504 in size
- * counts as 65504 there: SSS_FLAG_RANGE.
+ * sums of q times the codes, scaled in fp32; p_ij times the value's scale is rounded to fp16
+ * (for bf16 p_ij is rounded first) with a power of two taken off the row: below fp16's normal
+ * range it is at most 2^-35 off, a row's largest p_ij being 1, as long as the scales that the
+ * row sees are below 32, and 2^-39 of the largest scale from there on.
+ * More: the keys and values are first written to the workspace as fp16 values, fp16(s) c
+ * rounded once (and bf16 q as fp16 with a power of two taken off each row), and p_ij is rounded
+ * to fp16 (a row's largest being 1 to 2^8; for bf16 with a power of two more, so lost below
+ * 2^-32 only).  A key or value above 65504 in size counts as 65504 there: SSS_FLAG_RANGE.
  * That copy makes most of the workspace: 4 bytes a key and dimension of a key/value head, for
  * max_kv keys (whole pages, as the table has) of each request, or of more than one request for
  * the cache's slots where those are fewer.  It goes by the call as a whole: one request of
- * many tokens takes the others' keys with it, so in a step that mixes chunks of prompts with single
- * tokens, calls of their own for either (parts of cu_q, kv_len and the table's rows) are smaller
- * and faster.
+ * many tokens takes the others' keys with it, so in a step that mixes chunks of prompts with
+ * single tokens, calls of their own for either (parts of cu_q, kv_len and the table's rows)
+ * are smaller and faster (63 single tokens of 12000 to 16384 keys and a chunk of 512 after 4000:
+ * 1508 us and 3.7 GB in one, 241 us and 0.12 GB in two).
  * Errors: as sss_attention; SSS_E_UNSUPPORTED also where batch times max_kv (whole pages, as the
  * table has) is 2^31 or more with many rows.
  */
